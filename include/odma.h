@@ -351,6 +351,86 @@ int odma_prefill_attention(odma_pool_t* pool, int32_t layer, int32_t n, const vo
                            const int32_t* lengths, const int32_t* block_table, int32_t bt_stride,
                            void* out, void* stream);
 
+/* ---- preparing a batch, and attention over shared prefixes -----------------------------------------------------------
+ *
+ * Prefixes.  Requests whose first tokens are the same may share their K/V: prefix p sits once in a slab of its own
+ * (prefix_offsets[p], filled like any request's), and requests prefix_start[p] .. prefix_start[p + 1] - 1 of the batch begin
+ * with it (prefix_start does not decrease; requests before the first or behind the last start have no prefix).  What they
+ * share is the prefix's whole blocks, S = prefix_lengths[p] rounded down to a multiple of 16 tokens; the tokens behind them
+ * are each request's own and fill its own slab from its beginning.  So token t of a request sits at prefix_offsets[p] + t
+ * for t < S and at offsets[r] + t - S otherwise, and lengths[r] counts them all, shared ones included.
+ *   prefix_start DEVICE int32[n_prefixes + 1]   prefix_offsets DEVICE int64[n_prefixes]   prefix_lengths DEVICE int32[n_prefixes]
+ * (all three may be NULL with n_prefixes 0; 0 <= n_prefixes <= n). */
+#define ODMA_SLOT_NONE    (-1)   /* odma_append_qkv: the row is not there, nothing of it is read or written */
+#define ODMA_SLOT_SHARED  (-2)   /* the row's K and V are in a shared block already: only its queries are prepared */
+
+/* Tables of a batch from its lengths, in one launch and without the host: what the paged calls, odma_prefill_attention and
+ * odma_append_qkv read.  Request r brings n_new[r] new tokens, the last of its lengths[r].
+ *   lengths      DEVICE int32[n], new tokens included (0: a place of the batch that is empty)
+ *   n_new        DEVICE int32[n], taken as 0 to lengths[r], or NULL (one each, none where the length is 0)
+ *   offsets      DEVICE int64[n]
+ *   block_table  DEVICE int32[n][bt_stride] or NULL: the blocks of every request in order, shared ones first; entries behind the
+ *                last block, and of empty places, are 0.  A request with more blocks than bt_stride gets its first ones.
+ *   row_start    DEVICE int64[n + 1] or NULL: the exclusive sum of n_new, and the sum behind it: q_start of odma_prefill_attention,
+ *                src_start of odma_append_kv
+ *   row_position DEVICE int32[max_rows] or NULL, row_slot DEVICE int64[max_rows] or NULL: for every new row, requests in order,
+ *                its token index and the pool slot of its K/V (ODMA_SLOT_SHARED for a shared token); rows behind the
+ *                last request's get 0 and ODMA_SLOT_NONE, rows at or past max_rows do not exist
+ * n must not exceed max_requests; n = 0 writes nothing.  Uses no workspace: calls may overlap as far as their arrays allow. */
+int odma_build_tables(odma_pool_t* pool, int32_t n, const int32_t* lengths, const int32_t* n_new, const int64_t* offsets,
+                      int32_t n_prefixes, const int32_t* prefix_start, const int64_t* prefix_offsets,
+                      const int32_t* prefix_lengths, int32_t* block_table, int32_t bt_stride, int64_t max_rows,
+                      int64_t* row_start, int32_t* row_position, int64_t* row_slot, void* stream);
+
+/* How odma_append_qkv prepares queries and keys. */
+#define ODMA_ROT_HALVES      0    /* pair f: channels f and rot_dim / 2 + f */
+#define ODMA_ROT_ADJACENT    1    /* pair f: channels 2 f and 2 f + 1 */
+#define ODMA_MAX_AXES        4
+#define ODMA_MAX_ROT_PAIRS 128
+typedef struct odma_qk_prep {
+  const void*  q_weight;     /* DEVICE [head_dim], type of the rows; NULL: queries are not normed */
+  const void*  k_weight;     /* the same for keys */
+  const float* inv_freq;     /* DEVICE [rot_dim / 2]: radians per position of every pair */
+  float   eps;               /* of the norms, finite and >= 0 */
+  int32_t rot_dim;           /* channels that turn, from the first one on: a multiple of 8 up to head_dim; 0: none */
+  int32_t rot_pairs;         /* ODMA_ROT_* */
+  int32_t n_axes;            /* 1..ODMA_MAX_AXES: positions of a row (time, height, width) */
+  uint8_t axis[ODMA_MAX_ROT_PAIRS];   /* of every pair: which of the positions turns it, < n_axes */
+} odma_qk_prep_t;
+
+/* From the projections to the pool, in one pass: for every row and head, queries and keys are normed (root mean square over
+ * the head, times the weights), then turned by the row's positions; queries go to q_out, keys and values into the
+ * slot of the row.  All in fp32, rounded once when stored; angles are formed in 64 bits.  ODMA_FP8 pools take bf16 rows and
+ * store value * (1 / k_scale or 1 / v_scale) as E4M3, to nearest even, beyond the range the largest value.
+ *   q, k, v     DEVICE rows of [Hq][D], [Hkv][D], [Hkv][D], in fp32 for ODMA_F32 pools, else bf16; row i at element
+ *               i * q_stride (k_stride, v_stride): parts of one projection's rows, for instance.  Pointers and strides are
+ *               multiples of 16 bytes
+ *   row_slot    DEVICE int64[n_rows]: token slot of each row in the pool (odma_build_tables), ODMA_SLOT_NONE or
+ *               ODMA_SLOT_SHARED.  Slots past the pool are taken as ODMA_SLOT_NONE, other negative ones as ODMA_SLOT_SHARED.  No two rows may have the same slot (both
+ *               would be written, in any order)
+ *   positions   DEVICE int32[n_axes][n_rows] (NULL with rot_dim 0)
+ *   q_out       DEVICE [n_rows][Hq][D], type of the rows; may be q itself where q_stride is Hq * D, else apart from q, k, v
+ * Other slots of the pool keep what they hold.  Uses no workspace.  Capacity is the caller's business (odma_advance). */
+int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma_qk_prep_t* prep, const void* q,
+                    int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                    const int64_t* row_slot, const int32_t* positions, void* q_out, void* stream);
+
+/* Decode attention of a batch that shares prefixes: odma_decode_attention's result for every request's tokens, shared and
+ * own, with a prefix's K/V read for all its requests together -- their queries against it are one matrix product.
+ *   q, out      as for odma_decode_attention; lengths with the shared tokens (0: an empty place, zeros)
+ *   offsets     DEVICE int64[n], slabs of the own tokens (ignored when block_table != NULL)
+ *   block_table DEVICE int32[n][bt_stride] or NULL: every request's blocks, shared ones first (odma_build_tables); prefix_offsets
+ *               is then ignored (NULL allowed): a prefix is read through the row of one of its requests
+ * A request shorter than what its group shares attends to its lengths[r] first tokens.  n_prefixes = 0: odma_decode_attention.
+ * Matrix-core pools only (bf16 with head_dim 128 or 64, fp8), n <= ODMA_SHARED_MAX_REQUESTS; ODMA_INVALID_ARG otherwise.
+ * Partial results live in the pool's workspace: such calls must not overlap on different streams with each other, with
+ * decode calls or with odma_prefill_attention on the null stream.  A plan that decode calls may reuse survives. */
+#define ODMA_SHARED_MAX_REQUESTS 1024
+int odma_decode_attention_shared(odma_pool_t* pool, int32_t layer, int32_t n, const void* q, int32_t n_prefixes,
+                                 const int32_t* prefix_start, const int64_t* prefix_offsets, const int32_t* prefix_lengths,
+                                 const int64_t* offsets, const int32_t* lengths, const int32_t* block_table, int32_t bt_stride,
+                                 void* out, void* stream);
+
 /* Export of one request's KV in plain row-major order: k_out, v_out DEVICE
  * [length][Hkv][D] in kv_dtype.  block_row (DEVICE int32[]) selects the paged layout. */
 int odma_gather_kv(odma_pool_t* pool, int32_t layer, int64_t offset, int32_t length,

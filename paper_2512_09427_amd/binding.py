@@ -29,6 +29,10 @@ TUNE_ODD_XCD_WEIGHT = 6
 TUNE_LATE_WAVE_WEIGHT = 7
 TUNE_FUSE_REDUCE = 8
 TUNE_PREFILL_COLUMN_TILES = 9
+SLOT_NONE, SLOT_SHARED = -1, -2
+ROT_HALVES, ROT_ADJACENT = 0, 1
+MAX_AXES, MAX_ROT_PAIRS = 4, 128
+SHARED_MAX_REQUESTS = 1024
 
 EXPORTS = [
     "odma_workspace_bytes", "odma_pool_create", "odma_pool_destroy", "odma_inflate", "odma_assign",
@@ -38,7 +42,7 @@ EXPORTS = [
     "odma_pool_tune", "odma_decode_step", "odma_stream_read_probe", "odma_recalibrator_start",
     "odma_report_completions", "odma_recalibrator_drain", "odma_recalibrator_stop", "odma_migrate_batch",
     "odma_migrate_finish", "odma_prefill_attention", "odma_block_read_probe", "odma_stream_plan_ranges",
-    "odma_decode_attention_static",
+    "odma_decode_attention_static", "odma_build_tables", "odma_append_qkv", "odma_decode_attention_shared",
 ]
 
 
@@ -61,6 +65,13 @@ class odma_pool_config_t(C.Structure):
         ("sm_scale", C.c_float), ("max_splits", C.c_int32),
         ("k_scale", C.c_float), ("v_scale", C.c_float),
         ("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class odma_qk_prep_t(C.Structure):
+    _fields_ = [
+        ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("inv_freq", C.c_void_p), ("eps", C.c_float),
+        ("rot_dim", C.c_int32), ("rot_pairs", C.c_int32), ("n_axes", C.c_int32), ("axis", C.c_uint8 * MAX_ROT_PAIRS),
     ]
 
 
@@ -107,6 +118,10 @@ def _load() -> C.CDLL:
         "odma_prefill_attention": (C.c_int, [vp, C.c_int32, C.c_int32, vp, C.c_int64, vp, vp, vp, vp, vp, C.c_int32, vp, vp]),
         "odma_decode_step": (C.c_int, [vp, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp, C.c_int32, vp, C.c_uint32, vp]),
         "odma_gather_kv": (C.c_int, [vp, C.c_int32, C.c_int64, C.c_int32, vp, vp, vp, vp]),
+        "odma_build_tables": (C.c_int, [vp, C.c_int32, vp, vp, vp, C.c_int32, vp, vp, vp, vp, C.c_int32, C.c_int64, vp, vp, vp, vp]),
+        "odma_append_qkv": (C.c_int, [vp, C.c_int32, C.c_int64, C.POINTER(odma_qk_prep_t), vp, C.c_int64, vp, C.c_int64, vp, C.c_int64,
+                                      vp, vp, vp, vp]),
+        "odma_decode_attention_shared": (C.c_int, [vp, C.c_int32, C.c_int32, vp, C.c_int32, vp, vp, vp, vp, vp, vp, C.c_int32, vp, vp]),
         "odma_stream_read_probe": (C.c_int, [vp, C.c_size_t, vp, vp]),
         "odma_block_read_probe": (C.c_int, [vp, vp, vp, C.c_int64, vp, vp]),
         "odma_migrate_batch": (C.c_int, [vp, C.c_int32, i32p, C.c_uint32, vp, i64p, i32p, i32p]),
@@ -149,6 +164,17 @@ def _dev(t) -> Optional[int]:
         raise TypeError("DEVICE argument must be a CUDA tensor")
     if not t.is_contiguous():
         raise ValueError("DEVICE argument must be contiguous")
+    return t.data_ptr()
+
+
+def _rows(t) -> Optional[int]:
+    """Device address of rows that lie apart (a slice of a projection's output): the last dimension must be contiguous."""
+    if t is None or isinstance(t, int):
+        return t
+    if not t.is_cuda:
+        raise TypeError("DEVICE argument must be a CUDA tensor")
+    if t.dim() and t.stride(-1) != 1:
+        raise ValueError("the last dimension of a DEVICE argument must be contiguous")
     return t.data_ptr()
 
 
@@ -220,6 +246,21 @@ def make_config(*, n_layers, n_q_heads, n_kv_heads, head_dim, kv_dtype, out_dtyp
     cfg.workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     keep += [k_pool, v_pool, workspace]
     return cfg, keep
+
+
+def make_qk_prep(*, q_weight=None, k_weight=None, eps=1e-6, rot_dim=0, adjacent=False, inv_freq=None, n_axes=1, axis=None):
+    """Fills an odma_qk_prep_t, which keeps the tensors alive.  axis: of every pair, which position turns it (default: the
+    first)."""
+    prep = odma_qk_prep_t()
+    prep.q_weight, prep.k_weight, prep.inv_freq = _dev(q_weight), _dev(k_weight), _dev(inv_freq)
+    prep.eps, prep.rot_dim, prep.rot_pairs, prep.n_axes = eps, rot_dim, ROT_ADJACENT if adjacent else ROT_HALVES, n_axes
+    axis = [] if axis is None else [int(x) for x in axis]
+    if len(axis) > MAX_ROT_PAIRS or any(x < 0 or x > 255 for x in axis):
+        raise ValueError("axis: at most MAX_ROT_PAIRS entries of 0 to n_axes - 1")
+    for f, x in enumerate(axis):
+        prep.axis[f] = x
+    prep.keep = (q_weight, k_weight, inv_freq)
+    return prep
 
 
 def odma_workspace_bytes(cfg: odma_pool_config_t) -> int:
@@ -391,6 +432,25 @@ class Pool:
                                stream=None):
         _check(lib.odma_prefill_attention(self._h, layer, n, _dev(q), int(total_q), _dev(q_start), _dev(n_q), _dev(offsets),
                                           _dev(lengths), _dev(block_table), bt_stride, _dev(out), _stream(stream)))
+
+    def odma_build_tables(self, n, lengths, n_new, offsets, n_prefixes, prefix_start, prefix_offsets, prefix_lengths,
+                          block_table, bt_stride, max_rows, row_start, row_position, row_slot, stream=None):
+        _check(lib.odma_build_tables(self._h, n, _dev(lengths), _dev(n_new), _dev(offsets), n_prefixes, _dev(prefix_start),
+                                     _dev(prefix_offsets), _dev(prefix_lengths), _dev(block_table), bt_stride, int(max_rows),
+                                     _dev(row_start), _dev(row_position), _dev(row_slot), _stream(stream)))
+
+    def odma_append_qkv(self, layer, n_rows, prep, q, q_stride, k, k_stride, v, v_stride, row_slot, positions, q_out,
+                        stream=None):
+        """q, k, v may be slices of one tensor; strides are in elements between rows."""
+        _check(lib.odma_append_qkv(self._h, layer, int(n_rows), None if prep is None else C.byref(prep), _rows(q), int(q_stride),
+                                   _rows(k), int(k_stride), _rows(v), int(v_stride), _dev(row_slot), _dev(positions), _dev(q_out),
+                                   _stream(stream)))
+
+    def odma_decode_attention_shared(self, layer, n, q, n_prefixes, prefix_start, prefix_offsets, prefix_lengths, offsets,
+                                     lengths, block_table, bt_stride, out, stream=None):
+        _check(lib.odma_decode_attention_shared(self._h, layer, n, _dev(q), n_prefixes, _dev(prefix_start), _dev(prefix_offsets),
+                                                _dev(prefix_lengths), _dev(offsets), _dev(lengths), _dev(block_table), bt_stride,
+                                                _dev(out), _stream(stream)))
 
     def odma_gather_kv(self, layer, offset, length, block_row, k_out, v_out, stream=None):
         _check(lib.odma_gather_kv(self._h, layer, int(offset), int(length), _dev(block_row), _dev(k_out), _dev(v_out),
