@@ -1,6 +1,7 @@
 // Row-major rows <-> pool block format (append, export) and the migration copy.
 #pragma once
 
+#include "block_index.h"
 #include "kernels_common.h"
 
 namespace {
@@ -8,12 +9,6 @@ namespace {
 // ---------------------------------------------------------------------------------
 // append / export: row-major rows <-> pool block format
 // ---------------------------------------------------------------------------------
-// element index inside a block
-__device__ __forceinline__ int k_index(int t, int d, int X) { return ((d / X) * BLK + t) * X + d % X; }
-__device__ __forceinline__ int v_index(int t, int d) {
-  return (((d >> 5) * 4 + (t >> 2)) * 16 + (d & 15)) * 8 + ((d >> 4) & 1) * 4 + (t & 3);
-}
-
 constexpr int APPEND_GRID_X = 512;  // most work-groups per request in a bulk append (each takes every 512th group of 16 rows)
 constexpr int APPEND_FILL = 1024;   // work-groups up to which append_kernel deals out the chunks of its rows (beyond, four per
                                     // compute unit, the launch is bound by memory: with 4096, 256 prompts of 100 rows took 10 % more)
@@ -250,13 +245,6 @@ __global__ __launch_bounds__(256) void gather_kernel(RowArgs a, int64_t offset, 
 // channels 64k + 8 g4 .. +8 and 64k + 32 + 8 g4 .. +8 of token t.  V: lane (c, q) reads, per half k,
 // 16 bytes = for each of the four 16-channel groups of the half, channel c of tokens 4q .. 4q+3.
 // ---------------------------------------------------------------------------------
-__device__ __forceinline__ int k_index_fp8(int t, int d) {
-  return (((d >> 6) * 4 + ((d >> 3) & 3)) * 16 + t) * 16 + ((d >> 5) & 1) * 8 + (d & 7);
-}
-__device__ __forceinline__ int v_index_fp8(int t, int d) {
-  return ((d >> 6) * 64 + (t >> 2) * 16 + (d & 15)) * 16 + ((d >> 4) & 3) * 4 + (t & 3);
-}
-
 __global__ __launch_bounds__(256) void append_fp8_kernel(RowArgs a, int32_t n, const int64_t* __restrict__ offsets,
                                                          const int32_t* __restrict__ positions, int32_t pos_bias,
                                                          const int32_t* __restrict__ n_new,

@@ -13,8 +13,8 @@
 // log2(GROUP) exchanges.  k and v go through LDS so that they leave as the 16-byte pieces of their blocks.
 #pragma once
 
+#include "block_index.h"
 #include "kernels_common.h"
-#include "kv_rows.h"
 
 namespace {
 

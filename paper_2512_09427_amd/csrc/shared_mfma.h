@@ -7,33 +7,36 @@
 // columns against its tokens, a dense contraction with reuse, where a request by itself only streams.
 //
 // Two lines of work.  Line A: items (prefix, KV head, block of SHARED_COLS columns), each the pairs of 16-token tiles of the
-// prefix.  Line B: items (request, KV head), each the tiles of the request's own tokens.  An item also counts a few units for
-// its start and end.  Each line is cut into equal shares, one of each to every work-group, so line A's matrix
-// instructions and line B's memory traffic overlap on every compute unit without a number that weighs one against the other: half
-// of the work-groups begin with A, half with B.  A share's pieces leave their states in the workspace and
-// shared_merge_kernel joins them; where a piece lies follows from the positions on the lines alone.
+// prefix.  Line B: items (request, KV head), each the tiles of the request's own tokens.  Items are cut into chunks of tokens so
+// that every work-group gets a like share of either line, and line A's matrix instructions run beside line B's memory traffic on
+// every compute unit without a number that weighs one against the other: half of the work-groups begin with A, half with B.
+// A chunk's piece leaves its state in the workspace and shared_merge_kernel joins them.  Line A is ordered (prefix, KV head,
+// chunk, column block): the work-groups of an XCD read the same few chunks at a time, out of its L2.
 #pragma once
 
 #include "kernels_common.h"
-#include "batch_tables.h"
+#include "prefixes.h"
 
 namespace {
+
+typedef const int64_t __attribute__((address_space(4))) const_i64s;
 
 enum { SHARED_BF16_128, SHARED_FP8_128, SHARED_BF16_64 };
 constexpr int SHARED_COLS = 128;          // columns of an item of line A: four waves of two 16-column tiles
 constexpr int SHARED_CT = 2;
-constexpr int SHARED_A_EXTRA = 3;         // start and end of an item of line A, in pairs
-constexpr int SHARED_B_EXTRA = 4;         // and of line B, in tiles
-constexpr int SHARED_A_LEAST = 8;         // smallest share: pairs and tiles a work-group is given
+constexpr int SHARED_A_EXTRA = 5;         // start and end of a piece of line A, in pairs
+constexpr int SHARED_B_EXTRA = 8;         // and of line B, in tiles
+constexpr int SHARED_A_LEAST = 8;         // pairs and tiles below which an item is not cut
 constexpr int SHARED_B_LEAST = 12;
+constexpr int SHARED_B_PIECES = 2;        // pieces of line B that a work-group gets on the average, where items are long enough
 constexpr int SHARED_MAX_N = ODMA_SHARED_MAX_REQUESTS;
 constexpr int SHARED_THREADS = 256;
 
-struct SharedRecord {                     // of a request: where its parts lie on the lines
-  int64_t a_pos, b_pos;                   // of the first head's item
-  int32_t a_pairs, a_blocks, a_col;       // pairs of the prefix (0: none), column blocks per head, the request's first column
-  int32_t b_tiles;
-  int64_t a_total, b_total;
+struct SharedRecord {                     // of a request, for the merge
+  int32_t a_chunks, a_blocks, a_col;      // line A: chunks (0: it shares nothing) and column blocks of an item, its first column
+  int32_t a_extra;                        // cut pieces (chunks behind the first) in front of its group's
+  int32_t b_chunks, b_extra;              // line B
+  int32_t pad0, pad1;
 };
 
 struct SharedArgs {
@@ -48,40 +51,54 @@ struct SharedArgs {
   float scale_log2, out_scale;
   int32_t out_bf16;
   int32_t workers;                        // work-groups of the launch, a multiple of 8
-  int32_t cut_cols;                       // columns kept for the piece that a work-group continues on line A
+  int32_t cut_cols;                       // columns kept for a cut piece of line A
   SharedRecord* rec;                      // [n]
   float2* part_ml;                        // states of columns: reference and sum
   float* part_o;                          // [column][128]
 };
 
-// columns of the workspace: first pieces of line A and of line B by (request, head), then the continued ones by work-group
+// Columns of the workspace: first chunks of line A and of line B by (request, head), then the chunks behind them, in the order of
+// their line: at most `workers` of line A (SharedCut) and SHARED_B_PIECES times as many of line B.
 __device__ __forceinline__ int64_t shared_first(const SharedArgs& a, int line, int r, int hq) {
   return ((int64_t)line * a.n + r) * a.Hq + hq;
 }
-__device__ __forceinline__ int64_t shared_cut_a(const SharedArgs& a, int w) { return (int64_t)2 * a.n * a.Hq + (int64_t)w * a.cut_cols; }
-__device__ __forceinline__ int64_t shared_cut_b(const SharedArgs& a, int w) {
-  return (int64_t)2 * a.n * a.Hq + (int64_t)a.workers * a.cut_cols + (int64_t)w * 16;
+__device__ __forceinline__ int64_t shared_cut_a(const SharedArgs& a, int i) { return (int64_t)2 * a.n * a.Hq + (int64_t)i * a.cut_cols; }
+__device__ __forceinline__ int64_t shared_cut_b(const SharedArgs& a, int i) {
+  return (int64_t)2 * a.n * a.Hq + (int64_t)a.workers * a.cut_cols + (int64_t)i * 16;
 }
 
-// Shares of a line.  Share w of `used` is [start(w), start(w + 1)); an item at s with T units has unit 0 at s and unit i at
-// s + extra + i, and a unit belongs to the share that holds its position.
-struct SharedLine {
-  int64_t total;
-  int used;
-  __device__ __forceinline__ SharedLine(int64_t total_, int least, int workers) : total(total_) {
-    const int64_t w = total / least;
-    used = total == 0 ? 0 : (int)(w < 1 ? 1 : w < workers ? w : workers);
-    used = min((used + 7) / 8 * 8, workers);              // every XCD the same number
+// How a line with `units` in `items` items is cut for `pieces` pieces in all: into chunks of at most `length`.  An item of T units
+// has (T - 1) / length chunks behind its first, fewer than T / length, so all items together have fewer than units / length, which
+// is at most `pieces` (half of them where items abound, so that they are cut little).
+struct SharedCut {
+  int length, shift;                                        // costs count 2^shift units, so that a line's sum fits 30 bits
+  __device__ __forceinline__ SharedCut(float units, int items, int pieces, int least) {
+    const float l = units * 1.0002f / (float)max(pieces - items, pieces / 2);   // (the sum is within 2^-13)
+    length = max((int)fminf(l, 1e9f) + 1, least);
+    shift = max(ilogbf(fmaxf(units, 1.f)) - 27, 0);
   }
-  __device__ __forceinline__ int64_t start(int w) const { return total * w / used; }
-  __device__ __forceinline__ int holder(int64_t pos) const { return (int)(((pos + 1) * used - 1) / total); }
+  __device__ __forceinline__ int chunks(int T) const { return (T + length - 1) / length; }
 };
-// units of an item at s in front of position x
-__device__ __forceinline__ int units_before(int64_t x, int64_t s, int T, int extra) {
-  if (x <= s) return 0;
-  const int64_t i = x - s - extra;
-  return (int)(i < 1 ? 1 : i < T ? i : T);
+
+// first unit of a chunk of an item of T units: chunks differ by one at most
+__device__ __forceinline__ int chunk_start(int T, int chunks, int chunk) {
+  const int base = T / chunks;
+  return chunk * base + min(chunk, T - chunks * base);
 }
+
+// Work-group w takes the pieces of its share [start(w), start(w + 1)) of a line's cost.  The N pieces of an entry (a group, a request)
+// that begins at s and costs c are spread over it evenly.
+struct SharedShare {
+  int x0, x1;
+  __device__ __forceinline__ SharedShare(int total, int used, int w) {
+    const double step = (double)total / (double)used;
+    x0 = (int)((double)w * step);
+    x1 = w + 1 >= used ? total : (int)((double)(w + 1) * step);
+  }
+  static __device__ __forceinline__ int upto(int x, int s, int c, int N) {
+    return x <= s ? 0 : x >= s + c ? N : min((int)ceilf((float)(x - s) * (float)N / (float)c), N);   // (monotone in x)
+  }
+};
 
 template <bool HIGH_HALF>
 __device__ __forceinline__ unsigned widen_e4m3x2(unsigned w) {
@@ -91,27 +108,19 @@ __device__ __forceinline__ unsigned widen_e4m3x2(unsigned w) {
 }
 
 struct SharedPlan {
-  int64_t a_pos[SHARED_MAX_N + 1], b_pos[SHARED_MAX_N + 1];   // exclusive prefix: groups on line A, requests on line B
+  int32_t a_pos[SHARED_MAX_N + 1], b_pos[SHARED_MAX_N + 1];   // cost in front of a group on line A, of a request on line B
+  int32_t a_extra[SHARED_MAX_N], b_extra[SHARED_MAX_N];       // cut pieces in front of them
+  int32_t start[SHARED_MAX_N + 1];                            // first request of a group
+  int32_t tiles[SHARED_MAX_N];                                // of a group's shared part
   int32_t reader[SHARED_MAX_N];                               // of a group: its first request that holds all of the shared part
-  int64_t wave_sum[2][SHARED_THREADS / 64];
+  int32_t own[SHARED_MAX_N];                                  // of a request: tokens that it reads itself
+  int32_t skip[SHARED_MAX_N];                                 // ... and the blocks of its tokens in front of them (-1: in its group's prefix)
+  float wave_units[SHARED_THREADS / 64];
+  int32_t wave_items[SHARED_THREADS / 64];
+  int32_t wave_sum[SHARED_THREADS / 64][4];
 };
 
-// own tokens of request r (those of its prefix too, where it is shorter than the shared part), and what it shares
-struct SharedRequest {
-  int len, shared, group;
-  __device__ __forceinline__ SharedRequest(const SharedArgs& a, int r) {
-    len = max(a.lengths[r], 0);
-    group = prefix_of(a.prefix_start, a.n_prefixes, r);
-    shared = group >= 0 ? shared_tokens(a.prefix_lengths[group]) : 0;
-  }
-  __device__ __forceinline__ bool shares() const { return shared > 0 && len >= shared; }
-  __device__ __forceinline__ int own() const { return shares() ? len - shared : len; }
-};
-// members of group p
-__device__ __forceinline__ void shared_members(const SharedArgs& a, int p, int& begin, int& count) {
-  begin = min(max(a.prefix_start[p], 0), a.n);
-  count = max(min(a.prefix_start[p + 1], a.n) - begin, 0);
-}
+__device__ __forceinline__ int tiles_of(int tokens) { return (int)(((int64_t)tokens + BLK - 1) / BLK); }
 __device__ __forceinline__ int column_blocks(int count, int G) { return (count * G + SHARED_COLS - 1) / SHARED_COLS; }
 
 // Factor of a state joined to another.  At least the smallest number: 0 would make an infinite sum NaN.
@@ -123,31 +132,6 @@ __device__ __forceinline__ void two_parts(float w, __bf16& hi, __bf16& lo) {
   const unsigned bits = __float_as_uint(w) & 0xffff0000u;
   hi = __builtin_bit_cast(__bf16, (unsigned short)(bits >> 16));
   lo = (__bf16)fmaxf(w - __uint_as_float(bits), w * 0x1p-40f);
-}
-
-// exclusive scan of one value per thread over the work-group; the sum of all in `total`
-__device__ __forceinline__ int64_t scan_of_threads(int64_t x, int64_t* wave_sum, int64_t& total) {
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  int64_t inc = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up((long long)inc, o);
-    if (lane >= o) inc += y;
-  }
-  if (lane == 63) wave_sum[wv] = inc;
-  __syncthreads();
-  int64_t before = 0;
-  total = 0;
-  for (int i = 0; i < SHARED_THREADS / 64; ++i) {
-    if (i < wv) before += wave_sum[i];
-    total += wave_sum[i];
-  }
-  return before + inc - x;
-}
-
-__device__ __forceinline__ void store_result(const SharedArgs& a, int64_t at, int ch, float x) {
-  if (a.out_bf16) ((unsigned short*)a.out)[at + ch] = float_to_bf16_bits(x);
-  else ((float*)a.out)[at + ch] = x;
 }
 
 // LO: the weights of line A go through the matrix cores as two bf16 parts (16 bits) instead of one; for fp32 results.
@@ -171,66 +155,150 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
   const unsigned lane16 = lane * 16;
   const int G = a.G;
 
-  // ---- plan: every work-group for itself (a launch of its own would be one work-group's round trips on an empty chip)
-  for (int p = tid; p < a.n_prefixes; p += SHARED_THREADS) plan.reader[p] = a.n;
-  __syncthreads();
+  // ---- plan: every work-group for itself (a launch of its own would be one work-group's round trips on an empty chip).  One
+  // round of loads, then LDS alone.
   const int per = (a.n + SHARED_THREADS - 1) / SHARED_THREADS;
   const int r0 = min(tid * per, a.n), r1 = min(r0 + per, a.n);
-  int64_t mine = 0;
-  for (int r = r0; r < r1; ++r) {
-    const SharedRequest rq(a, r);
-    if (rq.shares()) atomicMin(&plan.reader[rq.group], r);
-    const int tiles = (int)(((int64_t)rq.own() + BLK - 1) / BLK);
-    plan.b_pos[r] = tiles;
-    if (tiles) mine += (int64_t)a.Hkv * (tiles + SHARED_B_EXTRA);
+  for (int r = tid; r < a.n; r += SHARED_THREADS) plan.own[r] = a.lengths[r];
+  for (int p = tid; p <= a.n_prefixes; p += SHARED_THREADS) {
+    plan.start[p] = min(max(a.prefix_start[p], 0), a.n);
+    if (p < a.n_prefixes) {
+      plan.tiles[p] = shared_tokens(a.prefix_lengths[p]) / BLK;
+      plan.reader[p] = a.n;
+    }
   }
-  int64_t b_total, a_total;
-  int64_t at = scan_of_threads(mine, plan.wave_sum[0], b_total);     // (its barrier: reader is whole)
+  __syncthreads();
+  float units = 0.f;
+  int items = 0;
   for (int r = r0; r < r1; ++r) {
-    const int64_t tiles = plan.b_pos[r];
-    plan.b_pos[r] = at;
-    if (tiles) at += (int64_t)a.Hkv * (tiles + SHARED_B_EXTRA);
+    const int len = max(plan.own[r], 0), p = prefix_of(plan.start, a.n_prefixes, r), shared = p >= 0 ? plan.tiles[p] * BLK : 0;
+    const bool shares = shared > 0 && len >= shared;
+    if (shares) atomicMin(&plan.reader[p], r);
+    const int own = shares ? len - shared : len;
+    plan.own[r] = own;
+    plan.skip[r] = shares ? shared / BLK : shared > 0 ? -1 : 0;
+    units += (float)tiles_of(own);
+    items += own > 0;
   }
+  units = wave_sum(units);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) items += __shfl_xor(items, o);
+  if (lane == 0) {
+    plan.wave_units[wv] = units;
+    plan.wave_items[wv] = items;
+  }
+  __syncthreads();
+  units = 0.f;
+  items = 0;
+  for (int i = 0; i < SHARED_THREADS / 64; ++i) {
+    units += plan.wave_units[i];
+    items += plan.wave_items[i];
+  }
+  const int b_items = items;
+  const SharedCut cut_b(units * (float)a.Hkv, items * a.Hkv, SHARED_B_PIECES * a.workers, SHARED_B_LEAST);
+  // groups, every wave for itself
+  auto group_blocks = [&](int p) {                          // column blocks of a KV head; 0: nobody attends to the prefix
+    return plan.reader[p] < a.n ? column_blocks(plan.start[p + 1] - plan.start[p], G) : 0;
+  };
+  units = 0.f;
+  items = 0;
+  for (int p = lane; p < a.n_prefixes; p += 64) {
+    const int blocks = group_blocks(p);
+    units += (float)blocks * (float)((plan.tiles[p] + 1) / 2);
+    items += blocks;
+  }
+  units = wave_sum(units);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) items += __shfl_xor(items, o);
+  const SharedCut cut_a(units * (float)a.Hkv, items * a.Hkv, a.workers, SHARED_A_LEAST);
+  // costs and cut pieces, and their exclusive sums
   const int perp = (a.n_prefixes + SHARED_THREADS - 1) / SHARED_THREADS;
   const int p0 = min(tid * perp, a.n_prefixes), p1 = min(p0 + perp, a.n_prefixes);
-  auto group_cost = [&](int p) -> int64_t {
-    int begin, count;
-    shared_members(a, p, begin, count);
-    const int pairs = (shared_tokens(a.prefix_lengths[p]) / BLK + 1) / 2;
-    return plan.reader[p] < a.n ? (int64_t)a.Hkv * column_blocks(count, G) * (pairs + SHARED_A_EXTRA) : 0;
+  struct Entry {
+    int cost, extra;
   };
-  mine = 0;
-  for (int p = p0; p < p1; ++p) mine += group_cost(p);
-  at = scan_of_threads(mine, plan.wave_sum[1], a_total);
+  auto group_entry = [&](int p) {
+    const int blocks = group_blocks(p), pairs = (plan.tiles[p] + 1) / 2, chunks = cut_a.chunks(pairs);
+    if (!blocks) return Entry{0, 0};
+    return Entry{(int)((int64_t)a.Hkv * blocks * (pairs + chunks * SHARED_A_EXTRA) >> cut_a.shift) + 1, a.Hkv * blocks * (chunks - 1)};
+  };
+  auto request_entry = [&](int r) {
+    const int tiles = tiles_of(plan.own[r]), chunks = cut_b.chunks(tiles);
+    if (!tiles) return Entry{0, 0};
+    return Entry{(int)((int64_t)a.Hkv * (tiles + chunks * SHARED_B_EXTRA) >> cut_b.shift) + 1, a.Hkv * (chunks - 1)};
+  };
+  int sum[4] = {0, 0, 0, 0};
   for (int p = p0; p < p1; ++p) {
-    plan.a_pos[p] = at;
-    at += group_cost(p);
+    const Entry e = group_entry(p);
+    sum[0] += e.cost;
+    sum[1] += e.extra;
+  }
+  for (int r = r0; r < r1; ++r) {
+    const Entry e = request_entry(r);
+    sum[2] += e.cost;
+    sum[3] += e.extra;
+  }
+  int before[4], total[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) before[i] = sum[i];
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int y = __shfl_up(before[i], o);
+      if (lane >= o) before[i] += y;
+    }
+  if (lane == 63)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) plan.wave_sum[wv][i] = before[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    before[i] -= sum[i];
+    total[i] = 0;
+    for (int w = 0; w < SHARED_THREADS / 64; ++w) {
+      if (w < wv) before[i] += plan.wave_sum[w][i];
+      total[i] += plan.wave_sum[w][i];
+    }
+  }
+  for (int p = p0; p < p1; ++p) {
+    const Entry e = group_entry(p);
+    plan.a_pos[p] = before[0];
+    plan.a_extra[p] = before[1];
+    before[0] += e.cost;
+    before[1] += e.extra;
+  }
+  for (int r = r0; r < r1; ++r) {
+    const Entry e = request_entry(r);
+    plan.b_pos[r] = before[2];
+    plan.b_extra[r] = before[3];
+    before[2] += e.cost;
+    before[3] += e.extra;
   }
   if (tid == 0) {
-    plan.a_pos[a.n_prefixes] = a_total;
-    plan.b_pos[a.n] = b_total;
+    plan.a_pos[a.n_prefixes] = total[0];
+    plan.b_pos[a.n] = total[2];
   }
   __syncthreads();
   if (blockIdx.x == gridDim.x - 1) {                        // for the merge
     for (int r = tid; r < a.n; r += SHARED_THREADS) {
-      const SharedRequest rq(a, r);
-      SharedRecord rec = {0, plan.b_pos[r], 0, 0, 0, (int)(((int64_t)rq.own() + BLK - 1) / BLK), a_total, b_total};
-      if (rq.shares()) {
-        int begin, count;
-        shared_members(a, rq.group, begin, count);
-        rec.a_pos = plan.a_pos[rq.group];
-        rec.a_pairs = (rq.shared / BLK + 1) / 2;
-        rec.a_blocks = column_blocks(count, G);
-        rec.a_col = (r - begin) * G;
+      SharedRecord rec = {0, 0, 0, 0, cut_b.chunks(tiles_of(plan.own[r])), plan.b_extra[r], 0, 0};
+      if (plan.skip[r] > 0) {
+        const int p = prefix_of(plan.start, a.n_prefixes, r);
+        rec.a_chunks = cut_a.chunks((plan.tiles[p] + 1) / 2);
+        rec.a_blocks = group_blocks(p);
+        rec.a_col = (r - plan.start[p]) * G;
+        rec.a_extra = plan.a_extra[p];
       }
       a.rec[r] = rec;
     }
   }
-  const SharedLine la(a_total, SHARED_A_LEAST + SHARED_A_EXTRA, a.workers), lb(b_total, SHARED_B_LEAST + SHARED_B_EXTRA, a.workers);
-  // XCD x (work-groups x, x + 8, ..) has neighbouring shares, which read the same heads; a line with few shares takes the first
-  // work-groups of every XCD (A) or the last (B).
+  // XCD x (work-groups x, x + 8, ..) has neighbouring shares, which read the same heads.  A short line goes to few work-groups (a piece
+  // each), the first ones of every XCD (A) or the last (B).
+  auto used_of = [&](int cost, int pieces) { return cost ? min((min(pieces, a.workers) + 7) / 8 * 8, a.workers) : 0; };
+  const int used_a = used_of(total[0], total[1] + items * a.Hkv), used_b = used_of(total[2], total[3] + b_items * a.Hkv);
   const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, turns = a.workers >> 3;
-  const int ja = la.used >> 3, jb = lb.used >> 3;
+  const int ja = used_a >> 3, jb = used_b >> 3;
   const int share_a = turn < ja ? xcd * ja + turn : -1, share_b = turns - 1 - turn < jb ? xcd * jb + turns - 1 - turn : -1;
 
   auto piece = [&](const uint4v (&w)[LOADS], int s) {       // 16-byte operand s (of NS) of a tile, as bf16
@@ -240,35 +308,38 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
   };
   auto join = [](uint2v lo, uint2v hi) { return __builtin_bit_cast(bf16x8, uint4v{lo[0], lo[1], hi[0], hi[1]}); };
 
+  auto larger = [](float x, float y) { return __builtin_elementwise_maximum(x, y); };   // (NaN passes; fmaxf quiets every operand first)
+  auto largest = [&](const float4v (&x)[2]) {
+    return larger(larger(larger(x[0][0], x[0][1]), larger(x[0][2], x[0][3])), larger(larger(x[1][0], x[1][1]), larger(x[1][2], x[1][3])));
+  };
+  const float slack = SLACK / a.scale_log2;
+
   // ================= line A
   auto line_a = [&]() {
-    const int64_t x0 = la.start(share_a), x1 = la.start(share_a + 1);
+    bf16x8 ones;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
+    const SharedShare share(total[0], used_a, share_a);
     // group that holds x0: the last one at or before it (groups without work repeat a position)
     int lo = 0, hi = a.n_prefixes;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (plan.a_pos[mid] <= x0) lo = mid;
+      if (plan.a_pos[mid] <= share.x0) lo = mid;
       else hi = mid;
     }
-    for (int p = rfl(lo); p < a.n_prefixes && plan.a_pos[p] < x1; ++p) {
-      if (plan.a_pos[p + 1] <= x0 || plan.a_pos[p + 1] == plan.a_pos[p]) continue;
-      int begin, count;
-      shared_members(a, p, begin, count);
-      begin = rfl(begin);
-      count = rfl(count);
-      const int n_tiles = rfl(shared_tokens(a.prefix_lengths[p]) / BLK), pairs = (n_tiles + 1) / 2;
-      const int blocks = column_blocks(count, G), cost = pairs + SHARED_A_EXTRA, items = a.Hkv * blocks, n_cols = count * G;
-      const int64_t base_pos = plan.a_pos[p];
-      const int64_t base_block = PAGED ? 0 : a.prefix_offsets[p] / BLK;
+    for (int p = rfl(lo); p < a.n_prefixes && plan.a_pos[p] < share.x1; ++p) {
+      const int pos = rfl(plan.a_pos[p]), cost = rfl(plan.a_pos[p + 1]) - pos;
+      if (!cost) continue;
+      const int begin = rfl(plan.start[p]), count = rfl(plan.start[p + 1]) - begin;
+      const int n_tiles = rfl(plan.tiles[p]), pairs = (n_tiles + 1) / 2, chunks = cut_a.chunks(pairs);
+      const int blocks = column_blocks(count, G), per_head = chunks * blocks, n_pieces = a.Hkv * per_head, n_cols = count * G;
+      const int64_t base_block = PAGED ? 0 : ((const const_i64s*)(uintptr_t)a.prefix_offsets)[p] / BLK;
       const const_i32* bt_row = as_constant(PAGED ? a.bt + (int64_t)rfl(plan.reader[p]) * a.bt_stride : nullptr);
-      int item = rfl(x0 > base_pos ? (int)((x0 - base_pos) / cost) : 0);
-      for (; item < items; ++item) {
-        const int64_t s = base_pos + (int64_t)item * cost;
-        if (s >= x1) break;
-        const int i0 = rfl(units_before(x0, s, pairs, SHARED_A_EXTRA)), i1 = rfl(units_before(x1, s, pairs, SHARED_A_EXTRA));
-        if (i0 >= i1) continue;
-        const bool continued = x0 > s;
-        const int g = rfl(item / blocks), cb = rfl(item - g * blocks);
+      const int last = rfl(SharedShare::upto(share.x1, pos, cost, n_pieces));
+      for (int id = rfl(SharedShare::upto(share.x0, pos, cost, n_pieces)); id < last; ++id) {
+        const int g = rfl(id / per_head), chunk = rfl((id - g * per_head) / blocks), cb = id - g * per_head - chunk * blocks;
+        const int i0 = rfl(chunk_start(pairs, chunks, chunk)), i1 = rfl(chunk_start(pairs, chunks, chunk + 1));
+        const int cut = chunk ? rfl(plan.a_extra[p]) + (g * (chunks - 1) + chunk - 1) * blocks + cb : -1;
         const int c0 = cb * SHARED_COLS + wv * 16 * CT;
         const bool active = c0 < n_cols;
         const int64_t plane = (int64_t)g * a.head_stride;
@@ -290,12 +361,14 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
             qreg[ct][st] = ok[ct] ? *(const bf16x8*)(qp + 32 * st) : z;
           }
         }
-        float m[CT], l[CT];
-        float4v O[CT][DT];
+        // A column's reference m, in raw scores, enters with the accumulators of its scores (minus m instead of 0); -inf: none yet.
+        // The sum of its weights is one more row of P V, with V = 1.
+        float m[CT];
+        float4v minus_m[CT], l[CT], O[CT][DT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          m[ct] = LOWEST_REF;
-          l[ct] = 0.f;
+          m[ct] = -INFINITY;
+          minus_m[ct] = l[ct] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) O[ct][dt] = float4v{0.f, 0.f, 0.f, 0.f};
         }
@@ -338,6 +411,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
             }
           }
         };
+        bool fresh = true;                                   // some column of the wave has no reference
         auto compute = [&](int pr) {
           const char* st = stage_mem + ((pr - i0) & 1) * STAGE_BYTES + lane16;
           bf16x8 av[DT];
@@ -351,31 +425,44 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
             for (int sp = 0; sp < NS; ++sp) kk[sp] = *(const bf16x8*)(st + b * NS * 1024 + sp * 1024);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-              float4v s4 = float4v{0.f, 0.f, 0.f, 0.f};
+              float4v s4 = minus_m[ct];
 #pragma unroll
               for (int sp = 0; sp < NS; ++sp) s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[sp], qreg[ct][sp], s4, 0, 0, 0);
               x[ct][b] = s4;
             }
           }
-          if (2 * pr + 1 >= n_tiles)
+          if (2 * pr + 1 >= n_tiles) {
+            asm volatile("");                                // (a branch: once an item, against eight selects a pair)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) x[ct][1] = float4v{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          bool move = false;
-          float top[CT];
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            top[ct] = fmaxf(fmaxf(fmaxf(x[ct][0][0], x[ct][0][1]), fmaxf(x[ct][0][2], x[ct][0][3])),
-                            fmaxf(fmaxf(x[ct][1][0], x[ct][1][1]), fmaxf(x[ct][1][2], x[ct][1][3]))) * a.scale_log2;
-            move |= top[ct] > m[ct] + SLACK;
           }
-          if (__builtin_amdgcn_ballot_w64(move) != 0) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) top = larger(top, largest(x[ct]));
+          if (fresh || __builtin_amdgcn_ballot_w64(top > slack) != 0) {
+            fresh = false;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-              top[ct] = fmaxf(top[ct], __shfl_xor(top[ct], 16));
-              top[ct] = fmaxf(top[ct], __shfl_xor(top[ct], 32));
-              const float m_new = fmaxf(m[ct], top[ct]), f = joined(m[ct], m_new);
-              m[ct] = m_new;
+              float up = largest(x[ct]);
+              up = fmaxf(up, __shfl_xor(up, 16));
+              up = fmaxf(up, __shfl_xor(up, 32));
+              float f = 1.f;
+              if (m[ct] == -INFINITY) {
+                m[ct] = up;
+                up = up == -INFINITY ? 0.f : up;
+              } else {
+                up = fmaxf(up, 0.f);
+                m[ct] += up;
+                f = joined(0.f, up * a.scale_log2);
+              }
+              fresh |= __builtin_amdgcn_ballot_w64(m[ct] == -INFINITY) != 0;
+              const float mm = m[ct] == -INFINITY ? 0.f : -m[ct];
+              minus_m[ct] = float4v{mm, mm, mm, mm};
               l[ct] *= f;
+#pragma unroll
+              for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[ct][b][i] -= up;
 #pragma unroll
               for (int dt = 0; dt < DT; ++dt) O[ct][dt] *= f;
             }
@@ -383,13 +470,11 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
           bf16x8 ph[CT], pl[CT];
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
-            float sum = 0.f;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(x[ct][b][i], a.scale_log2, -m[ct]));
-                sum += pv;
+                const float pv = __builtin_amdgcn_exp2f(x[ct][b][i] * a.scale_log2);
                 if (LO) {
                   __bf16 hi, lo;
                   two_parts(pv, hi, lo);
@@ -399,7 +484,8 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
                   ph[ct][4 * b + i] = (__bf16)pv;
                 }
               }
-            l[ct] += sum;
+            l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, ph[ct], l[ct], 0, 0, 0);
+            if (LO) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pl[ct], l[ct], 0, 0, 0);
           }
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt)
@@ -435,11 +521,9 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
         }
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          l[ct] += __shfl_xor(l[ct], 16);
-          l[ct] += __shfl_xor(l[ct], 32);
           if (!ok[ct]) continue;
-          const int64_t c = continued ? shared_cut_a(a, share_a) + wv * 16 * CT + 16 * ct + col16 : shared_first(a, 0, row[ct], head[ct]);
-          if (g4 == 0) a.part_ml[c] = make_float2(m[ct], l[ct]);
+          const int64_t c = cut >= 0 ? shared_cut_a(a, cut) + wv * 16 * CT + 16 * ct + col16 : shared_first(a, 0, row[ct], head[ct]);
+          if (g4 == 0) a.part_ml[c] = make_float2(m[ct] == -INFINITY ? LOWEST_REF : m[ct] * a.scale_log2, l[ct][0]);
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) *(float4v*)(a.part_o + c * 128 + 16 * dt + 4 * g4) = O[ct][dt];
         }
@@ -449,29 +533,28 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
 
   // ================= line B: one request and KV head at a time; the waves take turns at its pairs of tiles, straight into registers
   auto line_b = [&]() {
-    const int64_t x0 = lb.start(share_b), x1 = lb.start(share_b + 1);
+    const SharedShare share(total[2], used_b, share_b);
     int lo = 0, hi = a.n;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (plan.b_pos[mid] <= x0) lo = mid;
+      if (plan.b_pos[mid] <= share.x0) lo = mid;
       else hi = mid;
     }
-    for (int r = rfl(lo); r < a.n && plan.b_pos[r] < x1; ++r) {
-      if (plan.b_pos[r + 1] <= x0 || plan.b_pos[r + 1] == plan.b_pos[r]) continue;
-      const SharedRequest rq(a, r);
-      const int own = rfl(rq.own()), tiles = (own + BLK - 1) / BLK, cost = tiles + SHARED_B_EXTRA;
-      const int in_front = rfl(rq.shares() ? rq.shared / BLK : 0);        // blocks of the row that are not its own
+    for (int r = rfl(lo); r < a.n && plan.b_pos[r] < share.x1; ++r) {
+      const int pos = rfl(plan.b_pos[r]), cost = rfl(plan.b_pos[r + 1]) - pos;
+      if (!cost) continue;
+      const int own = rfl(plan.own[r]), tiles = tiles_of(own), chunks = cut_b.chunks(tiles), n_pieces = a.Hkv * chunks, skip = rfl(plan.skip[r]);
       // its own slab; a request shorter than the shared part reads its group's prefix
-      const int64_t base_block = PAGED ? 0 : (rq.shared > 0 && !rq.shares() ? a.prefix_offsets[rq.group] : a.offsets[r]) / BLK;
-      const const_i32* bt_row = as_constant(PAGED ? a.bt + (int64_t)r * a.bt_stride + in_front : nullptr);
-      const int64_t base_pos = plan.b_pos[r];
-      int g = rfl(x0 > base_pos ? (int)((x0 - base_pos) / cost) : 0);
-      for (; g < a.Hkv; ++g) {
-        const int64_t s = base_pos + (int64_t)g * cost;
-        if (s >= x1) break;
-        const int i0 = rfl(units_before(x0, s, tiles, SHARED_B_EXTRA)), i1 = rfl(units_before(x1, s, tiles, SHARED_B_EXTRA));
-        if (i0 >= i1) continue;
-        const bool continued = x0 > s;
+      int64_t base_block = 0;
+      if (!PAGED)
+        base_block = (skip >= 0 ? ((const const_i64s*)(uintptr_t)a.offsets)[r]
+                                : ((const const_i64s*)(uintptr_t)a.prefix_offsets)[rfl(prefix_of(plan.start, a.n_prefixes, r))]) / BLK;
+      const const_i32* bt_row = as_constant(PAGED ? a.bt + (int64_t)r * a.bt_stride + max(skip, 0) : nullptr);
+      const int last = rfl(SharedShare::upto(share.x1, pos, cost, n_pieces));
+      for (int id = rfl(SharedShare::upto(share.x0, pos, cost, n_pieces)); id < last; ++id) {
+        const int g = rfl(id / chunks), chunk = id - g * chunks;
+        const int i0 = rfl(chunk_start(tiles, chunks, chunk)), i1 = rfl(chunk_start(tiles, chunks, chunk + 1));
+        const int cut = chunk ? rfl(plan.b_extra[r]) + g * (chunks - 1) + chunk - 1 : -1;
         const int64_t plane = (int64_t)g * a.head_stride;
         bf16x8 qreg[NS];
         {
@@ -525,8 +608,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
               for (int i = 0; i < 4; ++i)
                 if ((t + b) * BLK + 4 * g4 + i >= held) x[b][i] = -INFINITY;
           }
-          float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
-                            fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3]))) * a.scale_log2;
+          float top = largest(x) * a.scale_log2;
           if (__builtin_amdgcn_ballot_w64(top > m + SLACK) != 0) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
@@ -583,7 +665,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) *(float4v*)(st + (wv * 16 + col16) * D + 16 * dt + 4 * g4) = O[dt];
         __syncthreads();
-        const int64_t c = continued ? shared_cut_b(a, share_b) : shared_first(a, 1, r, g * G);
+        const int64_t c = cut >= 0 ? shared_cut_b(a, cut) : shared_first(a, 1, r, g * G);
         for (int e = tid; e < G * D; e += SHARED_THREADS) {
           const int h = e / D, ch = e % D;
           float mm = LOWEST_REF, ll = 0.f, oo = 0.f;
@@ -612,57 +694,64 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
   }
 }
 
-// Joins the pieces of a request's two parts: a wave per (request, query head), two channels a lane.
+// Joins the pieces of a request's two parts: a wave per (request, query head), two channels a lane.  Lane i looks up piece i (64 a
+// round); the outputs of the first 16 are requested beside all references and sums, in one round trip.
 template <int D>
 __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t id = rfl(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (id >= (int64_t)a.n * a.Hq) return;
-  const int r = (int)(id / a.Hq), hq = (int)(id - (int64_t)r * a.Hq), g = hq / a.G;
+  const int id = rfl(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (id >= a.n * a.Hq) return;
+  const int r = id / a.Hq, hq = id - r * a.Hq, g = hq / a.G;
   const SharedRecord rec = a.rec[r];
+  const bool lane_has = 2 * lane < D;
+  const float* base = a.part_o + (lane_has ? 2 * lane : 0);
+  const int h = hq - g * a.G, col = rec.a_col + h, cb = col / SHARED_COLS;
+  const int n = rec.a_chunks + rec.b_chunks;
   float m = LOWEST_REF, l = 0.f;
   float2 o = {0.f, 0.f};
-  const bool lane_has = 2 * lane < D;
-  auto add = [&](int64_t c) {
-    const float2 ml = a.part_ml[c];
-    const float2 x = lane_has ? *(const float2*)(a.part_o + c * 128 + 2 * lane) : make_float2(0.f, 0.f);
-    const float m_new = fmaxf(m, ml.x), f = joined(m, m_new), fx = joined(ml.x, m_new);
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    // lane i: piece i0 + i, line A's first
+    const int i = i0 + lane, here = min(64, n - i0);
+    const bool on_a = i < rec.a_chunks, has = i < n;
+    const int j = on_a ? i : i - rec.a_chunks;               // chunk
+    const int64_t c = j == 0 ? shared_first(a, on_a ? 0 : 1, r, hq)
+                      : on_a ? shared_cut_a(a, rec.a_extra + (g * (rec.a_chunks - 1) + j - 1) * rec.a_blocks + cb) + col - cb * SHARED_COLS
+                             : shared_cut_b(a, rec.b_extra + g * (rec.b_chunks - 1) + j - 1) + h;
+    const int c_lo = has ? (int)c : 0;                       // (columns of the workspace fit 32 bits)
+    const float2 ml = has ? a.part_ml[c] : make_float2(LOWEST_REF, 0.f);
+    constexpr int ROUND = 16;
+    float2 x[ROUND];
+    auto load = [&](int k0) {
+#pragma unroll
+      for (int k = 0; k < ROUND; ++k)
+        x[k] = *(const float2*)(base + (int64_t)__builtin_amdgcn_readlane(c_lo, min(k0 + k, here - 1)) * 128);
+    };
+    load(0);                                                 // under way before the weights are known
+    const float m_new = fmaxf(m, wave_max(ml.x)), f = joined(m, m_new), fx = has ? joined(ml.x, m_new) : 0.f;
+    l = l * f + wave_sum(ml.y * fx);
+    o.x *= f;
+    o.y *= f;
     m = m_new;
-    l = l * f + ml.y * fx;
-    o.x = o.x * f + x.x * fx;
-    o.y = o.y * f + x.y * fx;
-  };
-  if (rec.a_pairs) {
-    const SharedLine line(rec.a_total, SHARED_A_LEAST + SHARED_A_EXTRA, a.workers);
-    const int col = rec.a_col + hq - g * a.G, cb = col / SHARED_COLS;
-    const int64_t s = rec.a_pos + (int64_t)(g * rec.a_blocks + cb) * (rec.a_pairs + SHARED_A_EXTRA);
-    int w = line.holder(s);
-    add(shared_first(a, 0, r, hq));
-    for (int before = units_before(line.start(w + 1), s, rec.a_pairs, SHARED_A_EXTRA); before < rec.a_pairs;) {
-      ++w;
-      const int upto = units_before(line.start(w + 1), s, rec.a_pairs, SHARED_A_EXTRA);
-      if (upto > before) add(shared_cut_a(a, w) + col - cb * SHARED_COLS);   // (a share shorter than an item's start may hold none)
-      before = upto;
-    }
-  }
-  if (rec.b_tiles) {
-    const SharedLine line(rec.b_total, SHARED_B_LEAST + SHARED_B_EXTRA, a.workers);
-    const int64_t s = rec.b_pos + (int64_t)g * (rec.b_tiles + SHARED_B_EXTRA);
-    int w = line.holder(s);
-    add(shared_first(a, 1, r, hq));
-    for (int before = units_before(line.start(w + 1), s, rec.b_tiles, SHARED_B_EXTRA); before < rec.b_tiles;) {
-      ++w;
-      const int upto = units_before(line.start(w + 1), s, rec.b_tiles, SHARED_B_EXTRA);
-      if (upto > before) add(shared_cut_b(a, w) + hq - g * a.G);
-      before = upto;
+    for (int k0 = 0;;) {
+#pragma unroll
+      for (int k = 0; k < ROUND; ++k) {
+        const float w_k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fx), min(k0 + k, 63)));
+        if (k0 + k < here && w_k != 0.f) {
+          o.x = __builtin_fmaf(x[k].x, w_k, o.x);
+          o.y = __builtin_fmaf(x[k].y, w_k, o.y);
+        }
+      }
+      if ((k0 += ROUND) >= here) break;
+      load(k0);
     }
   }
   if (lane_has) {
-    const float inv = rec.a_pairs || rec.b_tiles ? a.out_scale / l : 0.f;
-    const int64_t at = id * D + 2 * lane;
-    const bool empty = !rec.a_pairs && !rec.b_tiles;
-    store_result(a, at, 0, empty ? 0.f : o.x * inv);
-    store_result(a, at, 1, empty ? 0.f : o.y * inv);
+    const bool empty = n == 0;
+    const float inv = a.out_scale / l;
+    const int64_t at = (int64_t)id * D + 2 * lane;
+    const float x = empty ? 0.f : o.x * inv, y = empty ? 0.f : o.y * inv;
+    if (a.out_bf16) *(unsigned*)((unsigned short*)a.out + at) = (unsigned)float_to_bf16_bits(x) | ((unsigned)float_to_bf16_bits(y) << 16);
+    else *(float2*)((float*)a.out + at) = make_float2(x, y);
   }
 }
 
