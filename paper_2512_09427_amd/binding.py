@@ -178,10 +178,16 @@ def _rows(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_raw_stream = None           # torch's own short way to the current stream, where it has one (a Stream object costs 2.5 us a call)
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
+        global _raw_stream
         import torch
-        return torch.cuda.current_stream().cuda_stream or None
+        if _raw_stream is None:
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+        return _raw_stream(torch.cuda.current_device()) or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None

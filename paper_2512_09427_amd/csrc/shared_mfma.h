@@ -6,13 +6,16 @@
 // so the prefix can be attended to by the queries of all its requests together: (requests x heads of a KV head's group)
 // columns against its tokens, a dense contraction with reuse, where a request by itself only streams.
 //
-// Two lines of work.  Line A: items (prefix, KV head, block of SHARED_COLS columns), each the pairs of 16-token tiles of the
-// prefix.  Line B: items (request, KV head), each the tiles of the request's own tokens.  Items are cut into chunks of tokens so
-// that every work-group gets a like share of either line, and line A's matrix instructions run beside line B's memory traffic on
+// Two lines of work.  Line A: items (prefix, KV head, block of SHARED_COLS columns), cut into chunks of pairs of 16-token tiles, a
+// work-group's piece each.  Line B: items (request, KV head), each the pairs of tiles of the request's own tokens; the line is cut
+// into equal shares, one for every wave, which streams its share across the items in it, straight into registers.  Every
+// work-group gets a like share of both lines, so that line A's matrix instructions run beside line B's memory traffic on
 // every compute unit without a number that weighs one against the other: half of the work-groups begin with A, half with B.
-// A chunk's piece leaves its state in the workspace and shared_merge_kernel joins them.  Line A is ordered (prefix, KV head,
-// chunk, column block): the work-groups of an XCD read the same few chunks at a time, out of its L2.
+// Each piece of an item leaves its state in the workspace and shared_merge_kernel joins them.  Line A is ordered (prefix, KV
+// head, chunk, column block): the work-groups of an XCD read the same few chunks at a time, out of its L2.
 #pragma once
+
+#include <type_traits>
 
 #include "kernels_common.h"
 #include "prefixes.h"
@@ -25,18 +28,17 @@ enum { SHARED_BF16_128, SHARED_FP8_128, SHARED_BF16_64 };
 constexpr int SHARED_COLS = 128;          // columns of an item of line A: four waves of two 16-column tiles
 constexpr int SHARED_CT = 2;
 constexpr int SHARED_A_EXTRA = 5;         // start and end of a piece of line A, in pairs
-constexpr int SHARED_B_EXTRA = 8;         // and of line B, in tiles
-constexpr int SHARED_A_LEAST = 8;         // pairs and tiles below which an item is not cut
-constexpr int SHARED_B_LEAST = 12;
-constexpr int SHARED_B_PIECES = 2;        // pieces of line B that a work-group gets on the average, where items are long enough
+constexpr int SHARED_A_LEAST = 8;         // pairs below which an item of line A is not cut
+constexpr int SHARED_B_EXTRA = 2;         // start and end of an item of line B, in units
+constexpr int SHARED_B_LEAST = 2;         // units that a wave is given at least, beside an item's start and end
 constexpr int SHARED_MAX_N = ODMA_SHARED_MAX_REQUESTS;
-constexpr int SHARED_THREADS = 256;
+constexpr int SHARED_THREADS = 256, SHARED_WAVES = SHARED_THREADS / 64;
 
 struct SharedRecord {                     // of a request, for the merge
   int32_t a_chunks, a_blocks, a_col;      // line A: chunks (0: it shares nothing) and column blocks of an item, its first column
   int32_t a_extra;                        // cut pieces (chunks behind the first) in front of its group's
-  int32_t b_chunks, b_extra;              // line B
-  int32_t pad0, pad1;
+  int32_t b_pos, b_units;                 // line B: place of its first head's item, units of an item
+  int32_t b_total, b_used;                // of the line: units and waves
 };
 
 struct SharedArgs {
@@ -57,48 +59,62 @@ struct SharedArgs {
   float* part_o;                          // [column][128]
 };
 
-// Columns of the workspace: first chunks of line A and of line B by (request, head), then the chunks behind them, in the order of
-// their line: at most `workers` of line A (SharedCut) and SHARED_B_PIECES times as many of line B.
+// Columns of the workspace: first pieces of line A and of line B by (request, head); then line A's chunks behind the first, at most
+// `workers` (SharedCut); then of every wave the piece of the item that its share begins inside of.
 __device__ __forceinline__ int64_t shared_first(const SharedArgs& a, int line, int r, int hq) {
   return ((int64_t)line * a.n + r) * a.Hq + hq;
 }
 __device__ __forceinline__ int64_t shared_cut_a(const SharedArgs& a, int i) { return (int64_t)2 * a.n * a.Hq + (int64_t)i * a.cut_cols; }
-__device__ __forceinline__ int64_t shared_cut_b(const SharedArgs& a, int i) {
-  return (int64_t)2 * a.n * a.Hq + (int64_t)a.workers * a.cut_cols + (int64_t)i * 16;
+__device__ __forceinline__ int64_t shared_cut_b(const SharedArgs& a, int w) {
+  return (int64_t)2 * a.n * a.Hq + (int64_t)a.workers * a.cut_cols + (int64_t)w * a.G;
 }
 
-// How a line with `units` in `items` items is cut for `pieces` pieces in all: into chunks of at most `length`.  An item of T units
-// has (T - 1) / length chunks behind its first, fewer than T / length, so all items together have fewer than units / length, which
-// is at most `pieces` (half of them where items abound, so that they are cut little).
-struct SharedCut {
-  int length, shift;                                        // costs count 2^shift units, so that a line's sum fits 30 bits
-  __device__ __forceinline__ SharedCut(float units, int items, int pieces, int least) {
-    const float l = units * 1.0002f / (float)max(pieces - items, pieces / 2);   // (the sum is within 2^-13)
-    length = max((int)fminf(l, 1e9f) + 1, least);
-    shift = max(ilogbf(fmaxf(units, 1.f)) - 27, 0);
-  }
-  __device__ __forceinline__ int chunks(int T) const { return (T + length - 1) / length; }
-};
+// a / b for 0 <= a, 0 < b and quotients below 2^20 (the reciprocal's error is less than one there)
+__device__ __forceinline__ int small_quotient(int a, int b) {
+  int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));
+  q -= q * b > a;
+  q += (q + 1) * b <= a;
+  return q;
+}
 
+// How line A with `units` pairs in `items` items is cut for `pieces` work-groups: into chunks of at most about `length`.  An item of T
+// pairs has fewer than T / length chunks behind its first, all items together fewer than units / length, which is at
+// most `pieces` (half of them where items abound, so that they are cut little).
+struct SharedCut {
+  float inv_length;
+  int shift;                                                // costs count 2^shift pairs, so that the line's sum fits 30 bits
+  __device__ __forceinline__ SharedCut(float units, int items, int pieces, int least) {
+    const float length = fmaxf(units * 1.0005f * __builtin_amdgcn_rcpf((float)max(pieces - items, pieces / 2)), (float)least);   // (the sum is within 2^-13)
+    inv_length = __builtin_amdgcn_rcpf(length);
+    shift = max((int)(__float_as_uint(units) >> 23) - 127 - 27, 0);
+  }
+  __device__ __forceinline__ int chunks(int T) const { return max((int)ceilf((float)T * inv_length), 1); }
+};
 // first unit of a chunk of an item of T units: chunks differ by one at most
 __device__ __forceinline__ int chunk_start(int T, int chunks, int chunk) {
   const int base = T / chunks;
   return chunk * base + min(chunk, T - chunks * base);
 }
+// The N pieces of a group that begins at s on line A's cost and costs c are spread over it evenly: how many begin in front of x.
+__device__ __forceinline__ int pieces_before(int x, int s, int c, int N) {
+  return x <= s ? 0 : x >= s + c ? N : min((int)ceilf((float)(x - s) * (float)N / (float)c), N);   // (monotone in x)
+}
 
-// Work-group w takes the pieces of its share [start(w), start(w + 1)) of a line's cost.  The N pieces of an entry (a group, a request)
-// that begins at s and costs c are spread over it evenly.
-struct SharedShare {
-  int x0, x1;
-  __device__ __forceinline__ SharedShare(int total, int used, int w) {
-    const double step = (double)total / (double)used;
-    x0 = (int)((double)w * step);
-    x1 = w + 1 >= used ? total : (int)((double)(w + 1) * step);
-  }
-  static __device__ __forceinline__ int upto(int x, int s, int c, int N) {
-    return x <= s ? 0 : x >= s + c ? N : min((int)ceilf((float)(x - s) * (float)N / (float)c), N);   // (monotone in x)
+// Line B: wave w's share is [start(w), start(w + 1)), a unit at least.  An item at s with T units has unit 0 at s and unit i at
+// s + SHARED_B_EXTRA + i, and a unit belongs to the share that holds its position.
+struct SharedLine {
+  int total, used;
+  double step;
+  __device__ __forceinline__ SharedLine(int total_, int used_) : total(total_), used(used_), step((double)total_ / (double)used_) {}
+  __device__ __forceinline__ int start(int w) const { return w >= used ? total : (int)((double)w * step); }
+  __device__ __forceinline__ int holder(int pos) const {
+    const int w = min((int)((float)pos * (float)used * __builtin_amdgcn_rcpf((float)total)), used - 1);
+    return start(w) > pos ? w - 1 : start(w + 1) <= pos ? w + 1 : w;   // (the quotient, below 2^14, is within one)
   }
 };
+__device__ __forceinline__ int units_before(int x, int s, int T) {
+  return x <= s ? 0 : min(max(x - s - SHARED_B_EXTRA, 1), T);
+}
 
 template <bool HIGH_HALF>
 __device__ __forceinline__ unsigned widen_e4m3x2(unsigned w) {
@@ -108,17 +124,21 @@ __device__ __forceinline__ unsigned widen_e4m3x2(unsigned w) {
 }
 
 struct SharedPlan {
-  int32_t a_pos[SHARED_MAX_N + 1], b_pos[SHARED_MAX_N + 1];   // cost in front of a group on line A, of a request on line B
-  int32_t a_extra[SHARED_MAX_N], b_extra[SHARED_MAX_N];       // cut pieces in front of them
-  int32_t start[SHARED_MAX_N + 1];                            // first request of a group
-  int32_t tiles[SHARED_MAX_N];                                // of a group's shared part
-  int32_t reader[SHARED_MAX_N];                               // of a group: its first request that holds all of the shared part
-  int32_t own[SHARED_MAX_N];                                  // of a request: tokens that it reads itself
-  int32_t skip[SHARED_MAX_N];                                 // ... and the blocks of its tokens in front of them (-1: in its group's prefix)
-  float wave_units[SHARED_THREADS / 64];
-  int32_t wave_items[SHARED_THREADS / 64];
-  int32_t wave_sum[SHARED_THREADS / 64][4];
+  // requests
+  int32_t own[SHARED_MAX_N];              // tokens that it reads itself; SHARES: and all of its group's shared ones with the group
+  int32_t base[SHARED_MAX_N];             // block of the first of them, or its place in the request's row of the block table
+  int32_t b_pos[SHARED_MAX_N + 1];        // units of line B in front of it
+  // groups
+  int32_t start[SHARED_MAX_N + 1];        // first request
+  int32_t tiles[SHARED_MAX_N];            // of the shared part
+  int32_t first_block[SHARED_MAX_N];      // (contiguous)
+  int32_t reader[SHARED_MAX_N];           // its first request that holds all of the shared part
+  int32_t a_pos[SHARED_MAX_N + 1];        // cost of line A in front of it
+  int32_t a_extra[SHARED_MAX_N];          // cut pieces in front of it
+  float units[SHARED_WAVES][2];
+  int32_t items[SHARED_WAVES], sums[SHARED_WAVES][3];
 };
+constexpr int SHARES = (int)0x80000000;
 
 __device__ __forceinline__ int tiles_of(int tokens) { return (int)(((int64_t)tokens + BLK - 1) / BLK); }
 __device__ __forceinline__ int column_blocks(int count, int G) { return (count * G + SHARED_COLS - 1) / SHARED_COLS; }
@@ -134,6 +154,36 @@ __device__ __forceinline__ void two_parts(float w, __bf16& hi, __bf16& lo) {
   lo = (__bf16)fmaxf(w - __uint_as_float(bits), w * 0x1p-40f);
 }
 
+// inclusive sums over the lanes of a wave, by moves inside rows of 16 and broadcasts between them
+template <typename T>
+__device__ __forceinline__ T lanes_sum(T x) {
+  auto moved = [](T v, auto ctrl, auto rows) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+  };
+  using std::integral_constant;
+  x += moved(x, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});
+  x += moved(x, integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  x += moved(x, integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  x += moved(x, integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  x += moved(x, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
+  x += moved(x, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+  return x;
+}
+
+// Last entry of pos[0 .. n) (which does not decrease, and begins with 0) that is at most x >= 0; n <= 4096.
+__device__ __forceinline__ int last_at_most(const int32_t* pos, int n, int x) {
+  const int lane = threadIdx.x & 63;
+  auto probe = [&](int i) { return __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < n && pos[min(i, n - 1)] <= x)); };
+  int lo = 0;
+  if (n > 64) {
+    const int span = (n + 63) / 64;
+    lo = (probe(lane * span) - 1) * span;
+    const int last = min(span, n - lo);
+    return lo + __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < last && pos[min(lo + lane, n - 1)] <= x)) - 1;
+  }
+  return probe(lane) - 1;
+}
+
 // LO: the weights of line A go through the matrix cores as two bf16 parts (16 bits) instead of one; for fp32 results.
 // (Line B, bound by memory, always does.)  A single rounding of a weight is half a bf16 step of one term of the sum, as the
 // rounding of a bf16 result is of the whole.
@@ -146,9 +196,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
   constexpr int K_STAGE = 2 * NS * 1024, STAGE_BYTES = 2 * K_STAGE;
   constexpr int CT = SHARED_CT;
   constexpr float SLACK = 8.0f;                             // exponent units by which a score may exceed the reference
-  constexpr int MERGE_BYTES = 4 * 16 * D * 4;               // line B: the waves' states
-  __shared__ __attribute__((aligned(16))) char stage_mem[2 * STAGE_BYTES > MERGE_BYTES ? 2 * STAGE_BYTES : MERGE_BYTES];
-  __shared__ float2 wave_ml[4][16];
+  __shared__ __attribute__((aligned(16))) char stage_mem[2 * STAGE_BYTES];
   __shared__ SharedPlan plan;
   const int tid = threadIdx.x, lane = tid & 63, wv = rfl(tid >> 6);
   const int col16 = lane & 15, g4 = lane >> 4;
@@ -157,63 +205,64 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
 
   // ---- plan: every work-group for itself (a launch of its own would be one work-group's round trips on an empty chip).  One
   // round of loads, then LDS alone.
-  const int per = (a.n + SHARED_THREADS - 1) / SHARED_THREADS;
+  const int per = (a.n + SHARED_THREADS - 1) / SHARED_THREADS, perp = (a.n_prefixes + SHARED_THREADS - 1) / SHARED_THREADS;
   const int r0 = min(tid * per, a.n), r1 = min(r0 + per, a.n);
-  for (int r = tid; r < a.n; r += SHARED_THREADS) plan.own[r] = a.lengths[r];
+  const int p0 = min(tid * perp, a.n_prefixes), p1 = min(p0 + perp, a.n_prefixes);
+  for (int r = tid; r < a.n; r += SHARED_THREADS) {
+    plan.own[r] = max(a.lengths[r], 0);
+    if (!PAGED) plan.base[r] = (int)(a.offsets[r] / BLK);
+  }
   for (int p = tid; p <= a.n_prefixes; p += SHARED_THREADS) {
     plan.start[p] = min(max(a.prefix_start[p], 0), a.n);
     if (p < a.n_prefixes) {
       plan.tiles[p] = shared_tokens(a.prefix_lengths[p]) / BLK;
+      if (!PAGED) plan.first_block[p] = (int)(a.prefix_offsets[p] / BLK);
       plan.reader[p] = a.n;
     }
   }
   __syncthreads();
-  float units = 0.f;
-  int items = 0;
+  auto group_blocks = [&](int p) { return plan.tiles[p] ? column_blocks(max(plan.start[p + 1] - plan.start[p], 0), G) : 0; };
+  float units[2] = {0.f, 0.f};                               // pairs of lines A and B, per KV head
+  int items = 0;                                             // of line A
   for (int r = r0; r < r1; ++r) {
-    const int len = max(plan.own[r], 0), p = prefix_of(plan.start, a.n_prefixes, r), shared = p >= 0 ? plan.tiles[p] * BLK : 0;
+    const int len = plan.own[r], p = prefix_of(plan.start, a.n_prefixes, r), shared = p >= 0 ? plan.tiles[p] * BLK : 0;
     const bool shares = shared > 0 && len >= shared;
-    if (shares) atomicMin(&plan.reader[p], r);
     const int own = shares ? len - shared : len;
-    plan.own[r] = own;
-    plan.skip[r] = shares ? shared / BLK : shared > 0 ? -1 : 0;
-    units += (float)tiles_of(own);
-    items += own > 0;
+    plan.own[r] = own | (shares ? SHARES : 0);
+    if (shares) atomicMin(&plan.reader[p], r);
+    // its own slab, behind its shared blocks in a row of the table; a request shorter than the shared part reads its group's prefix
+    if (PAGED) plan.base[r] = shares ? shared / BLK : 0;
+    else if (shared > 0 && !shares) plan.base[r] = plan.first_block[p];
+    units[1] += (float)(tiles_of(own) / 2 + 1);
   }
-  units = wave_sum(units);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) items += __shfl_xor(items, o);
-  if (lane == 0) {
-    plan.wave_units[wv] = units;
-    plan.wave_items[wv] = items;
-  }
-  __syncthreads();
-  units = 0.f;
-  items = 0;
-  for (int i = 0; i < SHARED_THREADS / 64; ++i) {
-    units += plan.wave_units[i];
-    items += plan.wave_items[i];
-  }
-  const int b_items = items;
-  const SharedCut cut_b(units * (float)a.Hkv, items * a.Hkv, SHARED_B_PIECES * a.workers, SHARED_B_LEAST);
-  // groups, every wave for itself
-  auto group_blocks = [&](int p) {                          // column blocks of a KV head; 0: nobody attends to the prefix
-    return plan.reader[p] < a.n ? column_blocks(plan.start[p + 1] - plan.start[p], G) : 0;
-  };
-  units = 0.f;
-  items = 0;
-  for (int p = lane; p < a.n_prefixes; p += 64) {
+  for (int p = p0; p < p1; ++p) {
     const int blocks = group_blocks(p);
-    units += (float)blocks * (float)((plan.tiles[p] + 1) / 2);
+    units[0] += (float)blocks * (float)((plan.tiles[p] + 1) / 2);
     items += blocks;
   }
-  units = wave_sum(units);
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) items += __shfl_xor(items, o);
-  const SharedCut cut_a(units * (float)a.Hkv, items * a.Hkv, a.workers, SHARED_A_LEAST);
-  // costs and cut pieces, and their exclusive sums
-  const int perp = (a.n_prefixes + SHARED_THREADS - 1) / SHARED_THREADS;
-  const int p0 = min(tid * perp, a.n_prefixes), p1 = min(p0 + perp, a.n_prefixes);
+  for (int i = 0; i < 2; ++i) units[i] = lanes_sum(units[i]);
+  items = lanes_sum(items);
+  if (lane == 63) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) plan.units[wv][i] = units[i];
+    plan.items[wv] = items;
+  }
+  __syncthreads();
+  units[0] = units[1] = 0.f;
+  items = 0;
+#pragma unroll
+  for (int w = 0; w < SHARED_WAVES; ++w) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) units[i] += plan.units[w][i];
+    items += plan.items[w];
+  }
+  const SharedCut cut_a(units[0] * (float)a.Hkv, items * a.Hkv, a.workers, SHARED_A_LEAST);
+  // A unit of line B: 2^shift_b pairs, so that the line fits 30 bits (it always does unless tables name the same blocks over and over).
+  const int shift_b = rfl(max((int)(__float_as_uint(units[1] * (float)a.Hkv) >> 23) - 127 - 28, 0));
+  auto pairs_b = [&](int r) { return (tiles_of(plan.own[r] & ~SHARES) + 1) / 2; };
+  auto units_b = [&](int r) { return (pairs_b(r) + (1 << shift_b) - 1) >> shift_b; };
+  int sum[3] = {0, 0, 0};
   struct Entry {
     int cost, extra;
   };
@@ -222,44 +271,34 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
     if (!blocks) return Entry{0, 0};
     return Entry{(int)((int64_t)a.Hkv * blocks * (pairs + chunks * SHARED_A_EXTRA) >> cut_a.shift) + 1, a.Hkv * blocks * (chunks - 1)};
   };
-  auto request_entry = [&](int r) {
-    const int tiles = tiles_of(plan.own[r]), chunks = cut_b.chunks(tiles);
-    if (!tiles) return Entry{0, 0};
-    return Entry{(int)((int64_t)a.Hkv * (tiles + chunks * SHARED_B_EXTRA) >> cut_b.shift) + 1, a.Hkv * (chunks - 1)};
+  auto request_cost = [&](int r) {
+    const int T = units_b(r);
+    return T ? a.Hkv * (T + SHARED_B_EXTRA) : 0;
   };
-  int sum[4] = {0, 0, 0, 0};
   for (int p = p0; p < p1; ++p) {
     const Entry e = group_entry(p);
     sum[0] += e.cost;
     sum[1] += e.extra;
   }
-  for (int r = r0; r < r1; ++r) {
-    const Entry e = request_entry(r);
-    sum[2] += e.cost;
-    sum[3] += e.extra;
-  }
-  int before[4], total[4];
+  for (int r = r0; r < r1; ++r) sum[2] += request_cost(r);
+  int before[3], total[3];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) before[i] = sum[i];
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int y = __shfl_up(before[i], o);
-      if (lane >= o) before[i] += y;
-    }
+  for (int i = 0; i < 3; ++i) before[i] = lanes_sum(sum[i]);
   if (lane == 63)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) plan.wave_sum[wv][i] = before[i];
+    for (int i = 0; i < 3; ++i) plan.sums[wv][i] = before[i];
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 3; ++i) {
     before[i] -= sum[i];
     total[i] = 0;
-    for (int w = 0; w < SHARED_THREADS / 64; ++w) {
-      if (w < wv) before[i] += plan.wave_sum[w][i];
-      total[i] += plan.wave_sum[w][i];
+#pragma unroll
+    for (int w = 0; w < SHARED_WAVES; ++w) {
+      const int x = plan.sums[w][i];
+      if (w < wv) before[i] += x;
+      total[i] += x;
     }
+    total[i] = rfl(total[i]);
   }
   for (int p = p0; p < p1; ++p) {
     const Entry e = group_entry(p);
@@ -269,21 +308,27 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
     before[1] += e.extra;
   }
   for (int r = r0; r < r1; ++r) {
-    const Entry e = request_entry(r);
     plan.b_pos[r] = before[2];
-    plan.b_extra[r] = before[3];
-    before[2] += e.cost;
-    before[3] += e.extra;
+    before[2] += request_cost(r);
   }
   if (tid == 0) {
     plan.a_pos[a.n_prefixes] = total[0];
     plan.b_pos[a.n] = total[2];
   }
   __syncthreads();
+  // Shares.  XCD x (work-groups x, x + 8, ..) has neighbouring ones, which read the same heads.  A short line goes to few work-groups, the
+  // first ones of every XCD (A) or the last (B).
+  const int pieces_a = total[1] + items * a.Hkv, least_b = SHARED_WAVES * (SHARED_B_LEAST + SHARED_B_EXTRA);
+  const int used_a = rfl(total[0] ? min((min(pieces_a, a.workers) + 7) / 8 * 8, a.workers) : 0);
+  const int used_b = rfl(total[2] ? min((total[2] / least_b / 8 + 1) * 8, a.workers) : 0);
+  const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, turns = a.workers >> 3;
+  const int waves_b = min(used_b * SHARED_WAVES, total[2]);    // (a share is a unit at least)
+  const int ja = used_a >> 3, jb = used_b >> 3;
+  const int share_a = turn < ja ? xcd * ja + turn : -1, share_b = turns - 1 - turn < jb ? xcd * jb + turns - 1 - turn : -1;
   if (blockIdx.x == gridDim.x - 1) {                        // for the merge
     for (int r = tid; r < a.n; r += SHARED_THREADS) {
-      SharedRecord rec = {0, 0, 0, 0, cut_b.chunks(tiles_of(plan.own[r])), plan.b_extra[r], 0, 0};
-      if (plan.skip[r] > 0) {
+      SharedRecord rec = {0, 0, 0, 0, plan.b_pos[r], units_b(r), total[2], waves_b};
+      if (plan.own[r] & SHARES) {
         const int p = prefix_of(plan.start, a.n_prefixes, r);
         rec.a_chunks = cut_a.chunks((plan.tiles[p] + 1) / 2);
         rec.a_blocks = group_blocks(p);
@@ -293,13 +338,6 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
       a.rec[r] = rec;
     }
   }
-  // XCD x (work-groups x, x + 8, ..) has neighbouring shares, which read the same heads.  A short line goes to few work-groups (a piece
-  // each), the first ones of every XCD (A) or the last (B).
-  auto used_of = [&](int cost, int pieces) { return cost ? min((min(pieces, a.workers) + 7) / 8 * 8, a.workers) : 0; };
-  const int used_a = used_of(total[0], total[1] + items * a.Hkv), used_b = used_of(total[2], total[3] + b_items * a.Hkv);
-  const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, turns = a.workers >> 3;
-  const int ja = used_a >> 3, jb = used_b >> 3;
-  const int share_a = turn < ja ? xcd * ja + turn : -1, share_b = turns - 1 - turn < jb ? xcd * jb + turns - 1 - turn : -1;
 
   auto piece = [&](const uint4v (&w)[LOADS], int s) {       // 16-byte operand s (of NS) of a tile, as bf16
     if (!FP8) return w[s % LOADS];
@@ -319,29 +357,25 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
     bf16x8 ones;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
-    const SharedShare share(total[0], used_a, share_a);
-    // group that holds x0: the last one at or before it (groups without work repeat a position)
-    int lo = 0, hi = a.n_prefixes;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (plan.a_pos[mid] <= share.x0) lo = mid;
-      else hi = mid;
-    }
-    for (int p = rfl(lo); p < a.n_prefixes && plan.a_pos[p] < share.x1; ++p) {
-      const int pos = rfl(plan.a_pos[p]), cost = rfl(plan.a_pos[p + 1]) - pos;
-      if (!cost) continue;
+    const double step_a = (double)total[0] / (double)used_a;
+    const int x0 = rfl((int)((double)share_a * step_a)), x1 = rfl(share_a + 1 >= used_a ? total[0] : (int)((double)(share_a + 1) * step_a));
+    for (int p = rfl(last_at_most(plan.a_pos, a.n_prefixes, x0)); p < a.n_prefixes; ++p) {
+      const int pos = rfl(plan.a_pos[p]), cost = rfl(plan.a_pos[p + 1]) - pos, reader = rfl(plan.reader[p]);
+      if (pos >= x1) break;
+      if (!cost || reader == a.n) continue;                  // (nobody attends to it)
       const int begin = rfl(plan.start[p]), count = rfl(plan.start[p + 1]) - begin;
-      const int n_tiles = rfl(plan.tiles[p]), pairs = (n_tiles + 1) / 2, chunks = cut_a.chunks(pairs);
-      const int blocks = column_blocks(count, G), per_head = chunks * blocks, n_pieces = a.Hkv * per_head, n_cols = count * G;
-      const int64_t base_block = PAGED ? 0 : ((const const_i64s*)(uintptr_t)a.prefix_offsets)[p] / BLK;
-      const const_i32* bt_row = as_constant(PAGED ? a.bt + (int64_t)rfl(plan.reader[p]) * a.bt_stride : nullptr);
-      const int last = rfl(SharedShare::upto(share.x1, pos, cost, n_pieces));
-      for (int id = rfl(SharedShare::upto(share.x0, pos, cost, n_pieces)); id < last; ++id) {
-        const int g = rfl(id / per_head), chunk = rfl((id - g * per_head) / blocks), cb = id - g * per_head - chunk * blocks;
+      const int n_tiles = rfl(plan.tiles[p]), pairs = (n_tiles + 1) / 2, chunks = rfl(cut_a.chunks(pairs));
+      const int blocks = rfl(column_blocks(count, G)), per_head = chunks * blocks, n_pieces = a.Hkv * per_head, n_cols = count * G;
+      const int64_t base_block = PAGED ? 0 : rfl(plan.first_block[p]);
+      const const_i32* bt_row = as_constant(PAGED ? a.bt + (int64_t)reader * a.bt_stride : nullptr);
+      const int last = rfl(pieces_before(x1, pos, cost, n_pieces));
+      for (int id = rfl(pieces_before(x0, pos, cost, n_pieces)); id < last; ++id) {
+        const int g = rfl(small_quotient(id, per_head)), chunk = rfl(small_quotient(id - g * per_head, blocks));
+        const int cb = id - g * per_head - chunk * blocks;
         const int i0 = rfl(chunk_start(pairs, chunks, chunk)), i1 = rfl(chunk_start(pairs, chunks, chunk + 1));
         const int cut = chunk ? rfl(plan.a_extra[p]) + (g * (chunks - 1) + chunk - 1) * blocks + cb : -1;
         const int c0 = cb * SHARED_COLS + wv * 16 * CT;
-        const bool active = c0 < n_cols;
+        const bool active = rfl(c0 < n_cols);
         const int64_t plane = (int64_t)g * a.head_stride;
 
         bool ok[CT];
@@ -363,45 +397,42 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
         }
         // A column's reference m, in raw scores, enters with the accumulators of its scores (minus m instead of 0); -inf: none yet.
         // The sum of its weights is one more row of P V, with V = 1.
-        float m[CT];
-        float4v minus_m[CT], l[CT], O[CT][DT];
+        float m[CT], minus_m[CT];
+        float4v l[CT], O[CT][DT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
           m[ct] = -INFINITY;
-          minus_m[ct] = l[ct] = float4v{0.f, 0.f, 0.f, 0.f};
+          minus_m[ct] = 0.f;
+          l[ct] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) O[ct][dt] = float4v{0.f, 0.f, 0.f, 0.f};
         }
 
         // loading: waves 0 and 1 bring K of the first and second tile of a pair, 2 and 3 V.  A second tile that does not exist
-        // re-reads the first with its V zeroed (its scores are masked).
+        // re-reads the first with its V zeroed (its scores are masked).  K runs a pair ahead of V: load j is pair i0 + j of K and
+        // i0 + j - 1 of V.
         const bool loads_v = wv >= 2;
-        const int which = wv & 1;
+        const int which = wv & 1, behind = loads_v ? 1 : 0;
         const char* src_base = (loads_v ? a.v : a.k) + plane;
-        auto tile_of = [&](int pr) { return min(2 * min(pr, i1 - 1) + which, n_tiles - 1); };
+        auto pair_of = [&](int j) { return min(max(i0 + j - behind, i0), i1 - 1); };
+        auto tile_of = [&](int j) { return min(2 * pair_of(j) + which, n_tiles - 1); };
         int blk_next = 0;
-        auto lookup = [&](int pr) {
-          if (PAGED) blk_next = bt_row[tile_of(pr)];
+        auto lookup = [&](int j) {
+          if (PAGED) blk_next = bt_row[tile_of(j)];
         };
-        auto issue = [&](uint4v (&rg)[LOADS], int pr) {
-          const char* src = src_base + (PAGED ? (int64_t)blk_next : base_block + tile_of(pr)) * TILE_BYTES;
+        auto issue = [&](uint4v (&rg)[LOADS], int j) {
+          const char* src = src_base + (PAGED ? (int64_t)blk_next : base_block + tile_of(j)) * TILE_BYTES;
 #pragma unroll
           for (int i = 0; i < LOADS; ++i) rg[i] = *(const uint4v*)(src + i * 1024 + lane16);
         };
-        auto write_stage = [&](const uint4v (&rg)[LOADS], int pr) {
-          char* st = stage_mem + ((pr - i0) & 1) * STAGE_BYTES;
-          const bool absent = 2 * min(pr, i1 - 1) + which >= n_tiles;
+        auto write_stage = [&](const uint4v (&rg)[LOADS], int j) {
+          char* st = stage_mem + ((j - behind) & 1) * STAGE_BYTES;
           if (!loads_v) {
-            if (FP8) {
 #pragma unroll
-              for (int sp = 0; sp < NS; ++sp)
-                *(uint4v*)(st + which * NS * 1024 + ((4 * sp + g4) * 16 + col16) * 16) = piece(rg, sp);
-            } else {
-#pragma unroll
-              for (int i = 0; i < LOADS; ++i) *(uint4v*)(st + which * NS * 1024 + i * 1024 + lane16) = rg[i];
-            }
+            for (int sp = 0; sp < NS; ++sp) *(uint4v*)(st + which * NS * 1024 + sp * 1024 + lane16) = piece(rg, sp);
           } else {
             char* dst = st + K_STAGE + lane16 + which * 8;
+            const bool absent = 2 * pair_of(j) + which >= n_tiles;
 #pragma unroll
             for (int sp = 0; sp < NS; ++sp) {
               uint4v w = piece(rg, sp);
@@ -411,13 +442,8 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
             }
           }
         };
-        bool fresh = true;                                   // some column of the wave has no reference
-        auto compute = [&](int pr) {
-          const char* st = stage_mem + ((pr - i0) & 1) * STAGE_BYTES + lane16;
-          bf16x8 av[DT];
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) av[dt] = *(const bf16x8*)(st + K_STAGE + dt * 1024);
-          float4v x[CT][2];
+        auto scores = [&](float4v (&x)[CT][2], int j) {       // of pair i0 + j, less the references
+          const char* st = stage_mem + (j & 1) * STAGE_BYTES + lane16;
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             bf16x8 kk[NS];
@@ -425,12 +451,16 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
             for (int sp = 0; sp < NS; ++sp) kk[sp] = *(const bf16x8*)(st + b * NS * 1024 + sp * 1024);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-              float4v s4 = minus_m[ct];
+              const float mm = minus_m[ct];
+              float4v s4 = float4v{mm, mm, mm, mm};
 #pragma unroll
               for (int sp = 0; sp < NS; ++sp) s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[sp], qreg[ct][sp], s4, 0, 0, 0);
               x[ct][b] = s4;
             }
           }
+        };
+        int fresh = 1;                                        // some column of the wave has no reference
+        auto settle = [&](float4v (&x)[CT][2], int pr) {      // scores of pair pr: masked, and below the references by SLACK at most
           if (2 * pr + 1 >= n_tiles) {
             asm volatile("");                                // (a branch: once an item, against eight selects a pair)
 #pragma unroll
@@ -439,8 +469,8 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
           float top = -INFINITY;
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) top = larger(top, largest(x[ct]));
-          if (fresh || __builtin_amdgcn_ballot_w64(top > slack) != 0) {
-            fresh = false;
+          if (rfl(fresh | (__builtin_amdgcn_ballot_w64(top > slack) != 0))) {
+            fresh = 0;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
               float up = largest(x[ct]);
@@ -456,8 +486,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
                 f = joined(0.f, up * a.scale_log2);
               }
               fresh |= __builtin_amdgcn_ballot_w64(m[ct] == -INFINITY) != 0;
-              const float mm = m[ct] == -INFINITY ? 0.f : -m[ct];
-              minus_m[ct] = float4v{mm, mm, mm, mm};
+              minus_m[ct] = m[ct] == -INFINITY ? 0.f : -m[ct];
               l[ct] *= f;
 #pragma unroll
               for (int b = 0; b < 2; ++b)
@@ -467,9 +496,16 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
               for (int dt = 0; dt < DT; ++dt) O[ct][dt] *= f;
             }
           }
+        };
+        // Pair pr: its weights (vector instructions) beside the scores of the pair behind it (matrix instructions), then P V.  One
+        // wave's halves overlap by themselves: with scores, weights and P V one after the other a SIMD's two waves needed
+        // 2667 cycles for a pair each.
+        auto compute = [&](float4v (&x)[CT][2], float4v (&ahead)[CT][2], int pr) {
+          settle(x, pr);
+          scores(ahead, pr + 1 - i0);
           bf16x8 ph[CT], pl[CT];
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
+          for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -484,39 +520,50 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
                   ph[ct][4 * b + i] = (__bf16)pv;
                 }
               }
+          const char* st = stage_mem + ((pr - i0) & 1) * STAGE_BYTES + K_STAGE + lane16;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
             l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, ph[ct], l[ct], 0, 0, 0);
             if (LO) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pl[ct], l[ct], 0, 0, 0);
           }
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
+          for (int dt = 0; dt < DT; ++dt) {
+            const bf16x8 av = *(const bf16x8*)(st + dt * 1024);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-              O[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], ph[ct], O[ct][dt], 0, 0, 0);
-              if (LO) O[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], pl[ct], O[ct][dt], 0, 0, 0);
+              O[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, ph[ct], O[ct][dt], 0, 0, 0);
+              if (LO) O[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, pl[ct], O[ct][dt], 0, 0, 0);
             }
+          }
         };
-        // pipeline: the loads of pair p + 2 are in flight while pair p is computed; pair p + 1 goes from registers into the
-        // other stage behind it, and one barrier per pair makes it visible
+        // pipeline: load j + 3 is under way while pair j is computed; load j + 2 goes from registers into its stage behind it, where
+        // pair j + 1 finds it, and one barrier per pair makes it visible
         uint4v ra[LOADS], rb[LOADS];
-        lookup(i0);
-        issue(ra, i0);
-        lookup(i0 + 1);
-        issue(rb, i0 + 1);
-        lookup(i0 + 2);
+        float4v xa[CT][2], xb[CT][2];
+        lookup(0);
+        issue(ra, 0);
+        lookup(1);
+        issue(rb, 1);
+        lookup(2);
         __syncthreads();                                     // the stages of the piece before are done with
-        write_stage(ra, i0);
+        write_stage(ra, 0);
+        issue(ra, 2);
+        lookup(3);
         __syncthreads();
-        auto step = [&](uint4v (&near)[LOADS], uint4v (&far)[LOADS], int pr) {
-          issue(far, pr + 2);
-          lookup(pr + 3);
-          if (active) compute(pr);
-          write_stage(near, pr + 1);
+        if (active) scores(xa, 0);
+        write_stage(rb, 1);
+        __syncthreads();
+        auto step = [&](uint4v (&near)[LOADS], uint4v (&far)[LOADS], float4v (&x)[CT][2], float4v (&ahead)[CT][2], int pr) {
+          issue(far, pr - i0 + 3);
+          lookup(pr - i0 + 4);
+          if (active) compute(x, ahead, pr);
+          write_stage(near, pr - i0 + 2);
           __syncthreads();
         };
         for (int pr = i0;;) {
-          step(rb, ra, pr);
+          step(ra, rb, xa, xb, pr);
           if (++pr == i1) break;
-          step(ra, rb, pr);
+          step(rb, ra, xb, xa, pr);
           if (++pr == i1) break;
         }
 #pragma unroll
@@ -531,157 +578,158 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
     }
   };
 
-  // ================= line B: one request and KV head at a time; the waves take turns at its pairs of tiles, straight into registers
+  // ================= line B: every wave streams its share
   auto line_b = [&]() {
-    const SharedShare share(total[2], used_b, share_b);
-    int lo = 0, hi = a.n;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (plan.b_pos[mid] <= share.x0) lo = mid;
-      else hi = mid;
-    }
-    for (int r = rfl(lo); r < a.n && plan.b_pos[r] < share.x1; ++r) {
-      const int pos = rfl(plan.b_pos[r]), cost = rfl(plan.b_pos[r + 1]) - pos;
-      if (!cost) continue;
-      const int own = rfl(plan.own[r]), tiles = tiles_of(own), chunks = cut_b.chunks(tiles), n_pieces = a.Hkv * chunks, skip = rfl(plan.skip[r]);
-      // its own slab; a request shorter than the shared part reads its group's prefix
-      int64_t base_block = 0;
-      if (!PAGED)
-        base_block = (skip >= 0 ? ((const const_i64s*)(uintptr_t)a.offsets)[r]
-                                : ((const const_i64s*)(uintptr_t)a.prefix_offsets)[rfl(prefix_of(plan.start, a.n_prefixes, r))]) / BLK;
-      const const_i32* bt_row = as_constant(PAGED ? a.bt + (int64_t)r * a.bt_stride + max(skip, 0) : nullptr);
-      const int last = rfl(SharedShare::upto(share.x1, pos, cost, n_pieces));
-      for (int id = rfl(SharedShare::upto(share.x0, pos, cost, n_pieces)); id < last; ++id) {
-        const int g = rfl(id / chunks), chunk = id - g * chunks;
-        const int i0 = rfl(chunk_start(tiles, chunks, chunk)), i1 = rfl(chunk_start(tiles, chunks, chunk + 1));
-        const int cut = chunk ? rfl(plan.b_extra[r]) + g * (chunks - 1) + chunk - 1 : -1;
-        const int64_t plane = (int64_t)g * a.head_stride;
-        bf16x8 qreg[NS];
-        {
-          const unsigned short* qp = a.q + ((int64_t)r * a.Hq + g * G + min(col16, G - 1)) * D + 8 * g4;
-#pragma unroll
-          for (int st = 0; st < NS; ++st) {
-            const bf16x8 z = {0, 0, 0, 0, 0, 0, 0, 0};
-            qreg[st] = col16 < G ? *(const bf16x8*)(qp + 32 * st) : z;
+    const SharedLine line(total[2], waves_b);
+    const int w = share_b * SHARED_WAVES + wv;
+    if (w >= waves_b) return;
+    const int x0 = rfl(line.start(w)), x1 = rfl(line.start(w + 1));
+    struct Item {
+      int r, g, i0, i1;                                     // pairs [i0, i1) of the request's own tokens
+      int own, base;
+    };
+    // the first item at or behind (r, g) that has pairs in the share; r = n: there is none
+    auto item_from = [&](int r, int g) {
+      Item it = {a.n, 0, 0, 0, 0, 0};
+      for (; r < a.n; ++r, g = 0) {
+        const int pos = rfl(plan.b_pos[r]), T = rfl(units_b(r));
+        if (pos >= x1) break;
+        if (rfl(plan.b_pos[r + 1]) <= x0 || T == 0) continue;
+        for (; g < a.Hkv; ++g) {
+          const int s = pos + g * (T + SHARED_B_EXTRA), u0 = units_before(x0, s, T), u1 = units_before(x1, s, T);
+          if (u0 < u1) {
+            it = Item{r, g, u0 << shift_b, min(u1 << shift_b, rfl(pairs_b(r))), rfl(plan.own[r]) & ~SHARES, rfl(plan.base[r])};
+            return it;
           }
+          if (s >= x1) return it;
         }
-        float m = LOWEST_REF, l = 0.f;
-        float4v O[DT];
+      }
+      return it;
+    };
+    const int first = rfl(last_at_most(plan.b_pos, a.n, x0));
+    const int first_pos = rfl(plan.b_pos[first]), first_T = rfl(units_b(first));
+    Item cur = item_from(first, first_T ? rfl(small_quotient(x0 - first_pos, first_T + SHARED_B_EXTRA)) : 0);
+    if (cur.r >= a.n) return;
+    auto load_q = [&](bf16x8 (&q)[NS], const Item& it) {
+      const unsigned short* qp = a.q + ((int64_t)it.r * a.Hq + it.g * G + min(col16, G - 1)) * D + 8 * g4;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) O[dt] = float4v{0.f, 0.f, 0.f, 0.f};
-        uint4v kr[2][LOADS], vr[2][LOADS];
-        auto at_of = [&](int t, int b) {
-          const int tile = min(t + b, i1 - 1);
-          return plane + (PAGED ? (int64_t)bt_row[tile] : base_block + tile) * TILE_BYTES;
-        };
-        auto load = [&](uint4v (&to)[2][LOADS], const char* pool, int t) {
+      for (int st = 0; st < NS; ++st) {
+        const bf16x8 z = {0, 0, 0, 0, 0, 0, 0, 0};
+        q[st] = col16 < G ? *(const bf16x8*)(qp + 32 * st) : z;
+      }
+    };
+    // the tiles of pair pr (the first one again where there is no second)
+    auto blocks_of = [&](int64_t (&at)[2], const Item& it, int pr) {
+      const int tiles = tiles_of(it.own);
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const char* src = pool + at_of(t, b) + lane16;
+      for (int b = 0; b < 2; ++b) {
+        const int t = min(2 * pr + b, tiles - 1);
+        at[b] = (int64_t)it.g * a.head_stride + (PAGED ? (int64_t)as_constant(a.bt + (int64_t)it.r * a.bt_stride)[it.base + t] : (int64_t)it.base + t) * TILE_BYTES;
+      }
+    };
+    uint4v kr[2][LOADS], vr[2][LOADS];
+    auto load = [&](uint4v (&to)[2][LOADS], const char* pool, const int64_t (&at)[2]) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) to[b][i] = __builtin_nontemporal_load((const uint4v*)(src + i * 1024));
-          }
-        };
-        const int first = i0 + 2 * wv;
-        if (first < i1) {
-          load(kr, a.k, first);
-          load(vr, a.v, first);
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) to[b][i] = __builtin_nontemporal_load((const uint4v*)(pool + at[b] + lane16 + i * 1024));
+    };
+    bf16x8 qreg[NS], qnext[NS];
+    int64_t at[2];
+    load_q(qnext, cur);
+    blocks_of(at, cur, cur.i0);
+    load(kr, a.k, at);
+    load(vr, a.v, at);
+    while (cur.r < a.n) {
+      const Item next = cur.g + 1 < a.Hkv ? item_from(cur.r, cur.g + 1) : item_from(cur.r + 1, 0);
+#pragma unroll
+      for (int st = 0; st < NS; ++st) qreg[st] = qnext[st];
+      if (next.r < a.n) load_q(qnext, next);
+      float m = LOWEST_REF, l = 0.f;
+      float4v O[DT];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) O[dt] = float4v{0.f, 0.f, 0.f, 0.f};
+      for (int pr = cur.i0; pr < cur.i1; ++pr) {
+        // the loads of the pair behind this one, of this item or the next, go out as soon as their registers are free
+        const bool inside = pr + 1 < cur.i1, more = inside || next.r < a.n;
+        if (inside) blocks_of(at, cur, pr + 1);
+        else if (more) blocks_of(at, next, next.i0);
+        float4v x[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          float4v s4 = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int sp = 0; sp < NS; ++sp)
+            s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, piece(kr[b], sp)), qreg[sp], s4, 0, 0, 0);
+          x[b] = s4;
         }
-        for (int t = first; t < i1; t += 8) {
-          const bool more = t + 8 < i1;
-          float4v x[2];
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            float4v s4 = float4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int sp = 0; sp < NS; ++sp)
-              s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, piece(kr[b], sp)), qreg[sp], s4, 0, 0, 0);
-            x[b] = s4;
-          }
-          if (more) load(kr, a.k, t + 8);
-          // tokens behind the request's last one, and a second tile of another piece or of nobody
-          const int held = min(own, i1 * BLK);
-          if ((t + 2) * BLK > held) {
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if ((t + b) * BLK + 4 * g4 + i >= held) x[b][i] = -INFINITY;
-          }
-          float top = largest(x) * a.scale_log2;
-          if (__builtin_amdgcn_ballot_w64(top > m + SLACK) != 0) {
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float m_new = fmaxf(m, top), f = joined(m, m_new);
-            m = m_new;
-            l *= f;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) O[dt] *= f;
-          }
-          bf16x8 ph, pl;
-          float sum = 0.f;
+        if (more) load(kr, a.k, at);
+        const int t0 = 2 * pr * BLK;
+        const bool ragged = t0 + 2 * BLK > cur.own;           // some tokens of the pair are not there
+        if (ragged) {
 #pragma unroll
           for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][i], a.scale_log2, -m));
-              sum += pv;
-              __bf16 hi, lo;
-              two_parts(pv, hi, lo);
-              ph[4 * b + i] = hi;
-              pl[4 * b + i] = lo;
-            }
-          l += sum;
-          bf16x8 av[DT];
-#pragma unroll
-          for (int sp = 0; sp < NS; ++sp) {
-            const uint4v w0 = piece(vr[0], sp), w1 = piece(vr[1], sp);
-            av[2 * sp] = join(uint2v{w0[0], w0[1]}, uint2v{w1[0], w1[1]});
-            av[2 * sp + 1] = join(uint2v{w0[2], w0[3]}, uint2v{w1[2], w1[3]});
-          }
-          if ((t + 2) * BLK > held) {                        // stale V may be a NaN pattern, which a weight of 0 does not remove
-            uint4v keep;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const int tok = (t + (w >> 1)) * BLK + 4 * g4 + 2 * (w & 1);
-              keep[w] = (tok < held ? 0x0000ffffu : 0u) | (tok + 1 < held ? 0xffff0000u : 0u);
-            }
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) av[dt] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(uint4v, av[dt]) & keep);
-          }
-          if (more) load(vr, a.v, t + 8);
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], ph, O[dt], 0, 0, 0);
-            O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], pl, O[dt], 0, 0, 0);
-          }
+            for (int i = 0; i < 4; ++i)
+              if (t0 + b * BLK + 4 * g4 + i >= cur.own) x[b][i] = -INFINITY;
         }
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        // the four waves' states -> one
-        __syncthreads();                                     // the stages (line A), or the states of the piece before, are done with
-        float* st = (float*)stage_mem;
-        if (g4 == 0) wave_ml[wv][col16] = make_float2(m, l);
+        float top = largest(x) * a.scale_log2;
+        if (__builtin_amdgcn_ballot_w64(top > m + SLACK) != 0) {
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float m_new = fmaxf(m, top), f = joined(m, m_new);
+          m = m_new;
+          l *= f;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) *(float4v*)(st + (wv * 16 + col16) * D + 16 * dt + 4 * g4) = O[dt];
-        __syncthreads();
-        const int64_t c = cut >= 0 ? shared_cut_b(a, cut) : shared_first(a, 1, r, g * G);
-        for (int e = tid; e < G * D; e += SHARED_THREADS) {
-          const int h = e / D, ch = e % D;
-          float mm = LOWEST_REF, ll = 0.f, oo = 0.f;
+          for (int dt = 0; dt < DT; ++dt) O[dt] *= f;
+        }
+        bf16x8 ph, pl;
+        float sum = 0.f;
 #pragma unroll
-          for (int w = 0; w < 4; ++w) mm = fmaxf(mm, wave_ml[w][h].x);
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const float2 ml = wave_ml[w][h];
-            const float f = joined(ml.x, mm);
-            ll += ml.y * f;
-            oo += st[(w * 16 + h) * D + ch] * f;
+          for (int i = 0; i < 4; ++i) {
+            const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][i], a.scale_log2, -m));
+            sum += pv;
+            __bf16 hi, lo;
+            two_parts(pv, hi, lo);
+            ph[4 * b + i] = hi;
+            pl[4 * b + i] = lo;
           }
-          a.part_o[(c + h) * 128 + ch] = oo;
-          if (ch == 0) a.part_ml[c + h] = make_float2(mm, ll);
+        l += sum;
+        bf16x8 av[DT];
+#pragma unroll
+        for (int sp = 0; sp < NS; ++sp) {
+          const uint4v w0 = piece(vr[0], sp), w1 = piece(vr[1], sp);
+          av[2 * sp] = join(uint2v{w0[0], w0[1]}, uint2v{w1[0], w1[1]});
+          av[2 * sp + 1] = join(uint2v{w0[2], w0[3]}, uint2v{w1[2], w1[3]});
+        }
+        if (ragged) {                                          // stale V may be a NaN pattern, which a weight of 0 does not remove
+          uint4v keep;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int tok = t0 + (i >> 1) * BLK + 4 * g4 + 2 * (i & 1);
+            keep[i] = (tok < cur.own ? 0x0000ffffu : 0u) | (tok + 1 < cur.own ? 0xffff0000u : 0u);
+          }
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) av[dt] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(uint4v, av[dt]) & keep);
+        }
+        if (more) load(vr, a.v, at);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], ph, O[dt], 0, 0, 0);
+          O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], pl, O[dt], 0, 0, 0);
         }
       }
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      if (col16 < G) {
+        const int64_t c = (cur.i0 ? shared_cut_b(a, w) : shared_first(a, 1, cur.r, cur.g * G)) + col16;
+        if (g4 == 0) a.part_ml[c] = make_float2(m, l);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) *(float4v*)(a.part_o + c * 128 + 16 * dt + 4 * g4) = O[dt];
+      }
+      cur = next;
     }
   };
 
@@ -706,17 +754,23 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
   const bool lane_has = 2 * lane < D;
   const float* base = a.part_o + (lane_has ? 2 * lane : 0);
   const int h = hq - g * a.G, col = rec.a_col + h, cb = col / SHARED_COLS;
-  const int n = rec.a_chunks + rec.b_chunks;
+  // line B: the waves from the one that holds its first unit to the one that holds its last
+  const SharedLine line(rec.b_total, max(rec.b_used, 1));
+  const int s = rec.b_pos + g * (rec.b_units + SHARED_B_EXTRA), w0 = rec.b_units ? line.holder(s) : 0;
+  const int n_b = rec.b_units ? line.holder(s + (rec.b_units > 1 ? SHARED_B_EXTRA + rec.b_units - 1 : 0)) - w0 + 1 : 0;
+  const int n = rfl(rec.a_chunks + n_b);
   float m = LOWEST_REF, l = 0.f;
   float2 o = {0.f, 0.f};
   for (int i0 = 0; i0 < n; i0 += 64) {
     // lane i: piece i0 + i, line A's first
     const int i = i0 + lane, here = min(64, n - i0);
-    const bool on_a = i < rec.a_chunks, has = i < n;
-    const int j = on_a ? i : i - rec.a_chunks;               // chunk
+    const bool on_a = i < rec.a_chunks;
+    const int j = on_a ? i : i - rec.a_chunks, w = w0 + j;    // chunk; or wave, by its distance from the first
     const int64_t c = j == 0 ? shared_first(a, on_a ? 0 : 1, r, hq)
                       : on_a ? shared_cut_a(a, rec.a_extra + (g * (rec.a_chunks - 1) + j - 1) * rec.a_blocks + cb) + col - cb * SHARED_COLS
-                             : shared_cut_b(a, rec.b_extra + g * (rec.b_chunks - 1) + j - 1) + h;
+                             : shared_cut_b(a, w) + h;
+    // (a share shorter than an item's start may hold none of its units)
+    const bool has = i < n && (on_a || j == 0 || units_before(line.start(w), s, rec.b_units) < units_before(line.start(w + 1), s, rec.b_units));
     const int c_lo = has ? (int)c : 0;                       // (columns of the workspace fit 32 bits)
     const float2 ml = has ? a.part_ml[c] : make_float2(LOWEST_REF, 0.f);
     constexpr int ROUND = 16;

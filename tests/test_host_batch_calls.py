@@ -123,10 +123,10 @@ def test_shared(runtime):  # noqa: F811
         shared(p)
         assert launched(lambda: decode(p, 4, B.REUSE_PLAN)) == reusing
         # two work-groups for every compute unit, fewer where the workspace has little room: 8192 columns per query head hold two
-        # for each request and head, up to 144 for each work-group and a record of each request
+        # for each request and head, for each work-group up to 128 and a group of heads for each of its waves, and a record of each request
         for n, hq, hkv in ((1024, 28, 4), (1024, 8, 2), (1024, 1, 1), (3, 2, 1), (4, 16, 1)):
             grid = launched(lambda: shared(make_pool(hq=hq, hkv=hkv), n=n))[0][1]
-            used = 2 * n * hq + grid[0] * (min(128, (n * hq // hkv + 15) // 16 * 16) + 16)
+            used = 2 * n * hq + grid[0] * (min(128, (n * hq // hkv + 15) // 16 * 16) + 4 * hq // hkv)
             assert grid[0] % 8 == 0 and 8 <= grid[0] <= 512 and grid[1:] == (1, 1) and used + n // 8 <= 8192 * hq, (n, hq, grid)
         for kv, d in ((B.BF16, 64), (B.FP8, 128)):
             shared(make_pool(kv_dtype=kv, head_dim=d))
