@@ -62,10 +62,11 @@ int odma_decode_attention_shared(odma_pool_t* pool, int32_t layer, int32_t n, co
   // behind them.  First pieces take 2 columns per request and head; for each work-group there are the columns of a cut piece of line A and
   // of a group of heads for each of its waves: as many work-groups as that leaves room for, two per compute unit at most.
   const int64_t columns = (int64_t)2 * odma_plan::STREAM_MAX_WG * a.Hq;
-  const int64_t rec_columns = ((int64_t)n * sizeof(SharedRecord) + 511) / 512;
+  const int64_t rec_columns = ((int64_t)n * sizeof(SharedRecord) + sizeof(SharedShares) + 511) / 512;
   a.part_ml = (float2*)(ws + pool->ws.part_ml);
   a.part_o = (float*)(ws + pool->ws.part_o);
   a.rec = (SharedRecord*)(a.part_o + (columns - rec_columns) * 128);
+  a.shares = (SharedShares*)(a.rec + n);
   a.cut_cols = (int32_t)std::min<int64_t>(SHARED_COLS, ((int64_t)n * a.G + 15) / 16 * 16);
   const int64_t room = (columns - rec_columns - (int64_t)2 * n * a.Hq) / (a.cut_cols + SHARED_WAVES * a.G);
   a.workers = (int32_t)std::min<int64_t>(2 * (int64_t)pool->n_cu, room) / 8 * 8;

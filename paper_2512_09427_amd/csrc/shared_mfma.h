@@ -8,11 +8,15 @@
 //
 // Two lines of work.  Line A: items (prefix, KV head, block of SHARED_COLS columns), cut into chunks of pairs of 16-token tiles, a
 // work-group's piece each.  Line B: items (request, KV head), each the pairs of tiles of the request's own tokens; the line is cut
-// into equal shares, one for every wave, which streams its share across the items in it, straight into registers.  Every
-// work-group gets a like share of both lines, so that line A's matrix instructions run beside line B's memory traffic on
-// every compute unit without a number that weighs one against the other: half of the work-groups begin with A, half with B.
-// Each piece of an item leaves its state in the workspace and shared_merge_kernel joins them.  Line A is ordered (prefix, KV
-// head, chunk, column block): the work-groups of an XCD read the same few chunks at a time, out of its L2.
+// into shares, one for a wave, which streams it across the items in it, straight into registers.  Each piece of an item leaves
+// its state in the workspace and shared_merge_kernel joins them.
+//
+// Both lines run at once, line A's matrix instructions beside line B's memory traffic: some work-groups take line A, the others line
+// B.  Line B needs no more of them than fill the memory's rate (about 220 of 512), line A is as fast as it has work-groups; SHARED_TIMES
+// says how long either takes and the plan divides them so that both end together.  The states of line A are as large as its
+// columns (64 KiB a piece), so few long pieces are better than many short ones: with a piece for every work-group, 64 requests
+// behind 4096 tokens wrote and read 25 MB of states beside 105 MB of K and V.  Line A is ordered (prefix, KV head, chunk, column
+// block): the work-groups of an XCD read the same few chunks at a time, out of its L2.
 #pragma once
 
 #include <type_traits>
@@ -31,6 +35,12 @@ constexpr int SHARED_A_EXTRA = 5;         // start and end of a piece of line A,
 constexpr int SHARED_A_LEAST = 8;         // pairs below which an item of line A is not cut
 constexpr int SHARED_B_EXTRA = 2;         // start and end of an item of line B, in units
 constexpr int SHARED_B_LEAST = 2;         // units that a wave is given at least, beside an item's start and end
+// Microseconds: of a pair of line A for its work-group; of a pair of line B for its work-group while the memory has room (its
+// bytes in flight over the latency), and for the whole chip at the memory's rate (16 KiB at 5.4 TB/s; 8 in the other formats).
+struct SharedTimes {
+  float a, b, b_least;
+};
+constexpr SharedTimes SHARED_TIMES[3] = {{1.05f, 0.65f, 0.003f}, {1.05f, 0.45f, 0.0015f}, {0.6f, 0.45f, 0.0015f}};
 constexpr int SHARED_MAX_N = ODMA_SHARED_MAX_REQUESTS;
 constexpr int SHARED_THREADS = 256, SHARED_WAVES = SHARED_THREADS / 64;
 
@@ -38,7 +48,10 @@ struct SharedRecord {                     // of a request, for the merge
   int32_t a_chunks, a_blocks, a_col;      // line A: chunks (0: it shares nothing) and column blocks of an item, its first column
   int32_t a_extra;                        // cut pieces (chunks behind the first) in front of its group's
   int32_t b_pos, b_units;                 // line B: place of its first head's item, units of an item
-  int32_t b_total, b_used;                // of the line: units and waves
+  int32_t pad0, pad1;
+};
+struct SharedShares {                     // how line B is dealt out (SharedLine): units, and waves of an XCD
+  int32_t total, of_xcd;
 };
 
 struct SharedArgs {
@@ -55,6 +68,7 @@ struct SharedArgs {
   int32_t workers;                        // work-groups of the launch, a multiple of 8
   int32_t cut_cols;                       // columns kept for a cut piece of line A
   SharedRecord* rec;                      // [n]
+  SharedShares* shares;
   float2* part_ml;                        // states of columns: reference and sum
   float* part_o;                          // [column][128]
 };
@@ -100,16 +114,22 @@ __device__ __forceinline__ int pieces_before(int x, int s, int c, int N) {
   return x <= s ? 0 : x >= s + c ? N : min((int)ceilf((float)(x - s) * (float)N / (float)c), N);   // (monotone in x)
 }
 
-// Line B: wave w's share is [start(w), start(w + 1)), a unit at least.  An item at s with T units has unit 0 at s and unit i at
-// s + SHARED_B_EXTRA + i, and a unit belongs to the share that holds its position.
+// Line B: wave w's share is [start(w), start(w + 1)).  An item at s with T units has unit 0 at s and unit i at s + SHARED_B_EXTRA + i, and
+// a unit belongs to the share that holds its position.
 struct SharedLine {
-  int total, used;
+  int total, waves;
+  float inv;
   double step;
-  __device__ __forceinline__ SharedLine(int total_, int used_) : total(total_), used(used_), step((double)total_ / (double)used_) {}
-  __device__ __forceinline__ int start(int w) const { return w >= used ? total : (int)((double)w * step); }
+  __device__ __forceinline__ SharedLine(const SharedShares& s) : total(s.total), waves(8 * s.of_xcd) {
+    step = (double)total / (double)waves;
+    inv = (float)waves * __builtin_amdgcn_rcpf((float)total);
+  }
+  __device__ __forceinline__ int start(int w) const { return w >= waves ? total : (int)((double)w * step); }
   __device__ __forceinline__ int holder(int pos) const {
-    const int w = min((int)((float)pos * (float)used * __builtin_amdgcn_rcpf((float)total)), used - 1);
-    return start(w) > pos ? w - 1 : start(w + 1) <= pos ? w + 1 : w;   // (the quotient, below 2^14, is within one)
+    int w = min((int)((float)pos * inv), waves - 1);
+    while (start(w) > pos) --w;                              // (the estimate is within a few)
+    while (start(w + 1) <= pos) ++w;
+    return w;
   }
 };
 __device__ __forceinline__ int units_before(int x, int s, int T) {
@@ -170,6 +190,21 @@ __device__ __forceinline__ T lanes_sum(T x) {
   return x;
 }
 
+// the largest over the lanes of a wave
+__device__ __forceinline__ float lanes_max(float x) {
+  auto moved = [](float v, auto ctrl, auto rows) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+  };
+  using std::integral_constant;
+  x = fmaxf(x, moved(x, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{}));
+  x = fmaxf(x, moved(x, integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{}));
+  x = fmaxf(x, moved(x, integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{}));
+  x = fmaxf(x, moved(x, integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{}));
+  x = fmaxf(x, moved(x, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{}));
+  x = fmaxf(x, moved(x, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{}));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
 // Last entry of pos[0 .. n) (which does not decrease, and begins with 0) that is at most x >= 0; n <= 4096.
 __device__ __forceinline__ int last_at_most(const int32_t* pos, int n, int x) {
   const int lane = threadIdx.x & 63;
@@ -195,6 +230,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
   constexpr int TILE_BYTES = BLK * D * (FP8 ? 1 : 2), LOADS = TILE_BYTES / 1024;
   constexpr int K_STAGE = 2 * NS * 1024, STAGE_BYTES = 2 * K_STAGE;
   constexpr int CT = SHARED_CT;
+  constexpr int V_AHEAD = D == 64 ? DT : LO ? 2 : 5;        // V operands that there are registers for in front of their weights
   constexpr float SLACK = 8.0f;                             // exponent units by which a score may exceed the reference
   __shared__ __attribute__((aligned(16))) char stage_mem[2 * STAGE_BYTES];
   __shared__ SharedPlan plan;
@@ -257,9 +293,15 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
     for (int i = 0; i < 2; ++i) units[i] += plan.units[w][i];
     items += plan.items[w];
   }
-  const SharedCut cut_a(units[0] * (float)a.Hkv, items * a.Hkv, a.workers, SHARED_A_LEAST);
+  units[0] *= (float)a.Hkv;
+  units[1] *= (float)a.Hkv;
+  // work-groups for line A: as many as end with line B
+  const SharedTimes times = SHARED_TIMES[FMT];
+  const float time_a = (units[0] + (float)(items * a.Hkv * SHARED_A_EXTRA)) * times.a, time = fmaxf((time_a + units[1] * times.b) * __builtin_amdgcn_rcpf((float)a.workers), units[1] * times.b_least);
+  const int for_a = rfl(min(max((int)(time_a * __builtin_amdgcn_rcpf(fmaxf(time, 1e-3f)) + 4.f) / 8 * 8, 8), a.workers));
+  const SharedCut cut_a(units[0], items * a.Hkv, for_a, SHARED_A_LEAST);
   // A unit of line B: 2^shift_b pairs, so that the line fits 30 bits (it always does unless tables name the same blocks over and over).
-  const int shift_b = rfl(max((int)(__float_as_uint(units[1] * (float)a.Hkv) >> 23) - 127 - 28, 0));
+  const int shift_b = rfl(max((int)(__float_as_uint(units[1]) >> 23) - 127 - 28, 0));
   auto pairs_b = [&](int r) { return (tiles_of(plan.own[r] & ~SHARES) + 1) / 2; };
   auto units_b = [&](int r) { return (pairs_b(r) + (1 << shift_b) - 1) >> shift_b; };
   int sum[3] = {0, 0, 0};
@@ -316,18 +358,18 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
     plan.b_pos[a.n] = total[2];
   }
   __syncthreads();
-  // Shares.  XCD x (work-groups x, x + 8, ..) has neighbouring ones, which read the same heads.  A short line goes to few work-groups, the
-  // first ones of every XCD (A) or the last (B).
-  const int pieces_a = total[1] + items * a.Hkv, least_b = SHARED_WAVES * (SHARED_B_LEAST + SHARED_B_EXTRA);
-  const int used_a = rfl(total[0] ? min((min(pieces_a, a.workers) + 7) / 8 * 8, a.workers) : 0);
-  const int used_b = rfl(total[2] ? min((total[2] / least_b / 8 + 1) * 8, a.workers) : 0);
+  // Shares.  XCD x (work-groups x, x + 8, ..) has neighbouring ones, which read the same heads.  Line A goes to the first work-groups of
+  // every XCD, line B to the last, as many as have work.
   const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, turns = a.workers >> 3;
-  const int waves_b = min(used_b * SHARED_WAVES, total[2]);    // (a share is a unit at least)
-  const int ja = used_a >> 3, jb = used_b >> 3;
-  const int share_a = turn < ja ? xcd * ja + turn : -1, share_b = turns - 1 - turn < jb ? xcd * jb + turns - 1 - turn : -1;
+  const int used_a = rfl(total[0] ? min((min(total[1] + items * a.Hkv, for_a) + 7) / 8 * 8, for_a) : 0), ja = used_a >> 3;
+  const int jb = rfl(total[2] ? min(total[2] / (8 * SHARED_WAVES * (SHARED_B_LEAST + SHARED_B_EXTRA)) + 1, turns) : 0);
+  // Line B leaves the work-groups of line A alone, unless they are all there are.
+  const SharedShares shares = {total[2], SHARED_WAVES * min(jb, ja < turns ? turns - ja : turns)};
+  const int share_a = turn < ja ? xcd * ja + turn : -1;
+  const int in_xcd_b = SHARED_WAVES * (turns - 1 - turn) + wv;   // line B: the wave's number on its XCD
   if (blockIdx.x == gridDim.x - 1) {                        // for the merge
     for (int r = tid; r < a.n; r += SHARED_THREADS) {
-      SharedRecord rec = {0, 0, 0, 0, plan.b_pos[r], units_b(r), total[2], waves_b};
+      SharedRecord rec = {0, 0, 0, 0, plan.b_pos[r], units_b(r), 0, 0};
       if (plan.own[r] & SHARES) {
         const int p = prefix_of(plan.start, a.n_prefixes, r);
         rec.a_chunks = cut_a.chunks((plan.tiles[p] + 1) / 2);
@@ -337,6 +379,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
       }
       a.rec[r] = rec;
     }
+    if (tid == 0) *a.shares = shares;
   }
 
   auto piece = [&](const uint4v (&w)[LOADS], int s) {       // 16-byte operand s (of NS) of a tile, as bf16
@@ -442,21 +485,19 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
             }
           }
         };
-        auto scores = [&](float4v (&x)[CT][2], int j) {       // of pair i0 + j, less the references
+        auto read_k = [&](bf16x8 (&kk)[NS], int j, int b) {   // tile b of pair i0 + j
           const char* st = stage_mem + (j & 1) * STAGE_BYTES + lane16;
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            bf16x8 kk[NS];
+          for (int sp = 0; sp < NS; ++sp) kk[sp] = *(const bf16x8*)(st + b * NS * 1024 + sp * 1024);
+        };
+        auto scores = [&](float4v (&x)[CT][2], const bf16x8 (&kk)[NS], int b) {   // less the references
 #pragma unroll
-            for (int sp = 0; sp < NS; ++sp) kk[sp] = *(const bf16x8*)(st + b * NS * 1024 + sp * 1024);
+          for (int ct = 0; ct < CT; ++ct) {
+            const float mm = minus_m[ct];
+            float4v s4 = float4v{mm, mm, mm, mm};
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-              const float mm = minus_m[ct];
-              float4v s4 = float4v{mm, mm, mm, mm};
-#pragma unroll
-              for (int sp = 0; sp < NS; ++sp) s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[sp], qreg[ct][sp], s4, 0, 0, 0);
-              x[ct][b] = s4;
-            }
+            for (int sp = 0; sp < NS; ++sp) s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[sp], qreg[ct][sp], s4, 0, 0, 0);
+            x[ct][b] = s4;
           }
         };
         int fresh = 1;                                        // some column of the wave has no reference
@@ -501,8 +542,17 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
         // wave's halves overlap by themselves: with scores, weights and P V one after the other a SIMD's two waves needed
         // 2667 cycles for a pair each.
         auto compute = [&](float4v (&x)[CT][2], float4v (&ahead)[CT][2], int pr) {
+          // LDS first: K of the pair behind this one and V of this one are on their way while the references are looked at
+          bf16x8 k0[NS], k1[NS], av[DT];
+          const char* st = stage_mem + ((pr - i0) & 1) * STAGE_BYTES + K_STAGE + lane16;
+          read_k(k0, pr + 1 - i0, 0);
+#pragma unroll
+          for (int dt = 0; dt < V_AHEAD; ++dt) av[dt] = *(const bf16x8*)(st + dt * 1024);
+          __builtin_amdgcn_sched_barrier(0);
           settle(x, pr);
-          scores(ahead, pr + 1 - i0);
+          read_k(k1, pr + 1 - i0, 1);
+          scores(ahead, k0, 0);
+          scores(ahead, k1, 1);
           bf16x8 ph[CT], pl[CT];
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct)
@@ -520,21 +570,20 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
                   ph[ct][4 * b + i] = (__bf16)pv;
                 }
               }
-          const char* st = stage_mem + ((pr - i0) & 1) * STAGE_BYTES + K_STAGE + lane16;
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
             l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, ph[ct], l[ct], 0, 0, 0);
             if (LO) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pl[ct], l[ct], 0, 0, 0);
           }
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            const bf16x8 av = *(const bf16x8*)(st + dt * 1024);
+          for (int dt = V_AHEAD; dt < DT; ++dt) av[dt] = *(const bf16x8*)(st + dt * 1024);
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-              O[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, ph[ct], O[ct][dt], 0, 0, 0);
-              if (LO) O[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, pl[ct], O[ct][dt], 0, 0, 0);
+              O[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], ph[ct], O[ct][dt], 0, 0, 0);
+              if (LO) O[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], pl[ct], O[ct][dt], 0, 0, 0);
             }
-          }
         };
         // pipeline: load j + 3 is under way while pair j is computed; load j + 2 goes from registers into its stage behind it, where
         // pair j + 1 finds it, and one barrier per pair makes it visible
@@ -550,7 +599,14 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
         issue(ra, 2);
         lookup(3);
         __syncthreads();
-        if (active) scores(xa, 0);
+        if (active) {
+          bf16x8 kk[NS];
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            read_k(kk, 0, b);
+            scores(xa, kk, b);
+          }
+        }
         write_stage(rb, 1);
         __syncthreads();
         auto step = [&](uint4v (&near)[LOADS], uint4v (&far)[LOADS], float4v (&x)[CT][2], float4v (&ahead)[CT][2], int pr) {
@@ -580,9 +636,9 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
 
   // ================= line B: every wave streams its share
   auto line_b = [&]() {
-    const SharedLine line(total[2], waves_b);
-    const int w = share_b * SHARED_WAVES + wv;
-    if (w >= waves_b) return;
+    const SharedLine line(shares);
+    if (in_xcd_b >= shares.of_xcd) return;
+    const int w = xcd * shares.of_xcd + in_xcd_b;
     const int x0 = rfl(line.start(w)), x1 = rfl(line.start(w + 1));
     struct Item {
       int r, g, i0, i1;                                     // pairs [i0, i1) of the request's own tokens
@@ -733,32 +789,30 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
     }
   };
 
-  if (turn * 2 < turns) {
-    if (share_a >= 0) line_a();
-    if (share_b >= 0) line_b();
-  } else {
-    if (share_b >= 0) line_b();
-    if (share_a >= 0) line_a();
-  }
+  if (share_a >= 0) line_a();
+  line_b();
 }
 
 // Joins the pieces of a request's two parts: a wave per (request, query head), two channels a lane.  Lane i looks up piece i (64 a
-// round); the outputs of the first 16 are requested beside all references and sums, in one round trip.
+// round); the outputs of the first SHARED_ROUND are requested beside all references and sums, in one round trip.  Bound by its chain of
+// round trips (record, states) and by the states' bytes, not by its arithmetic.
+constexpr int SHARED_ROUND = 16;
 template <int D>
 __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
   const int lane = threadIdx.x & 63;
   const int id = rfl(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (id >= a.n * a.Hq) return;
-  const int r = id / a.Hq, hq = id - r * a.Hq, g = hq / a.G;
+  const int r = rfl(small_quotient(id, a.Hq)), hq = id - r * a.Hq, g = rfl(small_quotient(hq, a.G)), h = hq - g * a.G;
   const SharedRecord rec = a.rec[r];
-  const bool lane_has = 2 * lane < D;
-  const float* base = a.part_o + (lane_has ? 2 * lane : 0);
-  const int h = hq - g * a.G, col = rec.a_col + h, cb = col / SHARED_COLS;
+  const SharedLine line(*a.shares);
+  const int col = rec.a_col + h, cb = col / SHARED_COLS;
   // line B: the waves from the one that holds its first unit to the one that holds its last
-  const SharedLine line(rec.b_total, max(rec.b_used, 1));
-  const int s = rec.b_pos + g * (rec.b_units + SHARED_B_EXTRA), w0 = rec.b_units ? line.holder(s) : 0;
-  const int n_b = rec.b_units ? line.holder(s + (rec.b_units > 1 ? SHARED_B_EXTRA + rec.b_units - 1 : 0)) - w0 + 1 : 0;
+  const int s = rec.b_pos + g * (rec.b_units + SHARED_B_EXTRA), w0 = rec.b_units ? rfl(line.holder(s)) : 0;
+  const int n_b = rec.b_units ? rfl(line.holder(s + (rec.b_units > 1 ? SHARED_B_EXTRA + rec.b_units - 1 : 0))) - w0 + 1 : 0;
   const int n = rfl(rec.a_chunks + n_b);
+  const int a_stride = rec.a_blocks * a.cut_cols, a_cut = (int)shared_cut_a(a, rec.a_extra + g * (rec.a_chunks - 1) * rec.a_blocks + cb) + col - cb * SHARED_COLS;
+  const bool lane_has = 2 * lane < D;
+  const unsigned lane_at = lane_has ? lane * 8u : 0u;        // (columns of the workspace fit 23 bits, their bytes 32)
   float m = LOWEST_REF, l = 0.f;
   float2 o = {0.f, 0.f};
   for (int i0 = 0; i0 < n; i0 += 64) {
@@ -766,36 +820,35 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
     const int i = i0 + lane, here = min(64, n - i0);
     const bool on_a = i < rec.a_chunks;
     const int j = on_a ? i : i - rec.a_chunks, w = w0 + j;    // chunk; or wave, by its distance from the first
-    const int64_t c = j == 0 ? shared_first(a, on_a ? 0 : 1, r, hq)
-                      : on_a ? shared_cut_a(a, rec.a_extra + (g * (rec.a_chunks - 1) + j - 1) * rec.a_blocks + cb) + col - cb * SHARED_COLS
-                             : shared_cut_b(a, w) + h;
+    int c = j == 0 ? (int)shared_first(a, on_a ? 0 : 1, r, hq) : on_a ? a_cut + (j - 1) * a_stride : (int)shared_cut_b(a, w) + h;
     // (a share shorter than an item's start may hold none of its units)
     const bool has = i < n && (on_a || j == 0 || units_before(line.start(w), s, rec.b_units) < units_before(line.start(w + 1), s, rec.b_units));
-    const int c_lo = has ? (int)c : 0;                       // (columns of the workspace fit 32 bits)
+    if (!has) c = 0;
     const float2 ml = has ? a.part_ml[c] : make_float2(LOWEST_REF, 0.f);
-    constexpr int ROUND = 16;
-    float2 x[ROUND];
+    float2 x[SHARED_ROUND];
     auto load = [&](int k0) {
 #pragma unroll
-      for (int k = 0; k < ROUND; ++k)
-        x[k] = *(const float2*)(base + (int64_t)__builtin_amdgcn_readlane(c_lo, min(k0 + k, here - 1)) * 128);
+      for (int k = 0; k < SHARED_ROUND; ++k) {
+        const unsigned at = (unsigned)__builtin_amdgcn_readlane(c, min(k0 + k, here - 1)) * 512u + lane_at;
+        x[k] = *(const float2*)((const char*)a.part_o + at);
+      }
     };
     load(0);                                                 // under way before the weights are known
-    const float m_new = fmaxf(m, wave_max(ml.x)), f = joined(m, m_new), fx = has ? joined(ml.x, m_new) : 0.f;
-    l = l * f + wave_sum(ml.y * fx);
+    const float m_new = fmaxf(m, lanes_max(ml.x)), f = joined(m, m_new), fx = has ? joined(ml.x, m_new) : 0.f;
+    l = l * f + __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lanes_sum(ml.y * fx)), 63));
     o.x *= f;
     o.y *= f;
     m = m_new;
     for (int k0 = 0;;) {
 #pragma unroll
-      for (int k = 0; k < ROUND; ++k) {
+      for (int k = 0; k < SHARED_ROUND; ++k) {
         const float w_k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fx), min(k0 + k, 63)));
         if (k0 + k < here && w_k != 0.f) {
           o.x = __builtin_fmaf(x[k].x, w_k, o.x);
           o.y = __builtin_fmaf(x[k].y, w_k, o.y);
         }
       }
-      if ((k0 += ROUND) >= here) break;
+      if ((k0 += SHARED_ROUND) >= here) break;
       load(k0);
     }
   }
