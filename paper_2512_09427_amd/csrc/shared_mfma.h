@@ -32,7 +32,11 @@ enum { SHARED_BF16_128, SHARED_FP8_128, SHARED_BF16_64 };
 constexpr int SHARED_COLS = 128;          // columns of an item of line A: four waves of two 16-column tiles
 constexpr int SHARED_CT = 2;
 constexpr int SHARED_A_EXTRA = 5;         // start and end of a piece of line A, in pairs
-constexpr int SHARED_A_LEAST = 8;         // pairs below which an item of line A is not cut
+// Pairs below which line A is not cut: at least 4, and SHARED_A_ROOT times the root of all its pairs.  A pair takes 0.7 us of a work-group that
+// has its compute unit to itself, a piece 0.025 us of the memory's time for its states (128 columns, written and read), and
+// 0.7 x + 0.025 U / x is least at 0.19 sqrt(U).  (8 at least: 8 requests behind 992 tokens 16.8 us, 14.6 with 4; 4 always: 16 behind
+// 16 384 27.1 -> 31.9.)
+constexpr float SHARED_A_LEAST = 4.f, SHARED_A_ROOT = 0.19f;
 constexpr int SHARED_B_EXTRA = 2;         // start and end of an item of line B, in units
 constexpr int SHARED_B_LEAST = 2;         // units that a wave is given at least, beside an item's start and end
 // Microseconds: of a pair of line A for its work-group; of a pair of line B for its work-group while the memory has room (its
@@ -40,7 +44,7 @@ constexpr int SHARED_B_LEAST = 2;         // units that a wave is given at least
 struct SharedTimes {
   float a, b, b_least;
 };
-constexpr SharedTimes SHARED_TIMES[3] = {{1.05f, 0.65f, 0.003f}, {1.05f, 0.45f, 0.0015f}, {0.6f, 0.45f, 0.0015f}};
+constexpr SharedTimes SHARED_TIMES[3] = {{1.3f, 0.65f, 0.003f}, {1.3f, 0.45f, 0.0015f}, {0.8f, 0.45f, 0.0015f}};
 constexpr int SHARED_MAX_N = ODMA_SHARED_MAX_REQUESTS;
 constexpr int SHARED_THREADS = 256, SHARED_WAVES = SHARED_THREADS / 64;
 
@@ -97,8 +101,9 @@ __device__ __forceinline__ int small_quotient(int a, int b) {
 struct SharedCut {
   float inv_length;
   int shift;                                                // costs count 2^shift pairs, so that the line's sum fits 30 bits
-  __device__ __forceinline__ SharedCut(float units, int items, int pieces, int least) {
-    const float length = fmaxf(units * 1.0005f * __builtin_amdgcn_rcpf((float)max(pieces - items, pieces / 2)), (float)least);   // (the sum is within 2^-13)
+  __device__ __forceinline__ SharedCut(float units, int items, int pieces) {
+    const float least = fmaxf(SHARED_A_LEAST, SHARED_A_ROOT * __builtin_amdgcn_sqrtf(units));
+    const float length = fmaxf(units * 1.0005f * __builtin_amdgcn_rcpf((float)max(pieces - items, pieces / 2)), least);   // (the sum is within 2^-13)
     inv_length = __builtin_amdgcn_rcpf(length);
     shift = max((int)(__float_as_uint(units) >> 23) - 127 - 27, 0);
   }
@@ -153,10 +158,10 @@ struct SharedPlan {
   int32_t tiles[SHARED_MAX_N];            // of the shared part
   int32_t first_block[SHARED_MAX_N];      // (contiguous)
   int32_t reader[SHARED_MAX_N];           // its first request that holds all of the shared part
-  int32_t a_pos[SHARED_MAX_N + 1];        // cost of line A in front of it
+  int32_t a_pos[SHARED_MAX_N + 1];        // cost of line A in front of it, or pieces where every work-group gets one
   int32_t a_extra[SHARED_MAX_N];          // cut pieces in front of it
   float units[SHARED_WAVES][2];
-  int32_t items[SHARED_WAVES], sums[SHARED_WAVES][3];
+  int32_t items[SHARED_WAVES], sums[SHARED_WAVES][4];
 };
 constexpr int SHARES = (int)0x80000000;
 
@@ -298,20 +303,20 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
   // work-groups for line A: as many as end with line B
   const SharedTimes times = SHARED_TIMES[FMT];
   const float time_a = (units[0] + (float)(items * a.Hkv * SHARED_A_EXTRA)) * times.a, time = fmaxf((time_a + units[1] * times.b) * __builtin_amdgcn_rcpf((float)a.workers), units[1] * times.b_least);
-  const int for_a = rfl(min(max((int)(time_a * __builtin_amdgcn_rcpf(fmaxf(time, 1e-3f)) + 4.f) / 8 * 8, 8), a.workers));
-  const SharedCut cut_a(units[0], items * a.Hkv, for_a, SHARED_A_LEAST);
+  const int for_a = rfl(min(max((int)(time_a * __builtin_amdgcn_rcpf(fmaxf(time, 1e-3f)) + 7.f) / 8 * 8, 8), a.workers));
+  const SharedCut cut_a(units[0], items * a.Hkv, for_a);
   // A unit of line B: 2^shift_b pairs, so that the line fits 30 bits (it always does unless tables name the same blocks over and over).
   const int shift_b = rfl(max((int)(__float_as_uint(units[1]) >> 23) - 127 - 28, 0));
   auto pairs_b = [&](int r) { return (tiles_of(plan.own[r] & ~SHARES) + 1) / 2; };
   auto units_b = [&](int r) { return (pairs_b(r) + (1 << shift_b) - 1) >> shift_b; };
-  int sum[3] = {0, 0, 0};
+  int sum[4] = {0, 0, 0, 0};
   struct Entry {
-    int cost, extra;
+    int cost, extra, pieces;
   };
   auto group_entry = [&](int p) {
     const int blocks = group_blocks(p), pairs = (plan.tiles[p] + 1) / 2, chunks = cut_a.chunks(pairs);
-    if (!blocks) return Entry{0, 0};
-    return Entry{(int)((int64_t)a.Hkv * blocks * (pairs + chunks * SHARED_A_EXTRA) >> cut_a.shift) + 1, a.Hkv * blocks * (chunks - 1)};
+    if (!blocks) return Entry{0, 0, 0};
+    return Entry{(int)((int64_t)a.Hkv * blocks * (pairs + chunks * SHARED_A_EXTRA) >> cut_a.shift) + 1, a.Hkv * blocks * (chunks - 1), a.Hkv * blocks * chunks};
   };
   auto request_cost = [&](int r) {
     const int T = units_b(r);
@@ -321,17 +326,18 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
     const Entry e = group_entry(p);
     sum[0] += e.cost;
     sum[1] += e.extra;
+    sum[3] += e.pieces;
   }
   for (int r = r0; r < r1; ++r) sum[2] += request_cost(r);
-  int before[3], total[3];
+  int before[4], total[4];
 #pragma unroll
-  for (int i = 0; i < 3; ++i) before[i] = lanes_sum(sum[i]);
+  for (int i = 0; i < 4; ++i) before[i] = lanes_sum(sum[i]);
   if (lane == 63)
 #pragma unroll
-    for (int i = 0; i < 3; ++i) plan.sums[wv][i] = before[i];
+    for (int i = 0; i < 4; ++i) plan.sums[wv][i] = before[i];
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < 4; ++i) {
     before[i] -= sum[i];
     total[i] = 0;
 #pragma unroll
@@ -342,30 +348,34 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
     }
     total[i] = rfl(total[i]);
   }
+  // As a rule there are no more pieces than work-groups for them: one each, whatever they cost.
+  const bool one_each = total[3] <= for_a;
+  const int total_a = one_each ? total[3] : total[0];
   for (int p = p0; p < p1; ++p) {
     const Entry e = group_entry(p);
-    plan.a_pos[p] = before[0];
+    plan.a_pos[p] = one_each ? before[3] : before[0];
     plan.a_extra[p] = before[1];
     before[0] += e.cost;
     before[1] += e.extra;
+    before[3] += e.pieces;
   }
   for (int r = r0; r < r1; ++r) {
     plan.b_pos[r] = before[2];
     before[2] += request_cost(r);
   }
   if (tid == 0) {
-    plan.a_pos[a.n_prefixes] = total[0];
+    plan.a_pos[a.n_prefixes] = total_a;
     plan.b_pos[a.n] = total[2];
   }
   __syncthreads();
   // Shares.  XCD x (work-groups x, x + 8, ..) has neighbouring ones, which read the same heads.  Line A goes to the first work-groups of
   // every XCD, line B to the last, as many as have work.
   const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3, turns = a.workers >> 3;
-  const int used_a = rfl(total[0] ? min((min(total[1] + items * a.Hkv, for_a) + 7) / 8 * 8, for_a) : 0), ja = used_a >> 3;
+  const int used_a = rfl(min(total[3], for_a)), ja = (used_a + 7) >> 3;
   const int jb = rfl(total[2] ? min(total[2] / (8 * SHARED_WAVES * (SHARED_B_LEAST + SHARED_B_EXTRA)) + 1, turns) : 0);
   // Line B leaves the work-groups of line A alone, unless they are all there are.
   const SharedShares shares = {total[2], SHARED_WAVES * min(jb, ja < turns ? turns - ja : turns)};
-  const int share_a = turn < ja ? xcd * ja + turn : -1;
+  const int share_a = turn < ja && xcd * ja + turn < used_a ? xcd * ja + turn : -1;
   const int in_xcd_b = SHARED_WAVES * (turns - 1 - turn) + wv;   // line B: the wave's number on its XCD
   if (blockIdx.x == gridDim.x - 1) {                        // for the merge
     for (int r = tid; r < a.n; r += SHARED_THREADS) {
@@ -400,8 +410,8 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
     bf16x8 ones;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
-    const double step_a = (double)total[0] / (double)used_a;
-    const int x0 = rfl((int)((double)share_a * step_a)), x1 = rfl(share_a + 1 >= used_a ? total[0] : (int)((double)(share_a + 1) * step_a));
+    const double step_a = (double)total_a / (double)used_a;
+    const int x0 = rfl((int)((double)share_a * step_a)), x1 = rfl(share_a + 1 >= used_a ? total_a : (int)((double)(share_a + 1) * step_a));
     for (int p = rfl(last_at_most(plan.a_pos, a.n_prefixes, x0)); p < a.n_prefixes; ++p) {
       const int pos = rfl(plan.a_pos[p]), cost = rfl(plan.a_pos[p + 1]) - pos, reader = rfl(plan.reader[p]);
       if (pos >= x1) break;
@@ -440,13 +450,12 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
         }
         // A column's reference m, in raw scores, enters with the accumulators of its scores (minus m instead of 0); -inf: none yet.
         // The sum of its weights is one more row of P V, with V = 1.
-        float m[CT], minus_m[CT];
-        float4v l[CT], O[CT][DT];
+        float m[CT];
+        float4v minus_m[CT], l[CT], O[CT][DT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
           m[ct] = -INFINITY;
-          minus_m[ct] = 0.f;
-          l[ct] = float4v{0.f, 0.f, 0.f, 0.f};
+          minus_m[ct] = l[ct] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) O[ct][dt] = float4v{0.f, 0.f, 0.f, 0.f};
         }
@@ -478,11 +487,13 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
             const bool absent = 2 * pair_of(j) + which >= n_tiles;
 #pragma unroll
             for (int sp = 0; sp < NS; ++sp) {
-              uint4v w = piece(rg, sp);
-              if (absent) w = uint4v{0u, 0u, 0u, 0u};
+              const uint4v w = piece(rg, sp);
               *(uint2v*)(dst + (2 * sp) * 1024) = uint2v{w[0], w[1]};
               *(uint2v*)(dst + (2 * sp + 1) * 1024) = uint2v{w[2], w[3]};
             }
+            if (__builtin_expect(absent, 0))
+#pragma unroll
+              for (int dt = 0; dt < DT; ++dt) *(uint2v*)(dst + dt * 1024) = uint2v{0u, 0u};
           }
         };
         auto read_k = [&](bf16x8 (&kk)[NS], int j, int b) {   // tile b of pair i0 + j
@@ -493,8 +504,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
         auto scores = [&](float4v (&x)[CT][2], const bf16x8 (&kk)[NS], int b) {   // less the references
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
-            const float mm = minus_m[ct];
-            float4v s4 = float4v{mm, mm, mm, mm};
+            float4v s4 = minus_m[ct];
 #pragma unroll
             for (int sp = 0; sp < NS; ++sp) s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[sp], qreg[ct][sp], s4, 0, 0, 0);
             x[ct][b] = s4;
@@ -527,7 +537,8 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
                 f = joined(0.f, up * a.scale_log2);
               }
               fresh |= __builtin_amdgcn_ballot_w64(m[ct] == -INFINITY) != 0;
-              minus_m[ct] = m[ct] == -INFINITY ? 0.f : -m[ct];
+              const float mm = m[ct] == -INFINITY ? 0.f : -m[ct];
+              minus_m[ct] = float4v{mm, mm, mm, mm};
               l[ct] *= f;
 #pragma unroll
               for (int b = 0; b < 2; ++b)
@@ -793,73 +804,91 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
   line_b();
 }
 
-// Joins the pieces of a request's two parts: a wave per (request, query head), two channels a lane.  Lane i looks up piece i (64 a
-// round); the outputs of the first SHARED_ROUND are requested beside all references and sums, in one round trip.  Bound by its chain of
-// round trips (record, states) and by the states' bytes, not by its arithmetic.
-constexpr int SHARED_ROUND = 16;
-template <int D>
+// Joins the pieces of a request's two parts: a wave per (request, HEADS query heads of a KV head), two channels a lane.  Lane i looks up
+// piece i (64 a round); the outputs of the first ROUND are requested beside all references and sums, in one round trip.  Bound
+// by its chain of round trips (record, states) and, where there are many, by the states' bytes.  A head's columns lie behind one another
+// in all pieces (a column block that is not the last is whole).
+template <int D, int HEADS>
 __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
+  constexpr int ROUND = 16 / HEADS < 4 ? 4 : 16 / HEADS;
   const int lane = threadIdx.x & 63;
-  const int id = rfl(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (id >= a.n * a.Hq) return;
-  const int r = rfl(small_quotient(id, a.Hq)), hq = id - r * a.Hq, g = rfl(small_quotient(hq, a.G)), h = hq - g * a.G;
+  const int id = rfl(blockIdx.x * 4 + (threadIdx.x >> 6)), parts = (a.G + HEADS - 1) / HEADS;   // waves of a KV head
+  const int rg = rfl(small_quotient(id, parts)), r = rfl(small_quotient(rg, a.Hkv)), g = rg - r * a.Hkv, h0 = (id - rg * parts) * HEADS;
+  if (r >= a.n) return;
   const SharedRecord rec = a.rec[r];
   const SharedLine line(*a.shares);
-  const int col = rec.a_col + h, cb = col / SHARED_COLS;
+  const int heads = min(HEADS, a.G - h0);
   // line B: the waves from the one that holds its first unit to the one that holds its last
   const int s = rec.b_pos + g * (rec.b_units + SHARED_B_EXTRA), w0 = rec.b_units ? rfl(line.holder(s)) : 0;
   const int n_b = rec.b_units ? rfl(line.holder(s + (rec.b_units > 1 ? SHARED_B_EXTRA + rec.b_units - 1 : 0))) - w0 + 1 : 0;
   const int n = rfl(rec.a_chunks + n_b);
-  const int a_stride = rec.a_blocks * a.cut_cols, a_cut = (int)shared_cut_a(a, rec.a_extra + g * (rec.a_chunks - 1) * rec.a_blocks + cb) + col - cb * SHARED_COLS;
+  const int a_stride = rec.a_blocks * a.cut_cols, a_cut = (int)shared_cut_a(a, rec.a_extra + g * (rec.a_chunks - 1) * rec.a_blocks) + rec.a_col + h0;
   const bool lane_has = 2 * lane < D;
   const unsigned lane_at = lane_has ? lane * 8u : 0u;        // (columns of the workspace fit 23 bits, their bytes 32)
-  float m = LOWEST_REF, l = 0.f;
-  float2 o = {0.f, 0.f};
+  float m[HEADS], l[HEADS];
+  float2 o[HEADS];
+#pragma unroll
+  for (int h = 0; h < HEADS; ++h) {
+    m[h] = LOWEST_REF;
+    l[h] = 0.f;
+    o[h] = make_float2(0.f, 0.f);
+  }
   for (int i0 = 0; i0 < n; i0 += 64) {
     // lane i: piece i0 + i, line A's first
     const int i = i0 + lane, here = min(64, n - i0);
     const bool on_a = i < rec.a_chunks;
     const int j = on_a ? i : i - rec.a_chunks, w = w0 + j;    // chunk; or wave, by its distance from the first
-    int c = j == 0 ? (int)shared_first(a, on_a ? 0 : 1, r, hq) : on_a ? a_cut + (j - 1) * a_stride : (int)shared_cut_b(a, w) + h;
+    int c = j == 0 ? (int)shared_first(a, on_a ? 0 : 1, r, g * a.G + h0) : on_a ? a_cut + (j - 1) * a_stride : (int)shared_cut_b(a, w) + h0;
     // (a share shorter than an item's start may hold none of its units)
     const bool has = i < n && (on_a || j == 0 || units_before(line.start(w), s, rec.b_units) < units_before(line.start(w + 1), s, rec.b_units));
     if (!has) c = 0;
-    const float2 ml = has ? a.part_ml[c] : make_float2(LOWEST_REF, 0.f);
-    float2 x[SHARED_ROUND];
+    float2 ml[HEADS], x[HEADS][ROUND];
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) ml[h] = has ? a.part_ml[c + min(h, heads - 1)] : make_float2(LOWEST_REF, 0.f);
     auto load = [&](int k0) {
 #pragma unroll
-      for (int k = 0; k < SHARED_ROUND; ++k) {
+      for (int k = 0; k < ROUND; ++k) {
         const unsigned at = (unsigned)__builtin_amdgcn_readlane(c, min(k0 + k, here - 1)) * 512u + lane_at;
-        x[k] = *(const float2*)((const char*)a.part_o + at);
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h) x[h][k] = *(const float2*)((const char*)a.part_o + at + (h < heads ? h * 512u : 0u));
       }
     };
     load(0);                                                 // under way before the weights are known
-    const float m_new = fmaxf(m, lanes_max(ml.x)), f = joined(m, m_new), fx = has ? joined(ml.x, m_new) : 0.f;
-    l = l * f + __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lanes_sum(ml.y * fx)), 63));
-    o.x *= f;
-    o.y *= f;
-    m = m_new;
+    float fx[HEADS];
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      const float m_new = fmaxf(m[h], lanes_max(ml[h].x)), f = joined(m[h], m_new);
+      fx[h] = has ? joined(ml[h].x, m_new) : 0.f;
+      l[h] = l[h] * f + __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lanes_sum(ml[h].y * fx[h])), 63));
+      o[h].x *= f;
+      o[h].y *= f;
+      m[h] = m_new;
+    }
     for (int k0 = 0;;) {
 #pragma unroll
-      for (int k = 0; k < SHARED_ROUND; ++k) {
-        const float w_k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fx), min(k0 + k, 63)));
-        if (k0 + k < here && w_k != 0.f) {
-          o.x = __builtin_fmaf(x[k].x, w_k, o.x);
-          o.y = __builtin_fmaf(x[k].y, w_k, o.y);
+      for (int k = 0; k < ROUND; ++k)
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h) {
+          const float w_k = k0 + k < here ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(fx[h]), min(k0 + k, 63))) : 0.f;
+          const bool there = w_k != 0.f;                     // (a weight is 2^-149 at least; what is not there may hold anything)
+          o[h].x = __builtin_fmaf(there ? x[h][k].x : 0.f, w_k, o[h].x);
+          o[h].y = __builtin_fmaf(there ? x[h][k].y : 0.f, w_k, o[h].y);
         }
-      }
-      if ((k0 += SHARED_ROUND) >= here) break;
+      if ((k0 += ROUND) >= here) break;
       load(k0);
     }
   }
-  if (lane_has) {
-    const bool empty = n == 0;
-    const float inv = a.out_scale / l;
-    const int64_t at = (int64_t)id * D + 2 * lane;
-    const float x = empty ? 0.f : o.x * inv, y = empty ? 0.f : o.y * inv;
-    if (a.out_bf16) *(unsigned*)((unsigned short*)a.out + at) = (unsigned)float_to_bf16_bits(x) | ((unsigned)float_to_bf16_bits(y) << 16);
-    else *(float2*)((float*)a.out + at) = make_float2(x, y);
-  }
+  if (lane_has)
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      if (h >= heads) break;
+      const bool empty = n == 0;
+      const float inv = a.out_scale / l[h];
+      const int64_t at = ((int64_t)r * a.Hq + g * a.G + h0 + h) * D + 2 * lane;
+      const float x = empty ? 0.f : o[h].x * inv, y = empty ? 0.f : o[h].y * inv;
+      if (a.out_bf16) *(unsigned*)((unsigned short*)a.out + at) = (unsigned)float_to_bf16_bits(x) | ((unsigned)float_to_bf16_bits(y) << 16);
+      else *(float2*)((float*)a.out + at) = make_float2(x, y);
+    }
 }
 
 }  // namespace
