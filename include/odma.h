@@ -361,7 +361,7 @@ int odma_prefill_attention(odma_pool_t* pool, int32_t layer, int32_t n, const vo
  * for t < S and at offsets[r] + t - S otherwise, and lengths[r] counts them all, shared ones included.
  *   prefix_start DEVICE int32[n_prefixes + 1]   prefix_offsets DEVICE int64[n_prefixes]   prefix_lengths DEVICE int32[n_prefixes]
  * (all three may be NULL with n_prefixes 0; 0 <= n_prefixes <= n). */
-#define ODMA_SLOT_NONE    (-1)   /* odma_append_qkv: the row is not there, nothing of it is read or written */
+#define ODMA_SLOT_NONE    (-1)   /* odma_append_qkv: the row is not there: what its q, k and v hold is ignored, its q_out left as it was */
 #define ODMA_SLOT_SHARED  (-2)   /* the row's K and V are in a shared block already: only its queries are prepared */
 
 /* Tables of a batch from its lengths, in one launch and without the host: what the paged calls, odma_prefill_attention and

@@ -117,6 +117,7 @@ int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma
   a.k_pool = ra.k;
   a.v_pool = ra.v;
   a.eps = prep->eps;
+  a.inv_D = 1.0f / (float)c.head_dim;
   a.k_inv = 1.0f / c.k_scale;
   a.v_inv = 1.0f / c.v_scale;
   a.Hq = c.n_q_heads;

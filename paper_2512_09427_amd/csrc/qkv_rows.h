@@ -13,6 +13,8 @@
 // log2(GROUP) exchanges.  k and v go through LDS so that they leave as the 16-byte pieces of their blocks.
 #pragma once
 
+#include <type_traits>
+
 #include "block_index.h"
 #include "kernels_common.h"
 
@@ -28,22 +30,29 @@ struct QkvArgs {
   const int32_t* positions;                // [n_axes][n_rows]
   int64_t n_rows, pool_tokens, head_stride;
   char *k_pool, *v_pool;                   // layer base
-  float eps, k_inv, v_inv;                 // fp8: 1 / k_scale, 1 / v_scale
+  float eps, inv_D, k_inv, v_inv;          // 1 / D; fp8: 1 / k_scale, 1 / v_scale
   int32_t Hq, Hkv, D, rot_dim, adjacent, heads_per_wg;
   uint8_t axis[ODMA_MAX_ROT_PAIRS];
 };
 
-__device__ __forceinline__ void load4(const unsigned short* p, float (&x)[8], int at) {
-  const uint2v w = *(const uint2v*)p;
-  x[at] = __uint_as_float(w[0] << 16);
-  x[at + 1] = __uint_as_float(w[0] & 0xffff0000u);
-  x[at + 2] = __uint_as_float(w[1] << 16);
-  x[at + 3] = __uint_as_float(w[1] & 0xffff0000u);
+// four channels as they lie in memory, and as numbers
+struct Bf16x4 {
+  uint2v w;
+};
+struct F32x4 {
+  float4v w;
+};
+__device__ __forceinline__ Bf16x4 take4(const unsigned short* p) { return {*(const uint2v*)p}; }
+__device__ __forceinline__ F32x4 take4(const float* p) { return {*(const float4v*)p}; }
+__device__ __forceinline__ void widen4(const Bf16x4& r, float* x) {
+  x[0] = __uint_as_float(r.w[0] << 16);
+  x[1] = __uint_as_float(r.w[0] & 0xffff0000u);
+  x[2] = __uint_as_float(r.w[1] << 16);
+  x[3] = __uint_as_float(r.w[1] & 0xffff0000u);
 }
-__device__ __forceinline__ void load4(const float* p, float (&x)[8], int at) {
-  const float4v w = *(const float4v*)p;
+__device__ __forceinline__ void widen4(const F32x4& r, float* x) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[at + i] = w[i];
+  for (int i = 0; i < 4; ++i) x[i] = r.w[i];
 }
 __device__ __forceinline__ void store4(unsigned short* p, const float* x) {
   uint2v w;
@@ -59,6 +68,38 @@ __device__ __forceinline__ void store4(unsigned char* p, const float* x) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(x[0]), e4m3_range(x[1]), 0, false);
   w = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(x[2]), e4m3_range(x[3]), w, true);
   *(int*)p = w;
+}
+
+// 1 / sqrt(v); the instruction takes denormal numbers for 0
+__device__ __forceinline__ float root_of_inverse(float v) {
+  const bool tiny = v < 0x1p-96f;
+  return __builtin_amdgcn_rsqf(tiny ? v * 0x1p96f : v) * (tiny ? 0x1p48f : 1.f);
+}
+
+// The sum over the GROUP lanes that share a head's row, in all of them: moves inside quads, halves of rows and rows (each leaves its
+// lanes with equal sums, so a mirror adds the other half's).
+template <int GROUP>
+__device__ __forceinline__ float group_sum(float x) {
+  auto moved = [](float v, auto ctrl) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false)); };
+  x += moved(x, std::integral_constant<int, 0xb1>{});        // lanes 1 0 3 2
+  x += moved(x, std::integral_constant<int, 0x4e>{});        // lanes 2 3 0 1
+  if (GROUP >= 8) x += moved(x, std::integral_constant<int, 0x141>{});
+  if (GROUP >= 16) x += moved(x, std::integral_constant<int, 0x140>{});
+  if (GROUP >= 32) x += __shfl_xor(x, 16);
+  return x;
+}
+
+// sine and cosine of f turns, |f| <= 1/2: the nearest quarter turn and the Taylor series of what is left, at most an eighth (pi / 4
+// radians, where the terms that are left out are below 2^-28 and 2^-30)
+__device__ __forceinline__ void sincos_of_turn(float f, float& sn, float& cs) {
+  const float quarter = rintf(4.f * f);
+  const float t = __builtin_fmaf(-0.25f, quarter, f) * 6.2831853071795865f, t2 = t * t;
+  const float s = t * __builtin_fmaf(t2, __builtin_fmaf(t2, __builtin_fmaf(t2, __builtin_fmaf(t2, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), 1.f);
+  const float c = __builtin_fmaf(t2, __builtin_fmaf(t2, __builtin_fmaf(t2, __builtin_fmaf(t2, __builtin_fmaf(t2, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+  const int k = (int)quarter;                                // (NaN: the series are NaN)
+  const float a = k & 1 ? c : s, b = k & 1 ? s : c;
+  sn = k & 2 ? -a : a;
+  cs = (k + 1) & 2 ? -b : b;
 }
 
 // T: rows; S: storage of the pools (T, or unsigned char for E4M3).  GROUP: lanes of a head's row, a power of two >= D / 8.
@@ -79,9 +120,86 @@ __global__ __launch_bounds__(256) void append_qkv_kernel(QkvArgs a) {
   const int64_t row0 = (int64_t)blockIdx.x * BLK;
   const int H = a.Hq + 2 * a.Hkv, h0 = blockIdx.y * a.heads_per_wg, h1 = min(h0 + a.heads_per_wg, H);
 
-  // ---- the rows: every wave looks at all 16.  A quad is four rows that fill an aligned group of four slots of a block.
+  // this lane's channels: [ca, ca + 4) and [cb, cb + 4)
+  const bool in_head = u < a.D / 8, turned = 8 * u < a.rot_dim;
+  const int ca = a.adjacent || !turned ? 8 * u : 4 * u, cb = a.adjacent || !turned ? 8 * u + 4 : a.rot_dim / 2 + 4 * u;
+  int64_t row[RP];
+  bool there[RP];                                          // (the row is in the arrays; further down: and has a slot)
+#pragma unroll
+  for (int rp = 0; rp < RP; ++rp) {
+    row[rp] = row0 + row_in + rp * (BLK / RP);
+    there[rp] = in_head && row[rp] < a.n_rows;
+  }
+  // A batch: HB heads of one kind (0: queries, 1: keys, 2: values) from h on, up to end.
+  struct Batch {
+    int kind, h, end;
+  };
+  auto batch_at = [&](int head) {                          // head: of all, queries first
+    if (head < a.Hq) return Batch{0, head, min(h1, a.Hq)};
+    if (head < a.Hq + a.Hkv) return Batch{1, head - a.Hq, min(h1, a.Hq + a.Hkv) - a.Hq};
+    return Batch{2, head - a.Hq - a.Hkv, h1 - a.Hq - a.Hkv};
+  };
+  auto behind = [&](const Batch& b) { return (b.kind > 0 ? a.Hq : 0) + (b.kind > 1 ? a.Hkv : 0) + min(b.h + HB, b.end); };
+  using Four = decltype(take4((const T*)nullptr));
+  auto load = [&](Four (&x)[NB][RP][2], const Batch& bt) {
+    const T* src = (const T*)(bt.kind == 0 ? a.q : bt.kind == 1 ? a.k : a.v);
+    const int64_t stride = bt.kind == 0 ? a.q_stride : bt.kind == 1 ? a.k_stride : a.v_stride;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int rp = 0; rp < RP; ++rp) {
+        const int hh = bt.h + b * HP + sub;
+        x[b][rp][0] = x[b][rp][1] = Four{};
+        if (there[rp] && hh < bt.end) {
+          const T* p = src + row[rp] * stride + (int64_t)hh * a.D;
+          x[b][rp][0] = take4(p + ca);
+          x[b][rp][1] = take4(p + cb);
+        }
+      }
+  };
+
+  // ---- one round of loads: the first batch, slots, positions, frequencies, weights (of rows without a slot too)
+  Four next[NB][RP][2];
+  Batch bt = batch_at(h0);
+  load(next, bt);
   int64_t slot16 = ODMA_SLOT_NONE;
   if (lane < BLK && row0 + lane < a.n_rows) slot16 = a.row_slot[row0 + lane];
+  float cs[RP][4], sn[RP][4];
+  {
+    const bool angles = turned && bt.kind < 2;
+    int pos[RP][4];
+    float freq[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      freq[e] = angles ? a.inv_freq[4 * u + e] : 0.f;
+#pragma unroll
+      for (int rp = 0; rp < RP; ++rp) pos[rp][e] = angles && there[rp] ? a.positions[(int64_t)a.axis[4 * u + e] * a.n_rows + row[rp]] : 0;
+    }
+#pragma unroll
+    for (int rp = 0; rp < RP; ++rp)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        cs[rp][e] = 1.f;
+        sn[rp][e] = 0.f;
+        if (angles) {
+          const double turns = (double)pos[rp][e] * ((double)freq[e] * 0.15915494309189535);
+          sincos_of_turn((float)(turns - rint(turns)), sn[rp][e], cs[rp][e]);
+        }
+      }
+  }
+  float wq[8], wk[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) wq[i] = wk[i] = 1.f;
+  if (in_head && a.q_weight) {
+    widen4(take4((const T*)a.q_weight + ca), wq);
+    widen4(take4((const T*)a.q_weight + cb), wq + 4);
+  }
+  if (in_head && a.k_weight) {
+    widen4(take4((const T*)a.k_weight + ca), wk);
+    widen4(take4((const T*)a.k_weight + cb), wk + 4);
+  }
+
+  // ---- the rows' slots: every wave looks at all 16.  A quad is four rows that fill an aligned group of four slots of a block.
   if (slot16 >= a.pool_tokens) slot16 = ODMA_SLOT_NONE;
   unsigned quads, stored;
   {
@@ -92,49 +210,17 @@ __global__ __launch_bounds__(256) void append_qkv_kernel(QkvArgs a) {
     stored = (unsigned)__builtin_amdgcn_ballot_w64(slot16 >= 0) & 0xffffu;
   }
   const unsigned singles = stored & ~(quads | quads << 1 | quads << 2 | quads << 3);
-  if (tid < BLK) slots[tid] = slot16;
-  __syncthreads();
+  const unsigned present = (unsigned)__builtin_amdgcn_ballot_w64(slot16 != ODMA_SLOT_NONE) & 0xffffu;
+#pragma unroll
+  for (int rp = 0; rp < RP; ++rp) there[rp] = there[rp] && (present >> (row_in + rp * (BLK / RP)) & 1);
+  if (tid < BLK) slots[tid] = slot16;                        // (read behind the first barrier of keys or values)
 
-  // ---- this lane's channels: [ca, ca + 4) and [cb, cb + 4)
-  const bool in_head = u < a.D / 8, turned = 8 * u < a.rot_dim;
-  const int ca = a.adjacent || !turned ? 8 * u : 4 * u, cb = a.adjacent || !turned ? 8 * u + 4 : a.rot_dim / 2 + 4 * u;
-  bool there[RP];
-  int64_t row[RP];
-  float cs[RP][4], sn[RP][4];
-#pragma unroll
-  for (int rp = 0; rp < RP; ++rp) {
-    row[rp] = row0 + row_in + rp * (BLK / RP);
-    there[rp] = in_head && slots[row_in + rp * (BLK / RP)] != ODMA_SLOT_NONE && row[rp] < a.n_rows;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      cs[rp][e] = 1.f;
-      sn[rp][e] = 0.f;
-      if (there[rp] && turned && h0 < a.Hq + a.Hkv) {
-        const int f = 4 * u + e;
-        const double turns = (double)a.positions[(int64_t)a.axis[f] * a.n_rows + row[rp]] * ((double)a.inv_freq[f] * 0.15915494309189535);
-        sincospif(2.f * (float)(turns - rint(turns)), &sn[rp][e], &cs[rp][e]);
-      }
-    }
-  }
-  float wq[8], wk[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) wq[i] = wk[i] = 1.f;
-  if (in_head && a.q_weight) {
-    load4((const T*)a.q_weight + ca, wq, 0);
-    load4((const T*)a.q_weight + cb, wq, 4);
-  }
-  if (in_head && a.k_weight) {
-    load4((const T*)a.k_weight + ca, wk, 0);
-    load4((const T*)a.k_weight + cb, wk, 4);
-  }
   auto prepare = [&](float (&x)[8], const float (&w)[8], bool norm, int rp) {
     if (norm) {
       float ss = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(x[i], x[i], ss);
-#pragma unroll
-      for (int o = GROUP / 2; o >= 1; o >>= 1) ss += __shfl_xor(ss, o);
-      const float inv = 1.f / sqrtf(ss / (float)a.D + a.eps);
+      const float inv = root_of_inverse(__builtin_fmaf(group_sum<GROUP>(ss), a.inv_D, a.eps));
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = x[i] * inv * w[i];
     }
@@ -156,66 +242,57 @@ __global__ __launch_bounds__(256) void append_qkv_kernel(QkvArgs a) {
       }
     }
   };
-  // the same heads of all rows of the tile: HB heads from h on, of `src` with `heads` heads
-  auto load = [&](float (&x)[NB][RP][8], const T* src, int64_t stride, int h, int end) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int rp = 0; rp < RP; ++rp) {
-        const int hh = h + b * HP + sub;
-        if (there[rp] && hh < end) {
-          const T* p = src + row[rp] * stride + (int64_t)hh * a.D;
-          load4(p + ca, x[b][rp], 0);
-          load4(p + cb, x[b][rp], 4);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[b][rp][i] = 0.f;
-        }
-      }
-  };
-
-  // ---- queries
-  for (int h = h0; h < min(h1, a.Hq); h += HB) {
-    float x[NB][RP][8];
-    const int end = min(h1, a.Hq);
-    load(x, (const T*)a.q, a.q_stride, h, end);
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int rp = 0; rp < RP; ++rp) {
-        const int hh = h + b * HP + sub;
-        prepare(x[b][rp], wq, a.q_weight != nullptr, rp);
-        if (there[rp] && hh < end) {
-          T* o = (T*)a.q_out + (row[rp] * a.Hq + hh) * a.D;
-          store4(o + ca, x[b][rp]);
-          store4(o + cb, x[b][rp] + 4);
-        }
-      }
-  }
-  // ---- keys, then values: staged, then written piece by piece
   const int64_t block_bytes = (int64_t)BLK * a.D * (int)sizeof(S);
   const int pieces = a.D / X;                              // 16-byte pieces of a head's row
+  for (;;) {
+    Four raw[NB][RP][2];
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    const int lo = kv ? a.Hkv : 0;                         // heads of this kind: [Hq + lo, Hq + lo + Hkv)
-    const int begin = max(h0 - a.Hq - lo, 0), end = min(h1 - a.Hq - lo, a.Hkv);
-    for (int h = begin; h < end; h += HB) {
-      float x[NB][RP][8];
-      if (kv) load(x, (const T*)a.v, a.v_stride, h, end);
-      else load(x, (const T*)a.k, a.k_stride, h, end);
-      __syncthreads();                                     // the batch before has been written
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int rp = 0; rp < RP; ++rp)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) raw[b][rp][i] = next[b][rp][i];
+    const int head = behind(bt), h = bt.h, end = bt.end, kv = bt.kind - 1;
+    const Batch now = bt;
+    if (head < h1) {                                         // under way while this one is prepared and stored
+      bt = batch_at(head);
+      load(next, bt);
+    }
+    if (now.kind == 0) {
+      // ---- queries
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int rp = 0; rp < RP; ++rp) {
-          if (!kv) prepare(x[b][rp], wk, a.k_weight != nullptr, rp);
+          const int hh = h + b * HP + sub;
+          float x[8];
+          widen4(raw[b][rp][0], x);
+          widen4(raw[b][rp][1], x + 4);
+          prepare(x, wq, a.q_weight != nullptr, rp);
+          if (there[rp] && hh < end) {
+            T* o = (T*)a.q_out + (row[rp] * a.Hq + hh) * a.D;
+            store4(o + ca, x);
+            store4(o + cb, x + 4);
+          }
+        }
+    } else {
+      // ---- keys and values: staged, then written piece by piece
+      __syncthreads();                                       // the batch before has been written
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int rp = 0; rp < RP; ++rp) {
+          float x[8];
+          widen4(raw[b][rp][0], x);
+          widen4(raw[b][rp][1], x + 4);
+          if (!kv) prepare(x, wk, a.k_weight != nullptr, rp);
           if (FP8)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[b][rp][i] *= kv ? a.v_inv : a.k_inv;
+            for (int i = 0; i < 8; ++i) x[i] *= kv ? a.v_inv : a.k_inv;
           if (in_head) {
             S* o = stage + ((b * HP + sub) * BLK + row_in + rp * (BLK / RP)) * STRIDE;
-            store4(o + ca, x[b][rp]);
-            store4(o + cb, x[b][rp] + 4);
+            store4(o + ca, x);
+            store4(o + cb, x + 4);
           }
         }
       __syncthreads();
@@ -259,17 +336,25 @@ __global__ __launch_bounds__(256) void append_qkv_kernel(QkvArgs a) {
 #pragma unroll
             for (int k = 0; k < (int)sizeof(piece) / 16; ++k) to[k] = ((const uint4v*)piece)[k];
           }
-          // other rows: element by element
-          for (unsigned left = singles; left; left &= left - 1) {
-            const int t = __builtin_ctz(left);
+          // other rows: element by element, two rows at a time where their channels leave threads over
+          const int rows_at_once = a.D <= 128 ? 2 : 1, half = rows_at_once == 2 ? tid >> 7 : 0, d0 = rows_at_once == 2 ? tid & 127 : tid;
+          for (unsigned left = singles; left;) {
+            unsigned mine = left;
+            left &= left - 1;
+            if (rows_at_once == 2) {
+              if (half) mine = left;
+              left &= left - 1;
+            }
+            if (!mine || d0 >= a.D) continue;
+            const int t = __builtin_ctz(mine);
             const int64_t slot = slots[t];
             S* block = (S*)(plane + slot / BLK * block_bytes);
-            for (int d = tid; d < a.D; d += 256)
-              block[FP8 ? v_index_fp8((int)(slot % BLK), d) : v_index((int)(slot % BLK), d)] = rows[t * STRIDE + d];
+            block[FP8 ? v_index_fp8((int)(slot % BLK), d0) : v_index((int)(slot % BLK), d0)] = rows[t * STRIDE + d0];
           }
         }
       }
     }
+    if (head >= h1) break;
   }
 }
 
