@@ -126,6 +126,11 @@ int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma
   a.rot_dim = prep->rot_dim;
   a.adjacent = prep->rot_pairs == ODMA_ROT_ADJACENT;
   const int group = c.head_dim <= 32 ? 4 : c.head_dim <= 64 ? 8 : c.head_dim <= 128 ? 16 : 32;
+  // Beyond an XCD's L2, queries leave past the caches and leave those to the keys and values, if a wave's store fills what it
+  // touches (fp32 pairs in runs of four do not).  32 heads x 128 of bf16, 8 of k and v, before and after: 2 000 rows 14.0 -> 12.9 us,
+  // 8 000 34.8 -> 31.5, 65 869 246 -> 244, not rotated 32.6 -> 26.2 at 8 000; fp32 rotated in halves 64.7 -> 63.2 at 8 000, and
+  // 64.7 -> 67.7 not rotated, where it would touch halves of 32 bytes.
+  a.stream_q = n_rows * a.Hq * a.D * (pool->elem_bytes == 4 ? 4 : 2) > (4 << 20) && (pool->elem_bytes != 4 || (!a.adjacent && a.rot_dim == a.D));
   // few rows: the heads are dealt out, down to one pass of a work-group each
   const int64_t tiles = (n_rows + BLK - 1) / BLK;
   const int heads = a.Hq + 2 * a.Hkv, pass = group < 16 ? 16 / group : 1, passes = (heads + pass - 1) / pass;

@@ -32,6 +32,7 @@ struct QkvArgs {
   char *k_pool, *v_pool;                   // layer base
   float eps, inv_D, k_inv, v_inv;          // 1 / D; fp8: 1 / k_scale, 1 / v_scale
   int32_t Hq, Hkv, D, rot_dim, adjacent, heads_per_wg;
+  int32_t stream_q;                        // the queries are more than a cache keeps: they leave past it
   uint8_t axis[ODMA_MAX_ROT_PAIRS];
 };
 
@@ -54,14 +55,18 @@ __device__ __forceinline__ void widen4(const F32x4& r, float* x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i] = r.w[i];
 }
-__device__ __forceinline__ void store4(unsigned short* p, const float* x) {
+__device__ __forceinline__ uint2v rounded4(const unsigned short*, const float* x) {
   uint2v w;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
     w[i] = (unsigned)float_to_bf16_bits(x[2 * i]) | ((unsigned)float_to_bf16_bits(x[2 * i + 1]) << 16);
-  *(uint2v*)p = w;
+  return w;
 }
-__device__ __forceinline__ void store4(float* p, const float* x) { *(float4v*)p = float4v{x[0], x[1], x[2], x[3]}; }
+__device__ __forceinline__ float4v rounded4(const float*, const float* x) { return float4v{x[0], x[1], x[2], x[3]}; }
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const float* x) {
+  *(decltype(rounded4(p, x))*)p = rounded4(p, x);
+}
 // E4M3, to nearest even; beyond +-448 (infinities too) the largest value, NaN stays NaN
 __device__ __forceinline__ float e4m3_range(float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); }
 __device__ __forceinline__ void store4(unsigned char* p, const float* x) {
@@ -271,8 +276,25 @@ __global__ __launch_bounds__(256) void append_qkv_kernel(QkvArgs a) {
           prepare(x, wq, a.q_weight != nullptr, rp);
           if (there[rp] && hh < end) {
             T* o = (T*)a.q_out + (row[rp] * a.Hq + hh) * a.D;
-            store4(o + ca, x);
-            store4(o + cb, x + 4);
+            using Out = decltype(rounded4(o, x));
+            const Out lo = rounded4(o, x), hi = rounded4(o, x + 4);
+            if (!a.stream_q) {
+              *(Out*)(o + ca) = lo;
+              *(Out*)(o + cb) = hi;
+            } else {
+              asm volatile("" ::: "memory");                 // (or the compiler makes ordinary stores of all branches)
+              bool whole = false;
+              if constexpr (sizeof(T) == 2)
+                if (cb == ca + 4) {                          // a store past the caches has to fill what it touches
+                  __builtin_nontemporal_store(uint4v{lo[0], lo[1], hi[0], hi[1]}, (uint4v*)(o + ca));
+                  whole = true;
+                }
+              if (!whole) {
+                __builtin_nontemporal_store(lo, (Out*)(o + ca));
+                __builtin_nontemporal_store(hi, (Out*)(o + cb));
+              }
+              asm volatile("" ::: "memory");
+            }
           }
         }
     } else {
