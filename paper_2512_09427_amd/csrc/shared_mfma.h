@@ -171,12 +171,18 @@ __device__ __forceinline__ int column_blocks(int count, int G) { return (count *
 // Factor of a state joined to another.  At least the smallest number: 0 would make an infinite sum NaN.
 __device__ __forceinline__ float joined(float m, float m_new) { return fmaxf(__builtin_amdgcn_exp2f(m - m_new), 0x1p-149f); }
 
-// A weight as two bf16 parts: cut off, and the rest rounded (2^-16 in all).  Neither is negative, nor 0 unless the weight is: an
-// infinite V times the parts is that infinity, as times the weight.
-__device__ __forceinline__ void two_parts(float w, __bf16& hi, __bf16& lo) {
-  const unsigned bits = __float_as_uint(w) & 0xffff0000u;
-  hi = __builtin_bit_cast(__bf16, (unsigned short)(bits >> 16));
-  lo = (__bf16)fmaxf(w - __uint_as_float(bits), w * 0x1p-40f);
+// A weight as N bf16 parts: all but the last cut off, the last rounded (2^-9 of it in all for N = 1, 2^-17 for 2, exact for 3).
+// None is negative, nor 0 unless the weight is: an infinite V times the parts is that infinity, as times the weight.
+template <int N>
+__device__ __forceinline__ void weight_parts(float w, bf16x8 (&parts)[N], int at) {
+  float rest = w;
+#pragma unroll
+  for (int k = 0; k < N - 1; ++k) {
+    const unsigned bits = __float_as_uint(rest) & 0xffff0000u;
+    parts[k][at] = __builtin_bit_cast(__bf16, (unsigned short)(bits >> 16));
+    rest = fmaxf(rest - __uint_as_float(bits), w * 0x1p-40f);
+  }
+  parts[N - 1][at] = (__bf16)rest;
 }
 
 // inclusive sums over the lanes of a wave, by moves inside rows of 16 and broadcasts between them
@@ -224,10 +230,10 @@ __device__ __forceinline__ int last_at_most(const int32_t* pos, int n, int x) {
   return probe(lane) - 1;
 }
 
-// LO: the weights of line A go through the matrix cores as two bf16 parts (16 bits) instead of one; for fp32 results.
-// (Line B, bound by memory, always does.)  A single rounding of a weight is half a bf16 step of one term of the sum, as the
-// rounding of a bf16 result is of the whole.
-template <int FMT, bool PAGED, bool LO>
+// EXACT: the weights go through the matrix cores as three bf16 parts, all their bits; for fp32 results.  Otherwise as one part in
+// line A (half a bf16 step of one term of the sum, as the rounding of a bf16 result is of the whole) and as two in line B, where
+// matrix instructions wait for memory in any case.
+template <int FMT, bool PAGED, bool EXACT>
 __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedArgs a) {
   constexpr bool FP8 = FMT == SHARED_FP8_128;
   constexpr int D = FMT == SHARED_BF16_64 ? 64 : 128;
@@ -235,7 +241,8 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
   constexpr int TILE_BYTES = BLK * D * (FP8 ? 1 : 2), LOADS = TILE_BYTES / 1024;
   constexpr int K_STAGE = 2 * NS * 1024, STAGE_BYTES = 2 * K_STAGE;
   constexpr int CT = SHARED_CT;
-  constexpr int V_AHEAD = D == 64 ? DT : LO ? 2 : 5;        // V operands that there are registers for in front of their weights
+  constexpr int PARTS_A = EXACT ? 3 : 1, PARTS_B = EXACT ? 3 : 2;
+  constexpr int V_AHEAD = D == 64 ? DT : EXACT ? 1 : 5;       // V operands that there are registers for in front of their weights
   constexpr float SLACK = 8.0f;                             // exponent units by which a score may exceed the reference
   __shared__ __attribute__((aligned(16))) char stage_mem[2 * STAGE_BYTES];
   __shared__ SharedPlan plan;
@@ -564,37 +571,25 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
           read_k(k1, pr + 1 - i0, 1);
           scores(ahead, k0, 0);
           scores(ahead, k1, 1);
-          bf16x8 ph[CT], pl[CT];
+          bf16x8 w[CT][PARTS_A];
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float pv = __builtin_amdgcn_exp2f(x[ct][b][i] * a.scale_log2);
-                if (LO) {
-                  __bf16 hi, lo;
-                  two_parts(pv, hi, lo);
-                  ph[ct][4 * b + i] = hi;
-                  pl[ct][4 * b + i] = lo;
-                } else {
-                  ph[ct][4 * b + i] = (__bf16)pv;
-                }
-              }
+              for (int i = 0; i < 4; ++i) weight_parts(__builtin_amdgcn_exp2f(x[ct][b][i] * a.scale_log2), w[ct], 4 * b + i);
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, ph[ct], l[ct], 0, 0, 0);
-            if (LO) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pl[ct], l[ct], 0, 0, 0);
-          }
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int k = 0; k < PARTS_A; ++k) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, w[ct][k], l[ct], 0, 0, 0);
 #pragma unroll
           for (int dt = V_AHEAD; dt < DT; ++dt) av[dt] = *(const bf16x8*)(st + dt * 1024);
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-              O[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], ph[ct], O[ct][dt], 0, 0, 0);
-              if (LO) O[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], pl[ct], O[ct][dt], 0, 0, 0);
-            }
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+              for (int k = 0; k < PARTS_A; ++k) O[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], w[ct][k], O[ct][dt], 0, 0, 0);
         };
         // pipeline: load j + 3 is under way while pair j is computed; load j + 2 goes from registers into its stage behind it, where
         // pair j + 1 finds it, and one barrier per pair makes it visible
@@ -750,7 +745,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) O[dt] *= f;
         }
-        bf16x8 ph, pl;
+        bf16x8 w_parts[PARTS_B];
         float sum = 0.f;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -758,10 +753,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
           for (int i = 0; i < 4; ++i) {
             const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][i], a.scale_log2, -m));
             sum += pv;
-            __bf16 hi, lo;
-            two_parts(pv, hi, lo);
-            ph[4 * b + i] = hi;
-            pl[4 * b + i] = lo;
+            weight_parts(pv, w_parts, 4 * b + i);
           }
         l += sum;
         bf16x8 av[DT];
@@ -783,10 +775,9 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
         }
         if (more) load(vr, a.v, at);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], ph, O[dt], 0, 0, 0);
-          O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], pl, O[dt], 0, 0, 0);
-        }
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int k = 0; k < PARTS_B; ++k) O[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[dt], w_parts[k], O[dt], 0, 0, 0);
       }
       l += __shfl_xor(l, 16);
       l += __shfl_xor(l, 32);
