@@ -405,9 +405,9 @@ typedef struct odma_qk_prep {
  *   q, k, v     DEVICE rows of [Hq][D], [Hkv][D], [Hkv][D], in fp32 for ODMA_F32 pools, else bf16; row i at element
  *               i * q_stride (k_stride, v_stride): parts of one projection's rows, for instance.  Pointers and strides are
  *               multiples of 16 bytes
- *   row_slot    DEVICE int64[n_rows]: token slot of each row in the pool (odma_build_tables), ODMA_SLOT_NONE or
- *               ODMA_SLOT_SHARED.  Slots past the pool are taken as ODMA_SLOT_NONE, other negative ones as ODMA_SLOT_SHARED.  No two rows may have the same slot (both
- *               would be written, in any order)
+ *   row_slot    DEVICE int64[n_rows], n_rows <= 2^27: token slot of each row in the pool (odma_build_tables), ODMA_SLOT_NONE or
+ *               ODMA_SLOT_SHARED.  Slots past the pool are taken as ODMA_SLOT_NONE, other negative ones as ODMA_SLOT_SHARED.
+ *               No two rows may have the same slot (both would be written, in any order)
  *   positions   DEVICE int32[n_axes][n_rows] (NULL with rot_dim 0)
  *   q_out       DEVICE [n_rows][Hq][D], type of the rows; may be q itself where q_stride is Hq * D, else apart from q, k, v
  * Other slots of the pool keep what they hold.  Uses no workspace.  Capacity is the caller's business (odma_advance). */
@@ -422,7 +422,7 @@ int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma
  *   block_table DEVICE int32[n][bt_stride] or NULL: every request's blocks, shared ones first (odma_build_tables); prefix_offsets
  *               is then ignored (NULL allowed): a prefix is read through the row of one of its requests
  * A request shorter than what its group shares attends to its lengths[r] first tokens.  n_prefixes = 0: odma_decode_attention.
- * Matrix-core pools only (bf16 with head_dim 128 or 64, fp8), n <= ODMA_SHARED_MAX_REQUESTS; ODMA_INVALID_ARG otherwise.
+ * Matrix-core pools only (bf16 with head_dim 128 or 64, fp8), sm_scale > 0, n <= ODMA_SHARED_MAX_REQUESTS; ODMA_INVALID_ARG otherwise.
  * Partial results live in the pool's workspace: such calls must not overlap on different streams with each other, with
  * decode calls or with odma_prefill_attention on the null stream.  A plan that decode calls may reuse survives. */
 #define ODMA_SHARED_MAX_REQUESTS 1024

@@ -29,7 +29,8 @@ void launch_append_qkv(const QkvArgs& a, int group, dim3 grid, hipStream_t s) {
 }
 
 constexpr int TABLES_WG = 1024;   // work-groups up to which a launch is dealt out
-constexpr int ROWS_WG = 1024;
+constexpr int ROWS_WG = 1024;     // (four a compute unit: a round of them)
+constexpr int64_t MAX_ROWS = (int64_t)1 << 27;   // (a launch has fewer than 2^32 threads)
 
 }  // namespace
 
@@ -82,7 +83,7 @@ int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma
   const odma_pool_config_t& c = pool->cfg;
   if (layer < 0 || layer >= c.n_layers || n_rows < 0 || !prep || !q || !k || !v || !row_slot || !q_out)
     return refuse(where, "invalid argument");
-  if (n_rows > (int64_t)0x7fffffff * BLK) return refuse(where, "too many rows");
+  if (n_rows > MAX_ROWS) return refuse(where, "too many rows");
   const int unit = pool->elem_bytes == 4 ? 4 : 8;            // elements of 16 bytes of a row
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || q_stride < 0 || k_stride < 0 || v_stride < 0 ||
       q_stride % unit || k_stride % unit || v_stride % unit)
@@ -131,12 +132,17 @@ int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma
   // 8 000 34.8 -> 31.5, 65 869 246 -> 244, not rotated 32.6 -> 26.2 at 8 000; fp32 rotated in halves 64.7 -> 63.2 at 8 000, and
   // 64.7 -> 67.7 not rotated, where it would touch halves of 32 bytes.
   a.stream_q = n_rows * a.Hq * a.D * (pool->elem_bytes == 4 ? 4 : 2) > (4 << 20) && (pool->elem_bytes != 4 || (!a.adjacent && a.rot_dim == a.D));
-  // few rows: the heads are dealt out, down to one pass of a work-group each
-  const int64_t tiles = (n_rows + BLK - 1) / BLK;
+  // Whole rounds of ROWS_WG work-groups take 16 rows with all their heads each; the rows behind them (all, where there are few) deal
+  // their heads out to a round of their own, down to one pass of a work-group.
+  const int64_t tiles = (n_rows + BLK - 1) / BLK, whole = tiles / ROWS_WG * ROWS_WG, rest = tiles - whole;
   const int heads = a.Hq + 2 * a.Hkv, pass = group < 16 ? 16 / group : 1, passes = (heads + pass - 1) / pass;
-  const int split = (int)std::min<int64_t>(passes, std::max<int64_t>((ROWS_WG + tiles - 1) / tiles, 1));
+  const int split = rest ? (int)std::min<int64_t>(passes, (ROWS_WG + rest - 1) / rest) : 1;
   a.heads_per_wg = (passes + split - 1) / split * pass;
-  const dim3 grid((unsigned)tiles, (unsigned)((heads + a.heads_per_wg - 1) / a.heads_per_wg));
+  a.whole = (int32_t)whole;
+  const int parts = (heads + a.heads_per_wg - 1) / a.heads_per_wg;
+  a.rest = (int32_t)rest;
+  a.rest_inverse = rest > 1 ? (uint32_t)(((1ull << 32) + rest - 1) / rest) : 0;   // (exact: rest * parts, at most 2 ROWS_WG, times rest is below 2^32)
+  const dim3 grid((unsigned)(whole + rest * parts));
   hipStream_t s = (hipStream_t)stream;
   if (pool->elem_bytes == 1) hipLaunchKernelGGL((append_qkv_kernel<unsigned short, unsigned char, 16>), grid, dim3(256), 0, s, a);
   else if (pool->elem_bytes == 2) launch_append_qkv<unsigned short, unsigned short>(a, group, grid, s);

@@ -39,6 +39,7 @@ int odma_decode_attention_shared(odma_pool_t* pool, int32_t layer, int32_t n, co
     return refuse("0 to n prefixes, each with a start, an offset and a length");
   if (n_prefixes == 0)
     return odma_decode_attention(pool, layer, n, q, offsets, lengths, block_table, bt_stride, out, 0, stream);
+  if (!(c.sm_scale > 0.f)) return refuse("needs a positive softmax scale");   // (references are the largest raw scores)
   if (n > ODMA_SHARED_MAX_REQUESTS) return refuse("n exceeds ODMA_SHARED_MAX_REQUESTS");
   char* ws = (char*)c.workspace;
   const RowArgs ra = row_args(pool, layer);

@@ -31,7 +31,9 @@ struct QkvArgs {
   int64_t n_rows, pool_tokens, head_stride;
   char *k_pool, *v_pool;                   // layer base
   float eps, inv_D, k_inv, v_inv;          // 1 / D; fp8: 1 / k_scale, 1 / v_scale
-  int32_t Hq, Hkv, D, rot_dim, adjacent, heads_per_wg;
+  int32_t Hq, Hkv, D, rot_dim, adjacent;
+  int32_t whole, rest, heads_per_wg;       // tiles of 16 rows that a work-group takes whole; others, of which it takes some heads
+  uint32_t rest_inverse;                   // 2^32 / rest, upwards (0: rest is 1)
   int32_t stream_q;                        // the queries are more than a cache keeps: they leave past it
   uint8_t axis[ODMA_MAX_ROT_PAIRS];
 };
@@ -122,8 +124,10 @@ __global__ __launch_bounds__(256) void append_qkv_kernel(QkvArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int u = tid % GROUP, sub = HP > 1 ? tid / (GROUP * BLK) : 0;
   const int row_in = RP > 1 ? tid / GROUP : (tid / GROUP) % BLK;   // (RP = 2: and 8 rows on)
-  const int64_t row0 = (int64_t)blockIdx.x * BLK;
-  const int H = a.Hq + 2 * a.Hkv, h0 = blockIdx.y * a.heads_per_wg, h1 = min(h0 + a.heads_per_wg, H);
+  const int H = a.Hq + 2 * a.Hkv, cut = (int)blockIdx.x - a.whole;   // (cut >= 0: a piece of a tile)
+  const int part = cut < 0 ? 0 : a.rest_inverse ? (int)__umulhi((unsigned)cut, a.rest_inverse) : cut;
+  const int64_t row0 = (int64_t)(cut < 0 ? (int)blockIdx.x : a.whole + cut - part * a.rest) * BLK;
+  const int h0 = part * a.heads_per_wg, h1 = cut < 0 ? H : min(h0 + a.heads_per_wg, H);
 
   // this lane's channels: [ca, ca + 4) and [cb, cb + 4)
   const bool in_head = u < a.D / 8, turned = 8 * u < a.rot_dim;

@@ -71,7 +71,7 @@ def test_rows(runtime):  # noqa: F811
                     dict(q=Q + 8), dict(k=K + 2), dict(v=V + 4), dict(out=OUT + 8), dict(qs=1028), dict(ks=12), dict(vs=-8),
                     dict(q_weight=Q + 2), dict(k_weight=Q + 8), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")),
                     dict(rot_dim=-8), dict(rot_dim=136), dict(rot_dim=20), dict(inv_freq=None), dict(pos=None), dict(n_axes=0),
-                    dict(n_axes=5), dict(n_axes=2, axis=[0, 1, 2]), dict(n=1 << 40)):
+                    dict(n_axes=5), dict(n_axes=2, axis=[0, 1, 2]), dict(n=1 << 40), dict(n=(1 << 27) + 1)):
             assert refused(rows, p, **bad), bad
         prep = B.make_qk_prep(rot_dim=32, inv_freq=NEW)
         prep.rot_pairs = 2
@@ -87,11 +87,14 @@ def test_rows(runtime):  # noqa: F811
         # pairs behind the last that turns may name any axis; nothing turns: neither frequencies nor positions
         rows(p, axis=[0] * 16 + [7])
         rows(p, rot_dim=0, inv_freq=None, pos=None)
-        # one row: a work-group for each of the 8 + 2 + 2 heads; many: 16 rows a work-group, all heads
-        assert launched(lambda: rows(p, n=1))[0][1] == (1, 12, 1)
+        # one row: a work-group for each of the 8 + 2 + 2 heads; rounds of 1024 work-groups: 16 rows each, all heads; the rows
+        # behind them dealt out again
+        assert launched(lambda: rows(p, n=1))[0][1] == (12, 1, 1)
         assert launched(lambda: rows(p, n=16 * 1024))[0][1] == (1024, 1, 1)
-        assert launched(lambda: rows(p, n=16 * 1024 + 1))[0][1] == (1025, 1, 1)
-        assert launched(lambda: rows(p, n=16 * 300))[0][1] == (300, 4, 1)
+        assert launched(lambda: rows(p, n=16 * 1024 + 1))[0][1] == (1024 + 12, 1, 1)
+        assert launched(lambda: rows(p, n=16 * (2048 + 300)))[0][1] == (2048 + 4 * 300, 1, 1)
+        assert launched(lambda: rows(p, n=16 * 300))[0][1] == (4 * 300, 1, 1)
+        assert launched(lambda: rows(p, n=1 << 27))[0][1] == (1 << 23, 1, 1)
         for kv, d in ((B.F32, 32), (B.F32, 256), (B.BF16, 96), (B.FP8, 128)):
             assert "append_qkv_kernel" in names(lambda: rows(make_pool(kv_dtype=kv, head_dim=d)))[0]
         assert refused(rows, make_pool(kv_dtype=B.F32), qs=1026)
@@ -108,7 +111,7 @@ def test_shared(runtime):  # noqa: F811
                     dict(offsets=None), dict(bt=TABLE, stride=0), dict(np_=-1), dict(np_=5), dict(start=None), dict(plen=None),
                     dict(poff=None)):
             assert refused(shared, p, **bad), bad
-        for kw in (dict(kv_dtype=B.F32), dict(head_dim=96), dict(decode_kernel=B.KERNEL_VALU)):
+        for kw in (dict(kv_dtype=B.F32), dict(head_dim=96), dict(decode_kernel=B.KERNEL_VALU), dict(sm_scale=-0.1)):
             assert refused(shared, make_pool(**kw)), kw
         assert launched(lambda: shared(p, n=0)) == []
         names_of = names(lambda: shared(p))
