@@ -556,9 +556,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
             }
           }
         };
-        // Pair pr: its weights (vector instructions) beside the scores of the pair behind it (matrix instructions), then P V.  One
-        // wave's halves overlap by themselves: with scores, weights and P V one after the other a SIMD's two waves needed
-        // 2667 cycles for a pair each.
+        // Pair pr: its weights (vector instructions) beside the scores of the pair behind it (matrix instructions), then P V.
         auto compute = [&](float4v (&x)[CT][2], float4v (&ahead)[CT][2], int pr) {
           // LDS first: K of the pair behind this one and V of this one are on their way while the references are looked at
           bf16x8 k0[NS], k1[NS], av[DT];
