@@ -125,6 +125,7 @@ int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma
   a.Hkv = c.n_kv_heads;
   a.D = c.head_dim;
   a.rot_dim = prep->rot_dim;
+  a.n_axes = prep->n_axes;
   a.adjacent = prep->rot_pairs == ODMA_ROT_ADJACENT;
   const int group = c.head_dim <= 32 ? 4 : c.head_dim <= 64 ? 8 : c.head_dim <= 128 ? 16 : 32;
   // Beyond an XCD's L2, queries leave past the caches and leave those to the keys and values, if a wave's store fills what it

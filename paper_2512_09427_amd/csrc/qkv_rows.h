@@ -38,7 +38,8 @@ struct QkvArgs {
   int32_t whole, rest, heads_per_wg;       // tiles of 16 rows that a work-group takes whole; others, of which it takes some heads
   uint32_t rest_inverse;                   // 2^32 / rest, upwards (0: rest is 1)
   int32_t stream_q;                        // the queries are more than a cache keeps: they leave past it
-  uint8_t axis[ODMA_MAX_ROT_PAIRS];
+  int32_t n_axes;
+  alignas(4) uint8_t axis[ODMA_MAX_ROT_PAIRS];
 };
 
 // four channels as they lie in memory, and as numbers
@@ -170,46 +171,56 @@ __global__ __launch_bounds__(256) void append_qkv_kernel(QkvArgs a) {
       }
   };
 
-  // ---- one round of loads: the first batch, slots, positions, frequencies, weights (of rows without a slot too)
+  // ---- one round of loads: the first batch, slots, positions, frequencies, weights (of rows without a slot too).  None waits for
+  // another: a row's positions on all axes are loaded beside the axes of the lane's pairs.
   Four next[NB][RP][2];
   Batch bt = batch_at(h0);
   load(next, bt);
   int64_t slot16 = ODMA_SLOT_NONE;
   if (lane < BLK && row0 + lane < a.n_rows) slot16 = a.row_slot[row0 + lane];
+  const bool angles = turned && bt.kind < 2;
+  int on_axis[RP][ODMA_MAX_AXES];
+  float4v freq = {0.f, 0.f, 0.f, 0.f};
+  unsigned axes = 0;                                         // of the lane's four pairs, a byte each
+  if (angles) {
+    if (a.n_axes > 1) axes = *(const unsigned*)(a.axis + 4 * u);
+    freq = float4v{a.inv_freq[4 * u], a.inv_freq[4 * u + 1], a.inv_freq[4 * u + 2], a.inv_freq[4 * u + 3]};
+  }
+#pragma unroll
+  for (int rp = 0; rp < RP; ++rp)
+#pragma unroll
+    for (int ax = 0; ax < ODMA_MAX_AXES; ++ax) on_axis[rp][ax] = ax < a.n_axes && angles && there[rp] ? a.positions[ax * a.n_rows + row[rp]] : 0;
+  Four wq4[2], wk4[2];
+  const bool norm_q = a.q_weight != nullptr, norm_k = a.k_weight != nullptr;
+  wq4[0] = wq4[1] = wk4[0] = wk4[1] = Four{};
+  if (in_head && norm_q) {
+    wq4[0] = take4((const T*)a.q_weight + ca);
+    wq4[1] = take4((const T*)a.q_weight + cb);
+  }
+  if (in_head && norm_k) {
+    wk4[0] = take4((const T*)a.k_weight + ca);
+    wk4[1] = take4((const T*)a.k_weight + cb);
+  }
+  __builtin_amdgcn_sched_barrier(0);
   float cs[RP][4], sn[RP][4];
-  {
-    const bool angles = turned && bt.kind < 2;
-    int pos[RP][4];
-    float freq[4];
+#pragma unroll
+  for (int rp = 0; rp < RP; ++rp)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      freq[e] = angles ? a.inv_freq[4 * u + e] : 0.f;
-#pragma unroll
-      for (int rp = 0; rp < RP; ++rp) pos[rp][e] = angles && there[rp] ? a.positions[(int64_t)a.axis[4 * u + e] * a.n_rows + row[rp]] : 0;
-    }
-#pragma unroll
-    for (int rp = 0; rp < RP; ++rp)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        cs[rp][e] = 1.f;
-        sn[rp][e] = 0.f;
-        if (angles) {
-          const double turns = (double)pos[rp][e] * ((double)freq[e] * 0.15915494309189535);
-          sincos_of_turn((float)(turns - rint(turns)), sn[rp][e], cs[rp][e]);
-        }
+      cs[rp][e] = 1.f;
+      sn[rp][e] = 0.f;
+      if (angles) {
+        const unsigned ax = axes >> 8 * e & 255;
+        const int pos = ax == 0 ? on_axis[rp][0] : ax == 1 ? on_axis[rp][1] : ax == 2 ? on_axis[rp][2] : on_axis[rp][3];
+        const double turns = (double)pos * ((double)freq[e] * 0.15915494309189535);
+        sincos_of_turn((float)(turns - rint(turns)), sn[rp][e], cs[rp][e]);
       }
-  }
+    }
   float wq[8], wk[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) wq[i] = wk[i] = 1.f;
-  if (in_head && a.q_weight) {
-    widen4(take4((const T*)a.q_weight + ca), wq);
-    widen4(take4((const T*)a.q_weight + cb), wq + 4);
-  }
-  if (in_head && a.k_weight) {
-    widen4(take4((const T*)a.k_weight + ca), wk);
-    widen4(take4((const T*)a.k_weight + cb), wk + 4);
-  }
+  widen4(wq4[0], wq);
+  widen4(wq4[1], wq + 4);
+  widen4(wk4[0], wk);
+  widen4(wk4[1], wk + 4);
 
   // ---- the rows' slots: every wave looks at all 16.  A quad is four rows that fill an aligned group of four slots of a block.
   if (slot16 >= a.pool_tokens) slot16 = ODMA_SLOT_NONE;
@@ -280,7 +291,7 @@ __global__ __launch_bounds__(256) void append_qkv_kernel(QkvArgs a) {
           float x[8];
           widen4(raw[b][rp][0], x);
           widen4(raw[b][rp][1], x + 4);
-          prepare(x, wq, a.q_weight != nullptr, rp);
+          prepare(x, wq, norm_q, rp);
           if (there[rp] && hh < end) {
             T* o = (T*)a.q_out + (row[rp] * a.Hq + hh) * a.D;
             using Out = decltype(rounded4(o, x));
@@ -314,7 +325,7 @@ __global__ __launch_bounds__(256) void append_qkv_kernel(QkvArgs a) {
           float x[8];
           widen4(raw[b][rp][0], x);
           widen4(raw[b][rp][1], x + 4);
-          if (!kv) prepare(x, wk, a.k_weight != nullptr, rp);
+          if (!kv) prepare(x, wk, norm_k, rp);
           if (FP8)
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] *= kv ? a.v_inv : a.k_inv;
