@@ -129,16 +129,18 @@ int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma
   a.adjacent = prep->rot_pairs == ODMA_ROT_ADJACENT;
   const int group = c.head_dim <= 32 ? 4 : c.head_dim <= 64 ? 8 : c.head_dim <= 128 ? 16 : 32;
   // Beyond an XCD's L2, queries leave past the caches and leave those to the keys and values, if a wave's store fills what it
-  // touches (fp32 pairs in runs of four do not).  32 heads x 128 of bf16, 8 of k and v, before and after: 2 000 rows 14.0 -> 12.9 us,
+  // touches (fp32 pairs in runs of four do not).  28 / 4 heads x 128, without and with it: 2 000 rows 14.0 -> 12.9 us,
   // 8 000 34.8 -> 31.5, 65 869 246 -> 244, not rotated 32.6 -> 26.2 at 8 000; fp32 rotated in halves 64.7 -> 63.2 at 8 000, and
   // 64.7 -> 67.7 not rotated, where it would touch halves of 32 bytes.
   a.stream_q = n_rows * a.Hq * a.D * (pool->elem_bytes == 4 ? 4 : 2) > (4 << 20) && (pool->elem_bytes != 4 || (!a.adjacent && a.rot_dim == a.D));
   // Whole rounds of ROWS_WG work-groups take 16 rows with all their heads each; the rows behind them (all, where there are few) deal
-  // their heads out to a round of their own, down to one pass of a work-group.
+  // their heads out to a round of their own, in whole batches or down to one pass of a work-group (28 / 4 heads x 128, whole batches
+  // against any number of heads: 2 500 rows 14.7 -> 12.5 us, 3 000 16.8 -> 12.6, 10 000 41.9 -> 41.0).
   const int64_t tiles = (n_rows + BLK - 1) / BLK, whole = tiles / ROWS_WG * ROWS_WG, rest = tiles - whole;
-  const int heads = a.Hq + 2 * a.Hkv, pass = group < 16 ? 16 / group : 1, passes = (heads + pass - 1) / pass;
+  const int heads = a.Hq + 2 * a.Hkv, pass = rows_pass(group), batch = rows_batch(group, pool->elem_bytes), passes = (heads + pass - 1) / pass;
   const int split = rest ? (int)std::min<int64_t>(passes, (ROWS_WG + rest - 1) / rest) : 1;
   a.heads_per_wg = (passes + split - 1) / split * pass;
+  if (a.heads_per_wg > batch) a.heads_per_wg = (a.heads_per_wg + batch - 1) / batch * batch;
   a.whole = (int32_t)whole;
   const int parts = (heads + a.heads_per_wg - 1) / a.heads_per_wg;
   a.rest = (int32_t)rest;

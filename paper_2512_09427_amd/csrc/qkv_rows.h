@@ -113,15 +113,19 @@ __device__ __forceinline__ void sincos_of_turn(float f, float& sn, float& cs) {
   cs = (k + 1) & 2 ? -b : b;
 }
 
+// A work-group of 256 threads takes 16 rows of this many heads at a time (32 lanes a head: two rows a thread), and has the loads of a
+// few such passes, a batch, in flight together.
+constexpr int rows_pass(int group) { return group < 16 ? 16 / group : 1; }
+constexpr int rows_batch(int group, int elem_bytes) { return (group > 16 && elem_bytes == 4 ? 2 : 4) * rows_pass(group); }
+
 // T: rows; S: storage of the pools (T, or unsigned char for E4M3).  GROUP: lanes of a head's row, a power of two >= D / 8.
 template <typename T, typename S, int GROUP>
 __global__ __launch_bounds__(256) void append_qkv_kernel(QkvArgs a) {
   constexpr bool FP8 = sizeof(S) == 1;
   constexpr int X = 16 / (int)sizeof(S);
-  constexpr int HP = GROUP < 16 ? 16 / GROUP : 1;          // heads of a pass
+  constexpr int HP = rows_pass(GROUP);                     // heads of a pass
   constexpr int RP = GROUP > 16 ? GROUP / 16 : 1;          // rows of a thread
-  constexpr int NB = GROUP > 16 && sizeof(S) == 4 ? 2 : 4; // passes whose loads are in flight together
-  constexpr int HB = NB * HP;                              // heads of a batch
+  constexpr int HB = rows_batch(GROUP, sizeof(S)), NB = HB / HP;   // heads and passes of a batch
   constexpr int STRIDE = GROUP * 8 + X;                    // staged row, padded: 16 rows' pieces of a channel meet all banks
   __shared__ __attribute__((aligned(16))) S stage[HB * BLK * STRIDE];
   __shared__ int64_t slots[BLK];
