@@ -266,11 +266,10 @@ def make_qk_prep(*, q_weight=None, k_weight=None, eps=1e-6, rot_dim=0, adjacent=
     prep = odma_qk_prep_t()
     prep.q_weight, prep.k_weight, prep.inv_freq = _dev(q_weight), _dev(k_weight), _dev(inv_freq)
     prep.eps, prep.rot_dim, prep.rot_pairs, prep.n_axes = eps, rot_dim, ROT_ADJACENT if adjacent else ROT_HALVES, n_axes
-    axis = [] if axis is None else [int(x) for x in axis]
-    if len(axis) > MAX_ROT_PAIRS or any(x < 0 or x > 255 for x in axis):
+    axis = b"" if axis is None else bytes(int(x) for x in axis)       # (ValueError beyond 0 to 255)
+    if len(axis) > MAX_ROT_PAIRS:
         raise ValueError("axis: at most MAX_ROT_PAIRS entries of 0 to n_axes - 1")
-    for f, x in enumerate(axis):
-        prep.axis[f] = x
+    C.memmove(prep.axis, axis, len(axis))
     prep.keep = (q_weight, k_weight, inv_freq)
     return prep
 
