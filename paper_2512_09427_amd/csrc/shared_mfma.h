@@ -242,7 +242,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
   constexpr int K_STAGE = 2 * NS * 1024, STAGE_BYTES = 2 * K_STAGE;
   constexpr int CT = SHARED_CT;
   constexpr int PARTS_A = EXACT ? 3 : 1, PARTS_B = EXACT ? 3 : 2;
-  constexpr int V_AHEAD = D == 64 ? DT : EXACT ? 1 : 5;       // V operands that there are registers for in front of their weights
+  constexpr int V_AHEAD = D == 64 ? DT : EXACT ? 0 : 5;       // V operands that there are registers for in front of their weights
   constexpr float SLACK = 8.0f;                             // exponent units by which a score may exceed the reference
   __shared__ __attribute__((aligned(16))) char stage_mem[2 * STAGE_BYTES];
   __shared__ SharedPlan plan;
