@@ -37,7 +37,7 @@ class Server:
         rc, _, off, _, _ = self.pool.odma_assign(np.arange(self.n), np.full(self.n, 200))
         assert rc == 0
         self.off = torch.tensor(off, device=DEV)
-        self.pre = torch.tensor([2048, 3072], dtype=torch.int64, device=DEV)     # (prefix slabs: the rest of the arena is the caller's)
+        self.pre = torch.tensor([2048, 2592], dtype=torch.int64, device=DEV)     # (prefix slabs: the rest of the arena is the caller's)
         self.start = torch.tensor([0, 3, 5], dtype=torch.int32, device=DEV)
         self.plen = torch.tensor(PREFIX, dtype=torch.int32, device=DEV)
         self.wq, self.wk = ((1 + 0.2 * torch.randn(D, generator=gen, device=DEV)).bfloat16() for _ in range(2))
@@ -163,3 +163,41 @@ def test_prompts_and_steps_behind_shared_prefixes(kvd, paged):
         if dense and i == 2:
             lengths[5] = 0                                        # the last place empties: the other rows stay where they are
             at[5] = 0
+
+
+def test_slabs_past_32_bits():
+    """The same batch in slabs at the beginning of a pool and behind 4 GiB of one head's rows: the same results, bit for bit."""
+    n, own, shared = 3, [40, 1, 77], 160
+    tokens = (1 << 24) + 65536
+    pools = [torch.zeros((tokens + 256) * D, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    args = dict(n_layers=1, n_q_heads=4, n_kv_heads=1, head_dim=D, kv_dtype=B.BF16, out_dtype=B.F32, main_tokens=tokens, safety_tokens=256,
+                large_cap=256, boundaries=(256,), quantiles=((1, 2),), max_requests=4)
+    ws = torch.empty(B.odma_workspace_bytes(B.make_config(**args)[0]), dtype=torch.uint8, device=DEV)
+    pool = B.Pool(*B.make_config(**args, k_pool=pools[0], v_pool=pools[1], workspace=ws))
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    i32, i64 = dict(dtype=torch.int32, device=DEV), dict(dtype=torch.int64, device=DEV)
+    start, plen = torch.tensor([0, 3], **i32), torch.tensor([shared + 5], **i32)
+    lengths, new = torch.tensor([shared + o for o in own], **i32), torch.tensor(own, **i32)
+    total = sum(own)
+    qkv = torch.randn(shared + total, 6 * D, generator=gen, device=DEV).bfloat16()
+    prep = B.make_qk_prep(rot_dim=D, inv_freq=(10000.0 ** (-torch.arange(0, D, 2, device=DEV) / D)).float())
+    results = []
+    for base in (0, (1 << 24) + 4096):
+        pre = torch.tensor([base + 512], **i64)
+        off = torch.tensor([base, base + 1024, base + 2048], **i64)
+        pos, slot = torch.empty(total, **i32), torch.empty(total, **i64)
+        table = torch.empty(n, 16, **i32)
+        pool.odma_build_tables(n, lengths, new, off, 1, start, pre, plen, table, 16, total, None, pos, slot)
+        assert slot.tolist() == [base + o + j for o, c in zip((0, 1024, 2048), own) for j in range(c)]
+        t = torch.arange(shared, **i32)
+        q = torch.empty(shared + total, 4, D, dtype=torch.bfloat16, device=DEV)
+        for rows, s, p in ((slice(0, shared), pre + t, t), (slice(shared, None), slot, pos)):
+            x = qkv[rows]
+            pool.odma_append_qkv(0, x.shape[0], prep, x, 6 * D, x[:, 4 * D:], 6 * D, x[:, 5 * D:], 6 * D, s, p, q[rows])
+        for bt in (None, table):
+            out = torch.empty(n, 4, D, device=DEV)
+            pool.odma_decode_attention_shared(0, n, q[:n].contiguous(), 1, start, pre, plen, off, lengths, bt, 0 if bt is None else 16, out)
+            results.append(out)
+    for other in results[1:]:
+        assert torch.equal(other, results[0])
+    assert torch.isfinite(results[0]).all() and results[0].abs().max() > 0

@@ -99,8 +99,9 @@ class Batch:
 
     def check(self, got, ref, size, scores=4.0):
         # A weight is off by the fp32 sum of its score (128 terms of size up to |score|: 2^-20 of it) and by the exponential (2^-22).
-        # The parts of a weight keep 2^-16; results in bf16 let the weights of shared tokens be one bf16 number (2^-8).
-        weight = 2.0 ** -16 + scores * 2.0 ** -19 + (2.0 ** -8 if self.out == B.BF16 else 0.0)
+        # fp32 results keep all bits of a weight; results in bf16 let the weights of shared tokens be one bf16 number (2^-8), of own
+        # ones two (2^-16).  States are joined by factors that are off by an exponential (2^-22) each.
+        weight = 2.0 ** -21 + scores * 2.0 ** -19 + (2.0 ** -8 + 2.0 ** -16 if self.out == B.BF16 else 0.0)
         bound = weight * size + (2.0 ** -8 if self.out == B.BF16 else 2.0 ** -23) * np.abs(ref) + 1e-30
         err = np.abs(got.astype(np.float64) - ref)
         assert np.isfinite(got).all() and (err <= bound).all(), (err / bound).max()
