@@ -13,6 +13,10 @@ namespace {
 // Heads of the batch beyond which a wave of the merge takes four: more waves than that are not on the chip at once.  512 requests x 28
 // heads behind 200 tokens 52.1 -> 47.5 us, 256 x 28 96.2 either way; below it costs (16 x 28 behind 16 384 29.5 -> 38.5).
 constexpr int64_t SHARED_MANY = 8192;
+// Heads up to which four waves share a head's pieces, of which there are most where few heads share the chip: 2 requests x 5 heads
+// behind 30 623 tokens 25.2 -> 16.8 us, 1 x 28 behind 4096 15.5 -> 13.7, 1 x 1 with 30 000 of its own 29.4 -> 17.2, 4 x 28 behind 300 13.0 ->
+// 13.1; above it costs more than it gives (16 x 28 behind 1000 15.8 -> 16.6, behind 16 384 25.6 -> 24.4).
+constexpr int64_t SHARED_FEW = 128;
 }  // namespace
 
 extern "C" {
@@ -86,10 +90,12 @@ int odma_decode_attention_shared(odma_pool_t* pool, int32_t layer, int32_t n, co
   hipLaunchKernelGGL(kernels[fmt][block_table != nullptr][!a.out_bf16], dim3(a.workers), dim3(SHARED_THREADS), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(where, e);
-  const bool many = (int64_t)n * a.Hq > SHARED_MANY;
-  static void (*const merges[2][2])(SharedArgs) = {{shared_merge_kernel<128, 1>, shared_merge_kernel<128, 4>}, {shared_merge_kernel<64, 1>, shared_merge_kernel<64, 4>}};
-  const int64_t waves = (int64_t)n * a.Hkv * (many ? (a.G + 3) / 4 : a.G);
-  hipLaunchKernelGGL(merges[c.head_dim == 64][many], dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a);
+  const int64_t rows = (int64_t)n * a.Hq;
+  const int kind = rows > SHARED_MANY ? 2 : rows <= SHARED_FEW ? 0 : 1;
+  static void (*const merges[2][3])(SharedArgs) = {{shared_merge_kernel<128, 1, 4>, shared_merge_kernel<128, 1, 1>, shared_merge_kernel<128, 4, 1>},
+                                                   {shared_merge_kernel<64, 1, 4>, shared_merge_kernel<64, 1, 1>, shared_merge_kernel<64, 4, 1>}};
+  const int64_t waves = (int64_t)n * a.Hkv * (kind == 2 ? (a.G + 3) / 4 : a.G);
+  hipLaunchKernelGGL(merges[c.head_dim == 64][kind], dim3((unsigned)(kind == 0 ? waves : (waves + 3) / 4)), dim3(256), 0, s, a);
   e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(where, e);
   return ODMA_OK;

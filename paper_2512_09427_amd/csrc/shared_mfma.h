@@ -797,11 +797,14 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
 // piece i (64 a round); the outputs of the first ROUND are requested beside all references and sums, in one round trip.  Bound
 // by its chain of round trips (record, states) and, where there are many, by the states' bytes.  A head's columns lie behind one another
 // in all pieces (a column block that is not the last is whole).
-template <int D, int HEADS>
+// Where a prefix is long beside few heads, WAVES = 4 waves of a work-group take a quarter of the pieces each.
+template <int D, int HEADS, int WAVES>
 __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
+  static_assert(HEADS == 1 || WAVES == 1, "a wave per head hands its state on");
+  __shared__ float4 handed[WAVES > 1 ? WAVES - 1 : 1][64];   // reference, sum, two channels of each lane
   constexpr int ROUND = 16 / HEADS < 4 ? 4 : 16 / HEADS;
   const int lane = threadIdx.x & 63;
-  const int id = rfl(blockIdx.x * 4 + (threadIdx.x >> 6)), parts = (a.G + HEADS - 1) / HEADS;   // waves of a KV head
+  const int wave = rfl(threadIdx.x >> 6), id = WAVES > 1 ? (int)blockIdx.x : rfl(blockIdx.x * 4 + wave), parts = (a.G + HEADS - 1) / HEADS;   // waves of a KV head
   const int rg = rfl(small_quotient(id, parts)), r = rfl(small_quotient(rg, a.Hkv)), g = rg - r * a.Hkv, h0 = (id - rg * parts) * HEADS;
   if (r >= a.n) return;
   const SharedRecord rec = a.rec[r];
@@ -811,6 +814,7 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
   const int s = rec.b_pos + g * (rec.b_units + SHARED_B_EXTRA), w0 = rec.b_units ? rfl(line.holder(s)) : 0;
   const int n_b = rec.b_units ? rfl(line.holder(s + (rec.b_units > 1 ? SHARED_B_EXTRA + rec.b_units - 1 : 0))) - w0 + 1 : 0;
   const int n = rfl(rec.a_chunks + n_b);
+  const int share = WAVES > 1 ? (n + WAVES - 1) / WAVES : n, begin = WAVES > 1 ? min(wave * share, n) : 0, end = min(begin + share, n);
   const int a_stride = rec.a_blocks * a.cut_cols, a_cut = (int)shared_cut_a(a, rec.a_extra + g * (rec.a_chunks - 1) * rec.a_blocks) + rec.a_col + h0;
   const bool lane_has = 2 * lane < D;
   const unsigned lane_at = lane_has ? lane * 8u : 0u;        // (columns of the workspace fit 23 bits, their bytes 32)
@@ -822,14 +826,14 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
     l[h] = 0.f;
     o[h] = make_float2(0.f, 0.f);
   }
-  for (int i0 = 0; i0 < n; i0 += 64) {
+  for (int i0 = begin; i0 < end; i0 += 64) {
     // lane i: piece i0 + i, line A's first
-    const int i = i0 + lane, here = min(64, n - i0);
+    const int i = i0 + lane, here = min(64, end - i0);
     const bool on_a = i < rec.a_chunks;
     const int j = on_a ? i : i - rec.a_chunks, w = w0 + j;    // chunk; or wave, by its distance from the first
     int c = j == 0 ? (int)shared_first(a, on_a ? 0 : 1, r, g * a.G + h0) : on_a ? a_cut + (j - 1) * a_stride : (int)shared_cut_b(a, w) + h0;
     // (a share shorter than an item's start may hold none of its units)
-    const bool has = i < n && (on_a || j == 0 || units_before(line.start(w), s, rec.b_units) < units_before(line.start(w + 1), s, rec.b_units));
+    const bool has = i < end && (on_a || j == 0 || units_before(line.start(w), s, rec.b_units) < units_before(line.start(w + 1), s, rec.b_units));
     if (!has) c = 0;
     float2 ml[HEADS], x[HEADS][ROUND];
 #pragma unroll
@@ -865,6 +869,20 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
         }
       if ((k0 += ROUND) >= here) break;
       load(k0);
+    }
+  }
+  if (WAVES > 1) {
+    if (wave) handed[wave - 1][lane] = make_float4(m[0], l[0], o[0].x, o[0].y);
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int w = 0; w < WAVES - 1; ++w) {
+      const float4 x = handed[w][lane];
+      const float m_new = fmaxf(m[0], x.x), f = joined(m[0], m_new), g = joined(x.x, m_new);
+      m[0] = m_new;
+      l[0] = l[0] * f + x.y * g;
+      o[0].x = o[0].x * f + x.z * g;
+      o[0].y = o[0].y * f + x.w * g;
     }
   }
   if (lane_has)

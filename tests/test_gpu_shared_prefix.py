@@ -156,6 +156,14 @@ def test_long_prefixes_are_cut(kvd, d, out, paged):
     Batch([9000, 9500, 16000, 9100, 8999, 7000], [(0, 5, 9003)], kvd=kvd, d=d, hq=8, hkv=2, out=out, paged=paged).run()
 
 
+@pytest.mark.parametrize("out", [B.F32, B.BF16])
+@pytest.mark.parametrize("kvd,d", FORMATS)
+@pytest.mark.parametrize("hq,hkv,lengths,prefix", [(1, 1, [30000], 9000), (1, 1, [20003, 4, 0], 20000), (5, 1, [20, 30001], 30623), (28, 4, [9000, 9500, 16000, 9100, 8999, 7000], 9003)])
+def test_many_pieces_of_few_heads(hq, hkv, lengths, prefix, kvd, d, out):
+    """Prefixes and own tokens cut into hundreds of pieces, for as few heads as four waves join each, and for more."""
+    Batch(lengths, [(0, len(lengths), prefix)], kvd=kvd, d=d, hq=hq, hkv=hkv, out=out, seed=hq).run()
+
+
 @pytest.mark.parametrize("n,hq,hkv,prefixes", [(300, 28, 4, 3), (1024, 4, 2, 1), (1024, 2, 1, 1024), (777, 16, 1, 50), (1000, 1, 1, 2)])
 def test_many_requests(n, hq, hkv, prefixes):
     rng = np.random.default_rng(n)
