@@ -10,8 +10,8 @@
 #include "device_common.h"
 
 namespace {
-// Heads of the batch beyond which a wave of the merge takes four: more waves than that are not on the chip at once.  512 requests x 28
-// heads behind 200 tokens 52.1 -> 47.5 us, 256 x 28 96.2 either way; below it costs (16 x 28 behind 16 384 29.5 -> 38.5).
+// Heads of the batch beyond which a wave of the merge takes four: more waves than that are not on the chip at once.  1000 requests x 28
+// heads behind 100 tokens 50.6 -> 46.5 us, 512 behind 200 47.9 -> 46.0; below it costs (128 x 28 behind 2048 38.0 -> 40.1).
 constexpr int64_t SHARED_MANY = 8192;
 // Heads up to which four waves share a head's pieces, of which there are most where few heads share the chip: 2 requests x 5 heads
 // behind 30 623 tokens 25.2 -> 16.8 us, 1 x 28 behind 4096 15.5 -> 13.7, 1 x 1 with 30 000 of its own 29.4 -> 17.2, 4 x 28 behind 300 13.0 ->
