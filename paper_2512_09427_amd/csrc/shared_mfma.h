@@ -801,7 +801,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
 template <int D, int HEADS, int WAVES>
 __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
   static_assert(HEADS == 1 || WAVES == 1, "a wave per head hands its state on");
-  __shared__ float4 handed[WAVES > 1 ? WAVES - 1 : 1][64];   // reference, sum, two channels of each lane
+  __shared__ float4 handed[WAVES][64];                       // reference, sum, two channels of each lane
   constexpr int ROUND = HEADS == 1 ? 8 : 4;                  // (16: 256 requests behind 500 tokens 52.2 -> 54.4 us, 4: 16 behind 16 384 25.6 -> 28.0)
   const int lane = threadIdx.x & 63;
   const int wave = rfl(threadIdx.x >> 6), id = WAVES > 1 ? (int)blockIdx.x : rfl(blockIdx.x * 4 + wave), parts = (a.G + HEADS - 1) / HEADS;   // waves of a KV head
@@ -872,11 +872,11 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedArgs a) {
     }
   }
   if (WAVES > 1) {
-    if (wave) handed[wave - 1][lane] = make_float4(m[0], l[0], o[0].x, o[0].y);
+    if (wave) handed[wave][lane] = make_float4(m[0], l[0], o[0].x, o[0].y);
     __syncthreads();
     if (wave) return;
 #pragma unroll
-    for (int w = 0; w < WAVES - 1; ++w) {
+    for (int w = 1; w < WAVES; ++w) {
       const float4 x = handed[w][lane];
       const float m_new = fmaxf(m[0], x.x), f = joined(m[0], m_new), g = joined(x.x, m_new);
       m[0] = m_new;
