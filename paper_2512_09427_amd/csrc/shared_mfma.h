@@ -524,10 +524,11 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) x[ct][1] = float4v{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
           }
-          float top = -INFINITY;
+          // (Each tile by itself: a lane's columns are of different requests, and a NaN of one must not hide the other's rise.)
+          bool above = false;
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) top = larger(top, largest(x[ct]));
-          if (rfl(fresh | (__builtin_amdgcn_ballot_w64(top > slack) != 0))) {
+          for (int ct = 0; ct < CT; ++ct) above |= largest(x[ct]) > slack;
+          if (rfl(fresh | (__builtin_amdgcn_ballot_w64(above) != 0))) {
             fresh = 0;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {

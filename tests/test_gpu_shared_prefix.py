@@ -313,3 +313,34 @@ def test_prefix_of_its_pool_alone_is_read():
         for r, own in enumerate((64, 36)):
             k, v = (np.concatenate([kv[layer][2][i], kv[layer][r][i][:own]]) for i in range(2))
             np.testing.assert_allclose(out[r].cpu().numpy(), oa.attend_one(q[r], k, v, 1 / math.sqrt(128)), atol=2.0 ** -13)
+
+
+def number(kvd, x):
+    """A number as K and V hold it."""
+    return wl.f32_to_e4m3_bits(np.array([x], np.float32))[0] if kvd == "fp8" else wl.f32_to_bf16_bits(np.float32(x))
+
+
+@pytest.mark.parametrize("empty", [False, True])
+@pytest.mark.parametrize("hq", [16, 8])
+@pytest.mark.parametrize("out", [B.F32, B.BF16])
+@pytest.mark.parametrize("kvd,d", FORMATS)
+def test_a_nan_query_leaves_its_neighbours_references_moving(kvd, d, out, hq, empty):
+    """Scores that climb by more exponent units than a weight has, behind 32 tokens of low ones, beside a query that is NaN: of a live
+    request, or of an empty place, whose queries nobody has to fill.  The columns of one head of requests 0 and 1 (of requests 0 and 2
+    with eight heads) are sixteen apart."""
+    def edit(b):
+        # pairs of tiles score -7 q and 7 q in turn (q / sqrt(d) x 7: 53 to 76 either way)
+        high, low = (number(kvd, x / (wl.FP8_SCALE if kvd == "fp8" else 1.0)) for x in (7.0, -7.0))
+        for k, _ in b.kv:
+            k[:, :, 0] = np.where(np.arange(len(k)) // 32 % 2, high, low)[:, None]
+        b.q[:, :, 0] = wl.f32_to_bf16_bits(np.float32(87.0))
+        b.q[0] = 0x7fff
+
+    b = Batch([0 if empty else 530, 540, 520, 533], [(0, 4, 512)], kvd=kvd, d=d, hq=hq, hkv=1, out=out, seed=d, edit=edit)
+    got = b.values(b.call(b.tensors()))
+    assert (got[0] == 0).all() if empty else np.isnan(got[0]).all()
+    b.q[0] = 0
+    ref, size = b.reference()
+    for a in (got, ref, size):
+        a[0] = 0
+    b.check(got, ref, size, scores=7 * 87 / math.sqrt(d) + 6)
