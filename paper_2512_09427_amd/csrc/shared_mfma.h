@@ -168,6 +168,13 @@ constexpr int SHARES = (int)0x80000000;
 __device__ __forceinline__ int tiles_of(int tokens) { return (int)(((int64_t)tokens + BLK - 1) / BLK); }
 __device__ __forceinline__ int column_blocks(int count, int G) { return (count * G + SHARED_COLS - 1) / SHARED_COLS; }
 
+// A score in exponent units, rounded: a product that went into the subtraction of the reference unrounded would differ from the
+// reference (the largest of these numbers) by its rounding, which is more than an exponent holds where scores are large.
+__device__ __forceinline__ float in_exponent_units(float score, float scale_log2) {
+#pragma clang fp contract(off)
+  return score * scale_log2;
+}
+
 // Factor of a state joined to another.  At least the smallest number: 0 would make an infinite sum NaN.
 __device__ __forceinline__ float joined(float m, float m_new) { return fmaxf(__builtin_amdgcn_exp2f(m - m_new), 0x1p-149f); }
 
@@ -410,7 +417,6 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
   auto largest = [&](const float4v (&x)[2]) {
     return larger(larger(larger(x[0][0], x[0][1]), larger(x[0][2], x[0][3])), larger(larger(x[1][0], x[1][1]), larger(x[1][2], x[1][3])));
   };
-  const float slack = SLACK / a.scale_log2;
 
   // ================= line A
   auto line_a = [&]() {
@@ -455,14 +461,14 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
             qreg[ct][st] = ok[ct] ? *(const bf16x8*)(qp + 32 * st) : z;
           }
         }
-        // A column's reference m, in raw scores, enters with the accumulators of its scores (minus m instead of 0); -inf: none yet.
-        // The sum of its weights is one more row of P V, with V = 1.
+        // A column's reference m is subtracted behind the products: in the accumulators of the scores, one that lies far below the next
+        // pair's scores would leave them no bits.  The sum of its weights is one more row of P V, with V = 1.
         float m[CT];
-        float4v minus_m[CT], l[CT], O[CT][DT];
+        float4v l[CT], O[CT][DT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          m[ct] = -INFINITY;
-          minus_m[ct] = l[ct] = float4v{0.f, 0.f, 0.f, 0.f};
+          m[ct] = LOWEST_REF;
+          l[ct] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) O[ct][dt] = float4v{0.f, 0.f, 0.f, 0.f};
         }
@@ -508,50 +514,43 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
 #pragma unroll
           for (int sp = 0; sp < NS; ++sp) kk[sp] = *(const bf16x8*)(st + b * NS * 1024 + sp * 1024);
         };
-        auto scores = [&](float4v (&x)[CT][2], const bf16x8 (&kk)[NS], int b) {   // less the references
+        auto scores = [&](float4v (&x)[CT][2], const bf16x8 (&kk)[NS], int b) {
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
-            float4v s4 = minus_m[ct];
+            float4v s4 = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int sp = 0; sp < NS; ++sp) s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[sp], qreg[ct][sp], s4, 0, 0, 0);
             x[ct][b] = s4;
           }
         };
-        int fresh = 1;                                        // some column of the wave has no reference
-        auto settle = [&](float4v (&x)[CT][2], int pr) {      // scores of pair pr: masked, and below the references by SLACK at most
+        auto settle = [&](float4v (&x)[CT][2], int pr) {      // scores of pair pr: masked, and above the references by SLACK at most
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[ct][b][i] = in_exponent_units(x[ct][b][i], a.scale_log2);
           if (2 * pr + 1 >= n_tiles) {
             asm volatile("");                                // (a branch: once an item, against eight selects a pair)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) x[ct][1] = float4v{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
           }
           // (Each tile by itself: a lane's columns are of different requests, and a NaN of one must not hide the other's rise.)
+          float top[CT];
           bool above = false;
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) above |= largest(x[ct]) > slack;
-          if (rfl(fresh | (__builtin_amdgcn_ballot_w64(above) != 0))) {
-            fresh = 0;
+          for (int ct = 0; ct < CT; ++ct) {
+            top[ct] = largest(x[ct]);
+            above |= top[ct] > m[ct] + SLACK;
+          }
+          if (__builtin_amdgcn_ballot_w64(above) != 0) {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-              float up = largest(x[ct]);
-              up = fmaxf(up, __shfl_xor(up, 16));
+              float up = fmaxf(top[ct], __shfl_xor(top[ct], 16));
               up = fmaxf(up, __shfl_xor(up, 32));
-              float f = 1.f;
-              if (m[ct] == -INFINITY) {
-                m[ct] = up;
-                up = up == -INFINITY ? 0.f : up;
-              } else {
-                up = fmaxf(up, 0.f);
-                m[ct] += up;
-                f = joined(0.f, up * a.scale_log2);
-              }
-              fresh |= __builtin_amdgcn_ballot_w64(m[ct] == -INFINITY) != 0;
-              const float mm = m[ct] == -INFINITY ? 0.f : -m[ct];
-              minus_m[ct] = float4v{mm, mm, mm, mm};
+              const float m_new = fmaxf(m[ct], up), f = joined(m[ct], m_new);
+              m[ct] = m_new;
               l[ct] *= f;
-#pragma unroll
-              for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[ct][b][i] -= up;
 #pragma unroll
               for (int dt = 0; dt < DT; ++dt) O[ct][dt] *= f;
             }
@@ -576,7 +575,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) weight_parts(__builtin_amdgcn_exp2f(x[ct][b][i] * a.scale_log2), w[ct], 4 * b + i);
+              for (int i = 0; i < 4; ++i) weight_parts(__builtin_amdgcn_exp2f(x[ct][b][i] - m[ct]), w[ct], 4 * b + i);
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -631,7 +630,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
         for (int ct = 0; ct < CT; ++ct) {
           if (!ok[ct]) continue;
           const int64_t c = cut >= 0 ? shared_cut_a(a, cut) + wv * 16 * CT + 16 * ct + col16 : shared_first(a, 0, row[ct], head[ct]);
-          if (g4 == 0) a.part_ml[c] = make_float2(m[ct] == -INFINITY ? LOWEST_REF : m[ct] * a.scale_log2, l[ct][0]);
+          if (g4 == 0) a.part_ml[c] = make_float2(m[ct], l[ct][0]);
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) *(float4v*)(a.part_o + c * 128 + 16 * dt + 4 * g4) = O[ct][dt];
         }

@@ -344,3 +344,25 @@ def test_a_nan_query_leaves_its_neighbours_references_moving(kvd, d, out, hq, em
     for a in (got, ref, size):
         a[0] = 0
     b.check(got, ref, size, scores=7 * 87 / math.sqrt(d) + 6)
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("low", [3e3, 1e5, 1e9])
+@pytest.mark.parametrize("out", [B.F32, B.BF16])
+@pytest.mark.parametrize("kvd,d", FORMATS)
+def test_tokens_switched_off_by_large_finite_scores(kvd, d, out, low, paged):
+    """Tokens far below the others, but finite: the first ones of a prefix, of a piece of it and of a request's own, a stretch inside,
+    a whole prefix.  The scores of those that count keep all their bits."""
+    one = number(kvd, -1.0 / (wl.FP8_SCALE if kvd == "fp8" else 1.0))
+
+    def edit(b):
+        for k, _ in b.kv:
+            k[:, :, 0] = 0
+        b.q[:, :, 0] = wl.f32_to_bf16_bits(np.float32(low))
+        for tokens in (slice(0, 32), slice(128, 192), slice(330, 400), slice(512, 544), slice(640, 641)):
+            b.kv[b.n][0][tokens, :, 0] = one
+        b.kv[b.n + 1][0][:, :, 0] = one
+        b.kv[0][0][:40, :, 0] = one
+        b.kv[1][0][33:70, :, 0] = one
+
+    Batch([868, 900, 769, 768, 160, 100], [(0, 4, 770), (4, 6, 96)], kvd=kvd, d=d, hq=8, hkv=2, out=out, paged=paged, seed=d, edit=edit).run()
