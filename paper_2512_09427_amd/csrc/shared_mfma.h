@@ -721,7 +721,8 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
 #pragma unroll
           for (int sp = 0; sp < NS; ++sp)
             s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, piece(kr[b], sp)), qreg[sp], s4, 0, 0, 0);
-          x[b] = s4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[b][i] = in_exponent_units(s4[i], a.scale_log2);
         }
         if (more) load(kr, a.k, at);
         const int t0 = 2 * pr * BLK;
@@ -733,7 +734,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
             for (int i = 0; i < 4; ++i)
               if (t0 + b * BLK + 4 * g4 + i >= cur.own) x[b][i] = -INFINITY;
         }
-        float top = largest(x) * a.scale_log2;
+        float top = largest(x);
         if (__builtin_amdgcn_ballot_w64(top > m + SLACK) != 0) {
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
@@ -749,7 +750,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][i], a.scale_log2, -m));
+            const float pv = __builtin_amdgcn_exp2f(x[b][i] - m);
             sum += pv;
             weight_parts(pv, w_parts, 4 * b + i);
           }

@@ -366,3 +366,25 @@ def test_tokens_switched_off_by_large_finite_scores(kvd, d, out, low, paged):
         b.kv[1][0][33:70, :, 0] = one
 
     Batch([868, 900, 769, 768, 160, 100], [(0, 4, 770), (4, 6, 96)], kvd=kvd, d=d, hq=8, hkv=2, out=out, paged=paged, seed=d, edit=edit).run()
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("low", [1e12, 1e30, 3e38])
+@pytest.mark.parametrize("out", [B.F32, B.BF16])
+@pytest.mark.parametrize("kvd,d", FORMATS)
+def test_scores_whose_rounding_is_more_than_an_exponent_holds(kvd, d, out, low, paged):
+    """Tokens switched off by scores near the lowest finite number, among others and alone (then all of them weigh the same)."""
+    one = number(kvd, -1.0)
+
+    def edit(b):
+        for k, _ in b.kv:
+            k[:, :, 0] = 0
+        b.q[:, :, 0] = wl.f32_to_bf16_bits(np.float32(low))
+        b.kv[b.n][0][:50, :, 0] = one
+        b.kv[b.n + 1][0][:, :, 0] = one
+        b.kv[0][0][:40, :, 0] = one
+        b.kv[1][0][33:70, :, 0] = one
+        b.kv[4][0][:, :, 0] = one
+        b.q[4][:, 1:] = 0                                                # (all its scores are the same number)
+
+    Batch([300, 370, 257, 170, 140], [(0, 3, 256), (3, 5, 96)], kvd=kvd, d=d, hq=8, hkv=2, out=out, paged=paged, seed=d, edit=edit).run()
