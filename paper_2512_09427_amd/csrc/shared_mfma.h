@@ -178,8 +178,9 @@ __device__ __forceinline__ float in_exponent_units(float score, float scale_log2
 // Factor of a state joined to another.  At least the smallest number: 0 would make an infinite sum NaN.
 __device__ __forceinline__ float joined(float m, float m_new) { return fmaxf(__builtin_amdgcn_exp2f(m - m_new), 0x1p-149f); }
 
-// A weight as N bf16 parts: all but the last cut off, the last rounded (2^-9 of it in all for N = 1, 2^-17 for 2, exact for 3).
-// None is negative, nor 0 unless the weight is: an infinite V times the parts is that infinity, as times the weight.
+// A weight as N bf16 parts: all but the last cut off, the last rounded (2^-9 of it in all for N = 1, 2^-17 for 2, exact for 3, but
+// for a least part of 2^-126).  None is negative, nor 0 unless the weight is (a weight of less than 2^-126 is): an infinite V times the
+// parts is that infinity, as times the weight.  Beside the weights' sum, at least 1 in the end, the least parts are nothing.
 template <int N>
 __device__ __forceinline__ void weight_parts(float w, bf16x8 (&parts)[N], int at) {
   float rest = w;
@@ -187,7 +188,7 @@ __device__ __forceinline__ void weight_parts(float w, bf16x8 (&parts)[N], int at
   for (int k = 0; k < N - 1; ++k) {
     const unsigned bits = __float_as_uint(rest) & 0xffff0000u;
     parts[k][at] = __builtin_bit_cast(__bf16, (unsigned short)(bits >> 16));
-    rest = fmaxf(rest - __uint_as_float(bits), w * 0x1p-40f);
+    rest = fmaxf(rest - __uint_as_float(bits), fminf(w, 0x1p-126f));
   }
   parts[N - 1][at] = (__bf16)rest;
 }

@@ -388,3 +388,29 @@ def test_scores_whose_rounding_is_more_than_an_exponent_holds(kvd, d, out, low, 
         b.q[4][:, 1:] = 0                                                # (all its scores are the same number)
 
     Batch([300, 370, 257, 170, 140], [(0, 3, 256), (3, 5, 96)], kvd=kvd, d=d, hq=8, hkv=2, out=out, paged=paged, seed=d, edit=edit).run()
+
+
+@pytest.mark.parametrize("out", [B.F32, B.BF16])
+@pytest.mark.parametrize("kvd,d", [f for f in FORMATS if f[0] == "bf16"])
+def test_infinite_values_of_small_weights(kvd, d, out):
+    """A token whose weight is 2^-80 to 2^-123 of the largest one's: its infinite V is an infinite result, of shared and of own tokens."""
+    def edit(b):
+        for k, _ in b.kv:
+            k[:, :, 0] = 0
+        b.q[:, :, 0] = wl.f32_to_bf16_bits(np.float32(1.0))
+        # the others score 0 +- 1 in exponent units, the small ones 80, 81, .. less
+        b.q[:, :, 1:] = wl.f32_to_bf16_bits(wl.bf16_bits_to_f32(b.q[:, :, 1:]) / 8)
+        unit = math.sqrt(d) * math.log(2.0)
+        for rows, at in ((b.kv[b.n], 200), (b.kv[1], 20)):
+            for i in range(44):
+                rows[0][at + i, :, 0] = wl.f32_to_bf16_bits(np.float32(-(80 + i) * unit))
+                rows[1][at + i, :, i] = wl.f32_to_bf16_bits(np.float32(np.inf if i % 2 else -np.inf))
+
+    b = Batch([600, 660, 601], [(0, 3, 520)], kvd=kvd, d=d, hq=4, hkv=2, out=out, seed=d, edit=edit)
+    got = b.values(b.call(b.tensors()))
+    with np.errstate(invalid="ignore"):
+        ref, size = b.reference()
+    inf = np.isinf(ref)
+    assert not np.isnan(ref).any() and inf[:, :, :44].all() and not inf[:, :, 44:].any()
+    np.testing.assert_array_equal(got[inf], ref[inf])
+    b.check(np.where(inf, 0, got), np.where(inf, 0, ref), np.where(inf, 0, size))
