@@ -424,7 +424,8 @@ int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma
  * A request shorter than what its group shares attends to its lengths[r] first tokens.  n_prefixes = 0: odma_decode_attention.
  * Matrix-core pools only (bf16 with head_dim 128 or 64, fp8), sm_scale > 0, n <= ODMA_SHARED_MAX_REQUESTS; ODMA_INVALID_ARG otherwise.
  * Partial results live in the pool's workspace: such calls must not overlap on different streams with each other, with
- * decode calls or with odma_prefill_attention on the null stream.  A plan that decode calls may reuse survives. */
+ * decode calls or with odma_prefill_attention on the null stream.  A plan that decode calls may reuse survives; with n_prefixes = 0
+ * it does not, and the next decode call plans again, whatever its flags. */
 #define ODMA_SHARED_MAX_REQUESTS 1024
 int odma_decode_attention_shared(odma_pool_t* pool, int32_t layer, int32_t n, const void* q, int32_t n_prefixes,
                                  const int32_t* prefix_start, const int64_t* prefix_offsets, const int32_t* prefix_lengths,

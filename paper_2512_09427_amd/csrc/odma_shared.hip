@@ -41,8 +41,11 @@ int odma_decode_attention_shared(odma_pool_t* pool, int32_t layer, int32_t n, co
     return refuse("invalid argument");
   if (n_prefixes < 0 || n_prefixes > n || (n_prefixes && (!prefix_start || !prefix_lengths || (!block_table && !prefix_offsets))))
     return refuse("0 to n prefixes, each with a start, an offset and a length");
-  if (n_prefixes == 0)
-    return odma_decode_attention(pool, layer, n, q, offsets, lengths, block_table, bt_stride, out, 0, stream);
+  if (n_prefixes == 0) {
+    rc = odma_decode_attention(pool, layer, n, q, offsets, lengths, block_table, bt_stride, out, 0, stream);
+    pool->plan_stamp = {};                                     // (planned for lengths that no decode call has seen: not for reuse)
+    return rc;
+  }
   if (!(c.sm_scale > 0.f)) return refuse("needs a positive softmax scale");   // (references are the largest raw scores)
   if (n > ODMA_SHARED_MAX_REQUESTS) return refuse("n exceeds ODMA_SHARED_MAX_REQUESTS");
   char* ws = (char*)c.workspace;

@@ -414,3 +414,17 @@ def test_infinite_values_of_small_weights(kvd, d, out):
     assert not np.isnan(ref).any() and inf[:, :, :44].all() and not inf[:, :, 44:].any()
     np.testing.assert_array_equal(got[inf], ref[inf])
     b.check(np.where(inf, 0, got), np.where(inf, 0, ref), np.where(inf, 0, size))
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_decode_calls_around_one_without_prefixes(paged):
+    """A call without prefixes for other lengths between decode calls that ask for their earlier plan."""
+    b = Batch([900, 40, 333, 1200], [(0, 4, 0)], hq=8, hkv=2, paged=paged)
+    where = dict(block_table=b.table) if paged else dict(offsets=b.offsets)
+    want = H.decode(b.dp, 0, b.q, b.lengths, **where)
+    t = b.tensors()
+    full, b.lengths = b.lengths, np.array([100, 40, 20, 640])
+    t["lens"].copy_(H.to_dev(b.lengths.astype(np.int32)))
+    b.check(b.values(b.call(t, prefixes=0)), *b.reference())
+    for _ in range(2):
+        np.testing.assert_array_equal(H.decode(b.dp, 0, b.q, full, flags=B.REUSE_PLAN, **where), want)

@@ -136,3 +136,24 @@ def test_shared(runtime):  # noqa: F811
         hip.fake_fail_launch(0)
         assert fails(lambda: shared(p))
     """)
+
+
+def test_a_call_without_prefixes_leaves_no_plan_to_reuse(runtime):  # noqa: F811
+    """It plans for its own lengths, in the same place: a decode call of as many requests that asks for its earlier plan plans again."""
+    go(runtime, """
+        kernel = lambda call: [hip.fake_name(i).decode() for at in [hip.fake_launches()] for _ in [call()] for i in range(at, hip.fake_launches())]
+        for paged in (False, True):
+            p = make_pool()
+            planning = kernel(lambda: decode(p, 4, paged=paged))
+            reusing = kernel(lambda: decode(p, 4, B.REUSE_PLAN, paged))
+            assert planning != reusing
+            shared(p, np_=0, start=None, poff=None, plen=None, **(dict(bt=TABLE, stride=8, offsets=None) if paged else {}))
+            assert kernel(lambda: decode(p, 4, B.REUSE_PLAN, paged)) == planning
+            assert kernel(lambda: decode(p, 4, B.REUSE_PLAN, paged)) == reusing
+            shared(p)
+            assert kernel(lambda: decode(p, 4, B.REUSE_PLAN, paged)) == reusing
+            # one that is refused or has no requests changes nothing
+            assert refused(shared, p, np_=0, q=None)
+            shared(p, np_=0, n=0)
+            assert kernel(lambda: decode(p, 4, B.REUSE_PLAN, paged)) == reusing
+    """)
