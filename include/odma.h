@@ -376,6 +376,11 @@ int odma_prefill_attention(odma_pool_t* pool, int32_t layer, int32_t n, const vo
  *   row_position DEVICE int32[max_rows] or NULL, row_slot DEVICE int64[max_rows] or NULL: for every new row, requests in order,
  *                its token index and the pool slot of its K/V (ODMA_SLOT_SHARED for a shared token); rows behind the
  *                last request's get 0 and ODMA_SLOT_NONE, rows at or past max_rows do not exist
+ * Rows are dense: request r's are row_start[r] .. row_start[r + 1] - 1, and behind a place that brings none they move up, also in a
+ * decode step, where row and request numbers part from there on.  The projections that odma_append_qkv takes have to lie by row;
+ * decode attention reads q by request.  So a step whose batch has empty places gathers q_out by row_start (request r's query is row
+ * row_start[r]), or lays slots and positions out by place before odma_append_qkv: row_slot[row_start[r]] for r, ODMA_SLOT_NONE
+ * where row_start[r + 1] == row_start[r].
  * n must not exceed max_requests; n = 0 writes nothing.  Uses no workspace: calls may overlap as far as their arrays allow. */
 int odma_build_tables(odma_pool_t* pool, int32_t n, const int32_t* lengths, const int32_t* n_new, const int64_t* offsets,
                       int32_t n_prefixes, const int32_t* prefix_start, const int64_t* prefix_offsets,
@@ -417,7 +422,8 @@ int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma
 
 /* Decode attention of a batch that shares prefixes: odma_decode_attention's result for every request's tokens, shared and
  * own, with a prefix's K/V read for all its requests together -- their queries against it are one matrix product.
- *   q, out      as for odma_decode_attention; lengths with the shared tokens (0: an empty place, zeros)
+ *   q, out      as for odma_decode_attention, by request (not by row: odma_build_tables); lengths with the shared tokens (0: an empty
+ *               place, zeros, whatever its q holds)
  *   offsets     DEVICE int64[n], slabs of the own tokens (ignored when block_table != NULL)
  *   block_table DEVICE int32[n][bt_stride] or NULL: every request's blocks, shared ones first (odma_build_tables); prefix_offsets
  *               is then ignored (NULL allowed): a prefix is read through the row of one of its requests

@@ -201,3 +201,81 @@ def test_slabs_past_32_bits():
     for other in results[1:]:
         assert torch.equal(other, results[0])
     assert torch.isfinite(results[0]).all() and results[0].abs().max() > 0
+
+
+@pytest.mark.parametrize("by_place", [False, True])
+@pytest.mark.parametrize("kvd", ["bf16", "fp8"])
+def test_places_that_empty_in_the_middle(kvd, by_place):
+    """A captured loop of decode steps in which requests end in the middle of the batch and a place is filled again.  Rows are dense: behind
+    an empty place they move up, and row_start leads from requests to rows.  Either attention's queries are gathered by it, or slots
+    and positions are laid out by place, with ODMA_SLOT_NONE for the empty ones."""
+    s = Server(kvd, False)
+    n = s.n
+    i32, i64 = dict(dtype=torch.int32, device=DEV), dict(dtype=torch.int64, device=DEV)
+    for p, length in enumerate(PREFIX):
+        t = torch.arange(length, **i32)
+        s.rows(s.project(length), t.long() + s.pre[p], t, torch.empty(length, HQ, D, dtype=torch.bfloat16, device=DEV))
+    whole = [(PREFIX[0] // 16 * 16 if r < 3 else PREFIX[1] // 16 * 16 if r < 5 else 0) for r in range(n)]
+    own, lengths = torch.tensor(OWN, **i32), torch.tensor([w + o for w, o in zip(whole, OWN)], **i32)
+    start, pos, slot = torch.empty(n + 1, **i64), torch.empty(sum(OWN), **i32), torch.empty(sum(OWN), **i64)
+    table = torch.empty(n, 48, **i32)
+    build(s, lengths, own, table, start, pos, slot)
+    s.rows(s.project(sum(OWN)), slot, pos, torch.empty(sum(OWN), HQ, D, dtype=torch.bfloat16, device=DEV))
+    pos, slot = torch.empty(n, **i32), torch.empty(n, **i64)
+    qkv, q, out = s.project(n), torch.zeros(n, HQ, D, dtype=torch.bfloat16, device=DEV), torch.empty(n, HQ, D, device=DEV)
+    place_pos, place_slot, asked = torch.empty_like(pos), torch.empty_like(slot), torch.empty_like(q)
+
+    def step():
+        lengths.add_((lengths > 0).int())
+        build(s, lengths, None, table, start, pos, slot)
+        row = start[:n].clamp(max=n - 1)
+        if by_place:
+            place_slot.copy_(torch.where(start[1:] > start[:n], slot[row], B.SLOT_NONE))
+            place_pos.copy_(pos[row])
+            s.rows(qkv, place_slot, place_pos, q)
+            asked.copy_(q)
+        else:
+            s.rows(qkv, slot, pos, q)
+            asked.copy_(q[row])
+        s.pool.odma_decode_attention_shared(0, n, asked, 2, s.start, s.pre, s.plen, s.off, lengths, None, 0, out)
+
+    kept = lengths.clone()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    lengths.copy_(kept)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    lengths.copy_(kept)
+    at = kept.tolist()
+    for i in range(7):
+        if i in (2, 3):                                           # requests 1 and 4 end, one step apart
+            at[(1, 4)[i - 2]] = 0
+        if i == 5:                                                # another one in place 1, its tokens are there already
+            at[1] = whole[1] + 9
+        lengths.copy_(torch.tensor(at, **i32))
+        qkv.copy_(s.project(n))
+        q.fill_(float("nan"))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        at = [x + (x > 0) for x in at]
+        assert lengths.tolist() == at
+        k, v = s.stored()
+        live = [r for r in range(n) if at[r] > 0]
+        assert int(start[n]) == len(live) == n - [0, 0, 1, 2, 2, 1, 1][i]
+        for r in range(n):
+            if at[r] == 0:
+                assert (out[r] == 0).all()
+                continue
+            row = r if by_place else live.index(r)
+            here = s.slots_of(r, at[r])
+            assert int((place_slot if by_place else slot)[row]) == int(here[-1])
+            want = s.queries(qkv[row:row + 1], torch.tensor([at[r] - 1], device=DEV))[0]
+            assert ((q[row].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5).all()
+            moved = qkv[row, (HQ + HKV) * D:].double().view(HKV, D)       # (values go into the pool as they are; E4M3: half a step)
+            assert ((v[here[-1]] - moved).abs() <= (2.0 ** -4 * moved.abs() + s.scale * 2.0 ** -10 if kvd == "fp8" else 0.0)).all()
+            ref, size = s.attend(q[row], here, k, v)
+            assert ((out[r].double() - ref).abs() <= 2.0 ** -14 * size + 1e-6).all(), (i, r)
