@@ -29,7 +29,8 @@ void launch_append_qkv(const QkvArgs& a, int group, dim3 grid, hipStream_t s) {
 }
 
 constexpr int TABLES_WG = 1024;   // work-groups up to which a launch is dealt out
-constexpr int ROWS_WG = 1024;     // (four a compute unit: a round of them)
+constexpr int ROWS_WG = 1024;     // (four a compute unit: a round of bf16 rows up to 128 channels and of fp8 pools; the kernels of fp32 rows and of bf16
+                                  // rows beyond 128 channels hold 134 to 144 registers, three a compute unit, and a round is 768)
 constexpr int64_t MAX_ROWS = (int64_t)1 << 27;   // (a launch has fewer than 2^32 threads)
 
 }  // namespace
@@ -133,8 +134,8 @@ int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma
   // 8 000 34.8 -> 31.5, 65 869 246 -> 244, not rotated 32.6 -> 26.2 at 8 000; fp32 rotated in halves 64.7 -> 63.2 at 8 000, and
   // 64.7 -> 67.7 not rotated, where it would touch halves of 32 bytes.
   a.stream_q = n_rows * a.Hq * a.D * (pool->elem_bytes == 4 ? 4 : 2) > (4 << 20) && (pool->elem_bytes != 4 || (!a.adjacent && a.rot_dim == a.D));
-  // Whole rounds of ROWS_WG work-groups take 16 rows with all their heads each; the rows behind them (all, where there are few) deal
-  // their heads out to a round of their own, in whole batches or down to one pass of a work-group (28 / 4 heads x 128, whole batches
+  // Multiples of ROWS_WG work-groups take 16 rows with all their heads each; the rows behind them (all, where there are few) deal
+  // their heads out to about as many again, in whole batches or down to one pass of a work-group (28 / 4 heads x 128, whole batches
   // against any number of heads: 2 500 rows 14.7 -> 12.5 us, 3 000 16.8 -> 12.6, 10 000 41.9 -> 41.0).
   const int64_t tiles = (n_rows + BLK - 1) / BLK, whole = tiles / ROWS_WG * ROWS_WG, rest = tiles - whole;
   const int heads = a.Hq + 2 * a.Hkv, pass = rows_pass(group), batch = rows_batch(group, pool->elem_bytes), passes = (heads + pass - 1) / pass;

@@ -46,7 +46,7 @@ int odma_decode_attention_shared(odma_pool_t* pool, int32_t layer, int32_t n, co
     pool->plan_stamp = {};                                     // (planned for lengths that no decode call has seen: not for reuse)
     return rc;
   }
-  if (!(c.sm_scale > 0.f)) return refuse("needs a positive softmax scale");   // (references are the largest raw scores)
+  if (!(c.sm_scale > 0.f)) return refuse("needs a positive softmax scale");
   if (n > ODMA_SHARED_MAX_REQUESTS) return refuse("n exceeds ODMA_SHARED_MAX_REQUESTS");
   char* ws = (char*)c.workspace;
   const RowArgs ra = row_args(pool, layer);

@@ -7,8 +7,8 @@
 // all in fp32 and rounded once, when the result is stored.  The angle is formed in 64 bits and reduced to a fraction of a turn
 // there: in fp32 a position of a million is off by up to 2^-4 of a radian.
 //
-// Bound by memory, each element read once and written once: 65 869 rows of 28 / 4 heads x 128 in bf16 (1.21 GB) take 239 us, 5.1
-// TB/s, where a copy of 1 GiB reaches 5.2; 20 011 rows into fp8 pools with three axes (348 MB) 77.5 us; one row 5 us, a launch
+// Bound by memory, each element read once and written once: 65 869 rows of 28 / 4 heads x 128 in bf16 (1.21 GB) take 240 us, 5.1
+// TB/s, where a copy of 1 GiB reaches 5.2; 20 011 rows into fp8 pools with three axes (349 MB) 73 us; one row 5.5 us, a launch
 // and three round trips (slots and positions, rows, stores).
 //
 // A work-group takes 16 consecutive rows, so that a run of tokens fills whole blocks, and a run of heads; GROUP lanes share a head's row, eight channels each: two runs of four that lie where the rotation pairs them, so that every
