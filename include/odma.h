@@ -434,7 +434,8 @@ int odma_append_qkv(odma_pool_t* pool, int32_t layer, int64_t n_rows, const odma
  * When it pays: where the K and V of a layer that are not read again, about (requests - 1) x S tokens of each prefix, are 100 MB or
  * more and S is 1000 or more (up to four requests: 10 000 tokens).  Below that odma_decode_attention on the tables that
  * odma_build_tables makes, with the same result but for rounding, is faster by 1 to 8 us of its 9 to 30.
- * Matrix-core pools only (bf16 with head_dim 128 or 64, fp8), sm_scale > 0, n <= ODMA_SHARED_MAX_REQUESTS; ODMA_INVALID_ARG otherwise.
+ * Matrix-core pools only (bf16 with head_dim 128 or 64, fp8), sm_scale > 0, n <= ODMA_SHARED_MAX_REQUESTS, n x n_q_heads up to 4 million and
+ * n x n_kv_heads below 2^20; ODMA_INVALID_ARG otherwise.
  * Partial results live in the pool's workspace: such calls must not overlap on different streams with each other, with
  * decode calls or with odma_prefill_attention on the null stream.  A plan that decode calls may reuse survives; with n_prefixes = 0
  * it does not, and the next decode call plans again, whatever its flags. */

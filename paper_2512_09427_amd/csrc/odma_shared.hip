@@ -85,6 +85,9 @@ int odma_decode_attention_shared(odma_pool_t* pool, int32_t layer, int32_t n, co
   const int64_t room = (columns - rec_columns - (int64_t)2 * n * a.Hq) / (a.cut_cols + SHARED_WAVES * a.G);
   a.workers = (int32_t)std::min<int64_t>(2 * (int64_t)pool->n_cu, room) / 8 * 8;
   if (a.workers < 8) return refuse("too many requests for the partial results that the workspace holds");
+  // The merge finds a state by its byte, in 32 bits, and its request by quotients below 2^20 (small_quotient).
+  if ((int64_t)2 * n * a.Hq + (int64_t)a.workers * (a.cut_cols + SHARED_WAVES * a.G) >= 1 << 23 || (int64_t)n * a.Hkv >= 1 << 20)
+    return refuse("too many heads for so many requests");
   hipStream_t s = (hipStream_t)stream;
   // [format][paged][fp32 results]
 #define ODMA_SHARED(F) {{shared_parts_kernel<F, false, false>, shared_parts_kernel<F, false, true>}, {shared_parts_kernel<F, true, false>, shared_parts_kernel<F, true, true>}}

@@ -157,3 +157,13 @@ def test_a_call_without_prefixes_leaves_no_plan_to_reuse(runtime):  # noqa: F811
             shared(p, np_=0, n=0)
             assert kernel(lambda: decode(p, 4, B.REUSE_PLAN, paged)) == reusing
     """)
+
+
+def test_more_heads_than_the_merge_counts_are_refused(runtime):  # noqa: F811
+    """The merge finds a state by a 32-bit byte address (2^23 columns of 512 bytes) and its request by quotients below 2^20."""
+    go(runtime, """
+        for n, hq, hkv in ((1024, 1024, 1024), (1024, 8192, 512), (1024, 4096, 256), (600, 2048, 2048), (512, 8192, 512)):
+            assert refused(shared, make_pool(hq=hq, hkv=hkv), n=n), (n, hq, hkv)
+        for n, hq, hkv in ((1024, 1023, 1023), (1024, 4000, 250), (512, 2047, 2047), (500, 8000, 500)):
+            shared(make_pool(hq=hq, hkv=hkv), n=n)
+    """)
