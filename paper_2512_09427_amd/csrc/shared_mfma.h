@@ -551,7 +551,8 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_parts_kernel(SharedA
             for (int ct = 0; ct < CT; ++ct) {
               float up = fmaxf(top[ct], __shfl_xor(top[ct], 16));
               up = fmaxf(up, __shfl_xor(up, 32));
-              const float m_new = fmaxf(m[ct], up), f = joined(m[ct], m_new);
+              // (A column moves for its own scores alone: its bits do not depend on its neighbours', which may be an empty place's.)
+              const float m_new = up > m[ct] + SLACK ? up : m[ct], f = m_new > m[ct] ? joined(m[ct], m_new) : 1.f;
               m[ct] = m_new;
               l[ct] *= f;
 #pragma unroll

@@ -428,3 +428,18 @@ def test_decode_calls_around_one_without_prefixes(paged):
     b.check(b.values(b.call(t, prefixes=0)), *b.reference())
     for _ in range(2):
         np.testing.assert_array_equal(H.decode(b.dp, 0, b.q, full, flags=B.REUSE_PLAN, **where), want)
+
+
+@pytest.mark.parametrize("out", [B.F32, B.BF16])
+@pytest.mark.parametrize("kvd,d", FORMATS)
+def test_what_an_empty_place_holds_changes_no_bit(kvd, d, out):
+    """Queries of an empty place inside a group are whatever their memory held: zeros, large numbers, infinities, NaN."""
+    b = Batch([700, 0, 715, 690, 0, 720], [(0, 6, 680)], kvd=kvd, d=d, hq=8, hkv=2, out=out, seed=d)
+    want = b.run()
+    held = [np.zeros_like(b.q[1])]
+    for size in (3.0, 1e3, 1e20):
+        held.append(wl.draw_values(np.random.default_rng(int(size) % 97), b.q[1].shape, size, "bf16")[0])
+    held += [np.full_like(b.q[1], 0x7f80), np.full_like(b.q[1], 0x7fff)]
+    for x in held:
+        b.q[1] = b.q[4] = x
+        np.testing.assert_array_equal(b.values(b.call(b.tensors())), want)
