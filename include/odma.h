@@ -445,6 +445,121 @@ int odma_decode_attention_shared(odma_pool_t* pool, int32_t layer, int32_t n, co
                                  const int64_t* offsets, const int32_t* lengths, const int32_t* block_table, int32_t bt_stride,
                                  void* out, void* stream);
 
+/* ---- a batch's rows around the attention ----------------------------------------------------------------------------------
+ *
+ * What a step does with its rows (odma_build_tables) beside the projections: the residual stream between two blocks, low-rank
+ * adapters beside a projection, and the scores behind the last one.  Rows are fp32 for ODMA_F32 pools, else bf16; sums, norms and
+ * softmax statistics are fp32, and every result is rounded once, when it is stored.  row_slot, where a call takes it (DEVICE
+ * int64[n_rows] or NULL), are the slots of odma_build_tables: a row with ODMA_SLOT_NONE, or a slot past the pool, is not there, nothing of
+ * it is read and its results stay as they were. */
+
+#define ODMA_GATE_NONE     0
+#define ODMA_GATE_VALUE    1     /* the block's output times the gate */
+#define ODMA_GATE_SIGMOID  2     /* times 1 / (1 + e^-gate) */
+#define ODMA_MAX_WIDTH 32768
+
+/* How odma_add_norm joins a block to the residual. */
+typedef struct odma_add_norm {
+  const void* block_weight;  /* DEVICE [width], type of the rows: the block's output is normed and weighted first; NULL: it is taken as it is */
+  const void* next_weight;   /* DEVICE [width], type of the rows: weights of the norm behind the addition; NULL: no x_out */
+  const void* gate;          /* DEVICE rows of [width], type of the rows, row i at element i * gate_stride (0: one for all rows); NULL with ODMA_GATE_NONE */
+  int64_t gate_stride;
+  int32_t gate_kind;         /* ODMA_GATE_* */
+  int32_t width;             /* channels of a row: a multiple of 8 up to ODMA_MAX_WIDTH */
+  int32_t residual_dtype;    /* of residual and residual_out: the rows' type or ODMA_F32 */
+  float   eps;               /* of both norms, finite and >= 0 */
+  float   residual_scale, block_scale;   /* finite */
+} odma_add_norm_t;
+
+/* Between two blocks, in one pass: with norm(x) = x / sqrt(mean(x^2) + eps) over a row,
+ *   b = block_weight ? norm(block) * block_weight : block,   r = residual_scale * residual + block_scale * gate * b,
+ *   residual_out = r,   x_out = norm(r) * next_weight   (of r before it is rounded).
+ * The mean of a row's squares has to be within fp32's range.
+ *   block        DEVICE rows of [width], row i at element i * block_stride, or NULL (nothing is added: in front of the first block;
+ *                then no block_weight and no gate)
+ *   residual     DEVICE rows of [width] in residual_dtype, row i at element i * residual_stride
+ *   residual_out DEVICE, laid out as residual, may be residual itself; NULL only with x_out (the residual is then not kept)
+ *   x_out        DEVICE [n_rows][width], type of the rows, may be block itself where block_stride is width; NULL with next_weight NULL
+ * Outputs are otherwise apart from each other and from every input.  Pointers and strides are multiples of 16 bytes; n_rows <= 2^22.
+ * Uses no workspace. */
+int odma_add_norm(odma_pool_t* pool, int64_t n_rows, const odma_add_norm_t* how, const void* block, int64_t block_stride,
+                  const void* residual, int64_t residual_stride, const int64_t* row_slot, void* residual_out, void* x_out,
+                  void* stream);
+
+#define ODMA_ADAPTER_NONE       (-1)
+#define ODMA_ADAPTER_ITEM_ROWS   64   /* most rows of an item */
+#define ODMA_MAX_ADAPTERS     65536
+#define ODMA_MAX_PARTS            4
+#define ODMA_MAX_RANK           256
+
+/* A batch's rows by adapter, in one launch and without the host: the lists that odma_adapt_rows reads, once a step for all layers.
+ *   adapter    DEVICE int32[n]: of every request; outside 0 .. n_adapters - 1 (ODMA_ADAPTER_NONE): none
+ *   row_start  DEVICE int64[n + 1] or NULL (one row each): request r's rows are row_start[r] .. row_start[r + 1] - 1
+ *              (odma_build_tables; it does not decrease)
+ *   row_order  DEVICE int32[max_rows]: the rows of requests with an adapter, by adapter, and by request under each; -1 behind them.
+ *              Rows past max_rows of them do not exist
+ *   items      DEVICE int32[max_items][4]: {adapter, first, count, 0}: rows row_order[first] .. row_order[first + count - 1] have that
+ *              adapter, 1 <= count <= ODMA_ADAPTER_ITEM_ROWS; or {ODMA_ADAPTER_NONE, 0, 0, 0}: an item that is empty.  Adapters
+ *              ascend; the one with d other adapters in front of it begins at item first / ODMA_ADAPTER_ITEM_ROWS + d
+ *   max_items  at least max_rows / ODMA_ADAPTER_ITEM_ROWS + min(n, n_adapters), which is always enough
+ * n must not exceed max_requests, n_adapters ODMA_MAX_ADAPTERS, max_rows 2^27; with n = 0 the lists are empty.  Uses no workspace. */
+int odma_group_adapters(odma_pool_t* pool, int32_t n, const int32_t* adapter, int32_t n_adapters, const int64_t* row_start,
+                        int64_t max_rows, int32_t* row_order, int32_t max_items, int32_t* items, void* stream);
+
+/* Low-rank adapters beside a projection, or beside up to four that read the same rows (queries, keys and values). */
+typedef struct odma_adapters {
+  const void*    down;       /* DEVICE [n_adapters][n_parts][rank][width], type of the rows */
+  const void*    up;         /* DEVICE [n_adapters][part_start[n_parts]][rank], type of the rows */
+  const float*   scale;      /* DEVICE [n_adapters] or NULL (1) */
+  const int32_t* ranks;      /* DEVICE [n_adapters] or NULL (rank): of every adapter, taken as 0 to rank and as the next multiple of 8; what
+                                lies behind it in down and up is ignored */
+  int32_t n_adapters, rank;  /* rank: a multiple of 8 up to ODMA_MAX_RANK */
+  int32_t width;             /* channels of a row of x: a multiple of 8 */
+  int32_t n_parts;           /* 1..ODMA_MAX_PARTS */
+  int32_t part_start[ODMA_MAX_PARTS + 1];   /* columns of part p: part_start[p] .. part_start[p + 1] - 1; from 0 on, multiples of 16 */
+} odma_adapters_t;
+
+/* Bytes of scratch that odma_adapt_rows needs for max_items items; 0 if it would refuse these adapters. */
+size_t odma_adapt_scratch_bytes(const odma_pool_t* pool, const odma_adapters_t* adapters, int32_t max_items);
+
+/* The adapters' products beside what the shared projection left: for every row in the lists, with its adapter a and column c of part p,
+ *   y[row, c] = base[row, c] + scale[a] * sum_k up[a, c, k] * sum_d down[a, p, k, d] * x[row, d].
+ * fp32 throughout (bf16 rows: the inner sums enter the outer ones in two bf16 parts, 16 bits), rounded once.
+ *   items, row_order   DEVICE, from odma_group_adapters (row_order for n_rows rows; entries outside 0 .. n_rows - 1 and items that name
+ *                      no adapter are skipped).  No row may be there twice
+ *   x, base, y         DEVICE rows, row i at element i * its stride.  y may be base itself (same stride), else it lies apart from x and base;
+ *                      rows of y that are in no item stay as they were.  Pointers and strides are multiples of 16 bytes
+ *   scratch            DEVICE, odma_adapt_scratch_bytes() bytes or more, 256-byte aligned, any contents; calls that may overlap need
+ *                      scratch of their own.  Uses no workspace of the pool */
+int odma_adapt_rows(odma_pool_t* pool, int64_t n_rows, const odma_adapters_t* adapters, int32_t max_items, const int32_t* items,
+                    const int32_t* row_order, const void* x, int64_t x_stride, const void* base, int64_t base_stride, void* y,
+                    int64_t y_stride, void* scratch, size_t scratch_bytes, void* stream);
+
+#define ODMA_TOKEN_NONE (-1)
+#define ODMA_MAX_ALTERNATIVES 64
+
+/* Bytes of scratch that odma_score_tokens needs for n_rows rows; 0 if it would refuse these sizes. */
+size_t odma_score_scratch_bytes(const odma_pool_t* pool, int64_t n_rows, int32_t vocab, int32_t n_top);
+
+/* What a model says of its tokens, from the logits in one pass: p = softmax(scale * logits) over the first vocab elements of a row,
+ *   logprob[i] = log p[tokens[i]],   rank[i] = how many logits are larger than tokens[i]'s,   entropy[i] = -sum p log p,
+ *   top_id[i], top_logprob[i] = the n_top largest logits' tokens, largest first, equal ones by token, and their log p.
+ * Results are fp32 and int32; any of them may be NULL.  A logit of -inf is a token that is switched off: log p is -inf, it adds nothing,
+ * and top_id names ODMA_TOKEN_NONE (with -inf) where fewer tokens are on.  A row with none on has entropy 0.  A row with a NaN or
+ * +inf has NaN for every log p and its entropy; NaN is larger than no logit and not among the largest (tokens of +inf are).  A token
+ * outside 0 .. vocab - 1 has log p -inf and rank vocab.
+ *   logits       DEVICE rows of logits_dtype (ODMA_F32 or ODMA_BF16), row i at element i * logits_stride (vocab or more; rows
+ *                may begin at any element)
+ *   scale        1 / temperature, from 2^-64 to 2^64
+ *   tokens       DEVICE int32[n_rows]; NULL only with logprob and rank NULL
+ *   top_id       DEVICE int32[n_rows][n_top]   top_logprob DEVICE float[n_rows][n_top]   0 <= n_top <= min(vocab, ODMA_MAX_ALTERNATIVES)
+ *   scratch      DEVICE, odma_score_scratch_bytes() bytes or more, 256-byte aligned, any contents; calls that may overlap need
+ *                scratch of their own.  Uses no workspace of the pool
+ * vocab <= 2^24, n_rows <= 2^22. */
+int odma_score_tokens(odma_pool_t* pool, int64_t n_rows, const void* logits, int64_t logits_stride, int32_t logits_dtype, int32_t vocab,
+                      float scale, const int32_t* tokens, const int64_t* row_slot, int32_t n_top, float* logprob, int32_t* rank,
+                      float* entropy, int32_t* top_id, float* top_logprob, void* scratch, size_t scratch_bytes, void* stream);
+
 /* Export of one request's KV in plain row-major order: k_out, v_out DEVICE
  * [length][Hkv][D] in kv_dtype.  block_row (DEVICE int32[]) selects the paged layout. */
 int odma_gather_kv(odma_pool_t* pool, int32_t layer, int64_t offset, int32_t length,

@@ -33,6 +33,11 @@ SLOT_NONE, SLOT_SHARED = -1, -2
 ROT_HALVES, ROT_ADJACENT = 0, 1
 MAX_AXES, MAX_ROT_PAIRS = 4, 128
 SHARED_MAX_REQUESTS = 1024
+GATE_NONE, GATE_VALUE, GATE_SIGMOID = 0, 1, 2
+MAX_WIDTH = 32768
+ADAPTER_NONE, ADAPTER_ITEM_ROWS = -1, 64
+MAX_ADAPTERS, MAX_PARTS, MAX_RANK = 65536, 4, 256
+TOKEN_NONE, MAX_ALTERNATIVES = -1, 64
 
 EXPORTS = [
     "odma_workspace_bytes", "odma_pool_create", "odma_pool_destroy", "odma_inflate", "odma_assign",
@@ -43,6 +48,8 @@ EXPORTS = [
     "odma_report_completions", "odma_recalibrator_drain", "odma_recalibrator_stop", "odma_migrate_batch",
     "odma_migrate_finish", "odma_prefill_attention", "odma_block_read_probe", "odma_stream_plan_ranges",
     "odma_decode_attention_static", "odma_build_tables", "odma_append_qkv", "odma_decode_attention_shared",
+    "odma_add_norm", "odma_group_adapters", "odma_adapt_scratch_bytes", "odma_adapt_rows", "odma_score_scratch_bytes",
+    "odma_score_tokens",
 ]
 
 
@@ -72,6 +79,21 @@ class odma_qk_prep_t(C.Structure):
     _fields_ = [
         ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("inv_freq", C.c_void_p), ("eps", C.c_float),
         ("rot_dim", C.c_int32), ("rot_pairs", C.c_int32), ("n_axes", C.c_int32), ("axis", C.c_uint8 * MAX_ROT_PAIRS),
+    ]
+
+
+class odma_add_norm_t(C.Structure):
+    _fields_ = [
+        ("block_weight", C.c_void_p), ("next_weight", C.c_void_p), ("gate", C.c_void_p), ("gate_stride", C.c_int64),
+        ("gate_kind", C.c_int32), ("width", C.c_int32), ("residual_dtype", C.c_int32), ("eps", C.c_float),
+        ("residual_scale", C.c_float), ("block_scale", C.c_float),
+    ]
+
+
+class odma_adapters_t(C.Structure):
+    _fields_ = [
+        ("down", C.c_void_p), ("up", C.c_void_p), ("scale", C.c_void_p), ("ranks", C.c_void_p), ("n_adapters", C.c_int32),
+        ("rank", C.c_int32), ("width", C.c_int32), ("n_parts", C.c_int32), ("part_start", C.c_int32 * (MAX_PARTS + 1)),
     ]
 
 
@@ -122,6 +144,14 @@ def _load() -> C.CDLL:
         "odma_append_qkv": (C.c_int, [vp, C.c_int32, C.c_int64, C.POINTER(odma_qk_prep_t), vp, C.c_int64, vp, C.c_int64, vp, C.c_int64,
                                       vp, vp, vp, vp]),
         "odma_decode_attention_shared": (C.c_int, [vp, C.c_int32, C.c_int32, vp, C.c_int32, vp, vp, vp, vp, vp, vp, C.c_int32, vp, vp]),
+        "odma_add_norm": (C.c_int, [vp, C.c_int64, C.POINTER(odma_add_norm_t), vp, C.c_int64, vp, C.c_int64, vp, vp, vp, vp]),
+        "odma_group_adapters": (C.c_int, [vp, C.c_int32, vp, C.c_int32, vp, C.c_int64, vp, C.c_int32, vp, vp]),
+        "odma_adapt_scratch_bytes": (C.c_size_t, [vp, C.POINTER(odma_adapters_t), C.c_int32]),
+        "odma_adapt_rows": (C.c_int, [vp, C.c_int64, C.POINTER(odma_adapters_t), C.c_int32, vp, vp, vp, C.c_int64, vp, C.c_int64, vp,
+                                      C.c_int64, vp, C.c_size_t, vp]),
+        "odma_score_scratch_bytes": (C.c_size_t, [vp, C.c_int64, C.c_int32, C.c_int32]),
+        "odma_score_tokens": (C.c_int, [vp, C.c_int64, vp, C.c_int64, C.c_int32, C.c_int32, C.c_float, vp, vp, C.c_int32, vp, vp, vp, vp,
+                                        vp, vp, C.c_size_t, vp]),
         "odma_stream_read_probe": (C.c_int, [vp, C.c_size_t, vp, vp]),
         "odma_block_read_probe": (C.c_int, [vp, vp, vp, C.c_int64, vp, vp]),
         "odma_migrate_batch": (C.c_int, [vp, C.c_int32, i32p, C.c_uint32, vp, i64p, i32p, i32p]),
@@ -176,6 +206,11 @@ def _rows(t) -> Optional[int]:
     if t.dim() and t.stride(-1) != 1:
         raise ValueError("the last dimension of a DEVICE argument must be contiguous")
     return t.data_ptr()
+
+
+def _bytes(t) -> int:
+    """Bytes of a tensor."""
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 _current_stream = None       # address of torch's current stream of the current device
@@ -272,6 +307,33 @@ def make_qk_prep(*, q_weight=None, k_weight=None, eps=1e-6, rot_dim=0, adjacent=
     C.memmove(prep.axis, axis, len(axis))
     prep.keep = (q_weight, k_weight, inv_freq)
     return prep
+
+
+def make_add_norm(*, width, block_weight=None, next_weight=None, gate=None, gate_kind=None, gate_stride=0, eps=1e-6, residual_scale=1.0,
+                  block_scale=1.0, residual_dtype=BF16):
+    """Fills an odma_add_norm_t, which keeps the tensors alive.  gate_kind: GATE_VALUE where there is a gate, if not given."""
+    how = odma_add_norm_t()
+    how.block_weight, how.next_weight, how.gate = _dev(block_weight), _dev(next_weight), _rows(gate)
+    how.gate_kind = (GATE_NONE if gate is None else GATE_VALUE) if gate_kind is None else gate_kind
+    how.gate_stride, how.width, how.residual_dtype = gate_stride, width, residual_dtype
+    how.eps, how.residual_scale, how.block_scale = eps, residual_scale, block_scale
+    how.keep = (block_weight, next_weight, gate)
+    return how
+
+
+def make_adapters(*, down, up, n_adapters, rank, width, part_cols, scale=None, ranks=None):
+    """Fills an odma_adapters_t, which keeps the tensors alive.  part_cols: the columns of every projection beside which the adapters
+    stand."""
+    part_cols = [int(c) for c in part_cols]
+    if not 1 <= len(part_cols) <= MAX_PARTS:
+        raise ValueError("1 to MAX_PARTS parts")
+    ad = odma_adapters_t()
+    ad.down, ad.up, ad.scale, ad.ranks = _dev(down), _dev(up), _dev(scale), _dev(ranks)
+    ad.n_adapters, ad.rank, ad.width, ad.n_parts = n_adapters, rank, width, len(part_cols)
+    for p, cols in enumerate(part_cols):
+        ad.part_start[p + 1] = ad.part_start[p] + cols
+    ad.keep = (down, up, scale, ranks)
+    return ad
 
 
 def odma_workspace_bytes(cfg: odma_pool_config_t) -> int:
@@ -462,6 +524,41 @@ class Pool:
         _check(lib.odma_decode_attention_shared(self._h, layer, n, _dev(q), n_prefixes, _dev(prefix_start), _dev(prefix_offsets),
                                                 _dev(prefix_lengths), _dev(offsets), _dev(lengths), _dev(block_table), bt_stride,
                                                 _dev(out), _stream(stream)))
+
+    def odma_add_norm(self, n_rows, how, block, block_stride, residual, residual_stride, row_slot, residual_out, x_out, stream=None):
+        """block and residual may be slices of wider tensors; strides are in elements between rows."""
+        _check(lib.odma_add_norm(self._h, int(n_rows), None if how is None else C.byref(how), _rows(block), int(block_stride),
+                                 _rows(residual), int(residual_stride), _dev(row_slot), _rows(residual_out), _dev(x_out), _stream(stream)))
+
+    def odma_group_adapters(self, n, adapter, n_adapters, row_start, max_rows, row_order, max_items, items, stream=None):
+        _check(lib.odma_group_adapters(self._h, n, _dev(adapter), n_adapters, _dev(row_start), int(max_rows), _dev(row_order), max_items,
+                                       _dev(items), _stream(stream)))
+
+    def odma_adapt_scratch_bytes(self, adapters, max_items) -> int:
+        n = lib.odma_adapt_scratch_bytes(self._h, None if adapters is None else C.byref(adapters), max_items)
+        if n == 0:
+            raise OdmaError(INVALID_ARG, odma_last_error())
+        return n
+
+    def odma_adapt_rows(self, n_rows, adapters, max_items, items, row_order, x, x_stride, base, base_stride, y, y_stride, scratch,
+                        stream=None):
+        """x, base and y may be slices of wider tensors; strides are in elements between rows.  scratch: a tensor."""
+        _check(lib.odma_adapt_rows(self._h, int(n_rows), None if adapters is None else C.byref(adapters), max_items, _dev(items),
+                                   _dev(row_order), _rows(x), int(x_stride), _rows(base), int(base_stride), _rows(y), int(y_stride),
+                                   _dev(scratch), _bytes(scratch), _stream(stream)))
+
+    def odma_score_scratch_bytes(self, n_rows, vocab, n_top) -> int:
+        n = lib.odma_score_scratch_bytes(self._h, int(n_rows), vocab, n_top)
+        if n == 0:
+            raise OdmaError(INVALID_ARG, odma_last_error())
+        return n
+
+    def odma_score_tokens(self, n_rows, logits, logits_stride, logits_dtype, vocab, scale, tokens, row_slot, n_top, logprob, rank, entropy,
+                          top_id, top_logprob, scratch, stream=None):
+        """logits may be a slice of a wider tensor; its stride is in elements between rows.  scratch: a tensor."""
+        _check(lib.odma_score_tokens(self._h, int(n_rows), _rows(logits), int(logits_stride), logits_dtype, vocab, scale, _dev(tokens),
+                                     _dev(row_slot), n_top, _dev(logprob), _dev(rank), _dev(entropy), _dev(top_id), _dev(top_logprob),
+                                     _dev(scratch), _bytes(scratch), _stream(stream)))
 
     def odma_gather_kv(self, layer, offset, length, block_row, k_out, v_out, stream=None):
         _check(lib.odma_gather_kv(self._h, layer, int(offset), int(length), _dev(block_row), _dev(k_out), _dev(v_out),

@@ -19,7 +19,7 @@ DEPTH_PROBE = os.path.join(HERE, "read_depth_probe")
 DEVICE_UNITS = [("odma_stream", f"odma_stream_{f}_{p}", [f"-DODMA_STREAM_FMT={f}", f"-DODMA_STREAM_PLAN={p}"])
                 for f in (0, 1, 2) for p in ("false", "true")]
 DEVICE_UNITS += [(f"odma_wide_{t}", f"odma_wide_{t}_{p}", [f"-DODMA_STREAM_PLAN={p}"]) for t in ("f32", "bf16") for p in ("false", "true")]
-DEVICE_UNITS += [(u, u, []) for u in ("odma_prefill", "odma_device", "odma_batch", "odma_shared")]
+DEVICE_UNITS += [(u, u, []) for u in ("odma_prefill", "odma_device", "odma_batch", "odma_shared", "odma_rows", "odma_score")]
 
 HIP_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17",

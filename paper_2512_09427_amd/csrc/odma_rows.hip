@@ -1,0 +1,262 @@
+// Entry points of libodma for gfx950 on a batch's rows around the attention: the residual stream (add_norm.h), rows by adapter
+// (adapter_lists.h) and adapters beside a projection (adapt_rows.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <string>
+
+#include "odma_internal.h"
+#include "kernels_common.h"
+#include "add_norm.h"
+#include "adapter_lists.h"
+#include "adapt_rows.h"
+#include "device_common.h"
+
+namespace {
+
+int refuse(const char* where, const char* why) {
+  odma::set_error(std::string(where) + ": " + why);
+  return ODMA_INVALID_ARG;
+}
+
+bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+constexpr int64_t MAX_ROWS = (int64_t)1 << 22;       // of odma_add_norm (a launch has fewer than 2^32 threads, 1024 of them a row)
+constexpr int64_t MAX_LISTED = (int64_t)1 << 27;     // rows of lists
+constexpr int64_t MAX_WG = (1 << 24) - 1;            // work-groups of 256 threads of a launch
+constexpr int LIST_WG = 1024;                    // work-groups up to which the making of lists is dealt out
+
+template <typename T, typename R, int W, int P>
+void launch_add_norm(const AddNormArgs& a, hipStream_t s) {
+  constexpr int rows = W > 4 ? 1 : 4 / W;
+  hipLaunchKernelGGL((add_norm_kernel<T, R, W, P>), dim3((unsigned)((a.n_rows + rows - 1) / rows)), dim3(W > 4 ? W * 64 : 256), 0, s, a);
+}
+
+// Waves of a row and pieces of a lane: as many waves as a row fills with one piece a lane, four pieces from 16 waves on; in calls of many
+// rows fewer waves with more pieces each, since a wave alone with its row waits for nobody.
+template <typename T, typename R>
+void launch_add_norm(const AddNormArgs& a, bool many, hipStream_t s) {
+  const int pieces = (a.width + 511) / 512;                   // of 64 lanes
+  if (many && pieces <= 4) {
+    if (pieces == 1) launch_add_norm<T, R, 1, 1>(a, s);
+    else if (pieces == 2) launch_add_norm<T, R, 1, 2>(a, s);
+    else launch_add_norm<T, R, 1, 4>(a, s);
+  } else if (many && pieces <= 16) {
+    if (pieces <= 8) launch_add_norm<T, R, 2, 4>(a, s);
+    else launch_add_norm<T, R, 4, 4>(a, s);
+  } else if (pieces == 1) launch_add_norm<T, R, 1, 1>(a, s);
+  else if (pieces == 2) launch_add_norm<T, R, 2, 1>(a, s);
+  else if (pieces <= 4) launch_add_norm<T, R, 4, 1>(a, s);
+  else if (pieces <= 8) launch_add_norm<T, R, 8, 1>(a, s);
+  else if (pieces <= 16) launch_add_norm<T, R, 16, 1>(a, s);
+  else if (pieces <= 32) launch_add_norm<T, R, 16, 2>(a, s);
+  else launch_add_norm<T, R, 16, 4>(a, s);
+}
+
+// What the adapters' launches look like, or why they are refused
+struct AdaptShape {
+  int flat, tiles, groups, splits, split_channels, chunk_columns, chunks;
+  size_t scratch;
+};
+const char* adapt_shape(const odma_adapters_t* ad, int64_t max_items, AdaptShape* shape) {
+  if (!ad || !ad->down || !ad->up) return "adapters without weights";
+  if (ad->n_adapters < 1 || ad->n_adapters > ODMA_MAX_ADAPTERS) return "1 to ODMA_MAX_ADAPTERS adapters";
+  if (ad->rank < 8 || ad->rank > ODMA_MAX_RANK || ad->rank % 8) return "the rank must be a multiple of 8 up to ODMA_MAX_RANK";
+  if (ad->width < 8 || ad->width % 8 || ad->width > ODMA_MAX_WIDTH) return "the width must be a multiple of 8 up to ODMA_MAX_WIDTH";
+  if (ad->n_parts < 1 || ad->n_parts > ODMA_MAX_PARTS) return "1 to ODMA_MAX_PARTS parts";
+  if (ad->part_start[0] != 0) return "the first part must start at column 0";
+  for (int p = 0; p < ad->n_parts; ++p)
+    if (ad->part_start[p + 1] <= ad->part_start[p] || ad->part_start[p + 1] % 16) return "parts must ascend by multiples of 16 columns";
+  if (max_items < 0) return "invalid argument";
+  if (!aligned(ad->down, 16) || !aligned(ad->up, 16)) return "weights must start on 16-byte boundaries";
+  shape->flat = ad->n_parts * ad->rank;
+  const int all = (shape->flat + 15) / 16;
+  shape->tiles = all <= 4 ? all : 4;
+  shape->groups = (all + shape->tiles - 1) / shape->tiles;
+  // Channels are cut between work-groups where items are few: 512 each at least, and no more work-groups than the chip holds a few times.
+  const int most = (ad->width + 511) / 512;
+  shape->splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 4096 / std::max<int64_t>(max_items, 1)));
+  shape->split_channels = ((ad->width + shape->splits - 1) / shape->splits + 63) / 64 * 64;
+  shape->splits = (ad->width + shape->split_channels - 1) / shape->split_channels;
+  shape->scratch = std::max<size_t>((size_t)max_items * ODMA_ADAPTER_ITEM_ROWS * shape->flat * sizeof(float) * shape->splits, 256);
+  shape->chunk_columns = 512;
+  shape->chunks = 0;
+  for (int p = 0; p < ad->n_parts; ++p) shape->chunks += (ad->part_start[p + 1] - ad->part_start[p] + shape->chunk_columns - 1) / shape->chunk_columns;
+  if ((int64_t)max_items * std::max(shape->chunks, shape->splits * shape->groups) > MAX_WG) return "too many items";
+  return nullptr;
+}
+
+template <typename T>
+void launch_adapt(const AdaptArgs& a, const AdaptShape& shape, hipStream_t s) {
+  const dim3 grid((unsigned)(shape.splits * shape.groups * a.max_items));
+  if (shape.tiles == 1) hipLaunchKernelGGL((adapt_down_kernel<T, 1>), grid, dim3(256), 0, s, a);
+  else if (shape.tiles == 2) hipLaunchKernelGGL((adapt_down_kernel<T, 2>), grid, dim3(256), 0, s, a);
+  else if (shape.tiles == 3) hipLaunchKernelGGL((adapt_down_kernel<T, 3>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((adapt_down_kernel<T, 4>), grid, dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int odma_add_norm(odma_pool_t* pool, int64_t n_rows, const odma_add_norm_t* how, const void* block, int64_t block_stride,
+                  const void* residual, int64_t residual_stride, const int64_t* row_slot, void* residual_out, void* x_out,
+                  void* stream) {
+  const char* where = "odma_add_norm";
+  int rc = device_ready(pool, where);
+  if (rc) return rc;
+  if (n_rows == 0) return ODMA_OK;
+  if (n_rows < 0 || !how || !residual || (!residual_out && !x_out)) return refuse(where, "invalid argument");
+  if (n_rows > MAX_ROWS) return refuse(where, "too many rows");
+  if (how->width < 8 || how->width % 8 || how->width > ODMA_MAX_WIDTH) return refuse(where, "the width must be a multiple of 8 up to ODMA_MAX_WIDTH");
+  const bool f32 = pool->elem_bytes == 4;
+  if (how->residual_dtype != ODMA_F32 && (f32 || how->residual_dtype != ODMA_BF16))
+    return refuse(where, "the residual has the rows' type or ODMA_F32");
+  if (!x_out != !how->next_weight) return refuse(where, "x_out and next_weight go together");
+  if (!block && (how->block_weight || how->gate)) return refuse(where, "weights or a gate without a block");
+  if (how->gate_kind < ODMA_GATE_NONE || how->gate_kind > ODMA_GATE_SIGMOID || (how->gate_kind == ODMA_GATE_NONE) != !how->gate)
+    return refuse(where, "gate and gate_kind do not go together");
+  if (!(how->eps >= 0.f) || std::isinf(how->eps)) return refuse(where, "eps must be a finite number, 0 or more");
+  if (!std::isfinite(how->residual_scale) || !std::isfinite(how->block_scale)) return refuse(where, "scales must be finite");
+  const int unit = f32 ? 4 : 8, residual_unit = how->residual_dtype == ODMA_F32 ? 4 : 8;    // elements of 16 bytes
+  if (!aligned(block, 16) || !aligned(residual, 16) || !aligned(residual_out, 16) || !aligned(x_out, 16) || !aligned(how->gate, 16) ||
+      !aligned(how->block_weight, 16) || !aligned(how->next_weight, 16) || block_stride < 0 || block_stride % unit || residual_stride < 0 ||
+      residual_stride % residual_unit || (how->gate && (how->gate_stride < 0 || how->gate_stride % unit)))
+    return refuse(where, "rows and weights must start on 16-byte boundaries");
+  if (residual_out && n_rows > 1 && residual_stride < how->width) return refuse(where, "rows of residual_out overlap");
+  AddNormArgs a;
+  a.block = block;
+  a.residual = residual;
+  a.gate = how->gate;
+  a.block_weight = how->block_weight;
+  a.next_weight = how->next_weight;
+  a.row_slot = row_slot;
+  a.residual_out = residual_out;
+  a.x_out = x_out;
+  a.n_rows = n_rows;
+  a.pool_tokens = pool->pool_blocks * BLK;
+  a.block_stride = block_stride;
+  a.residual_stride = residual_stride;
+  a.gate_stride = how->gate_stride;
+  a.eps = how->eps;
+  a.inv_width = 1.0f / (float)how->width;
+  a.residual_scale = how->residual_scale;
+  a.block_scale = how->block_scale;
+  a.width = how->width;
+  a.gate_kind = how->gate_kind;
+  hipStream_t s = (hipStream_t)stream;
+  const bool many = n_rows >= 4 * (int64_t)pool->n_cu;
+  if (f32) launch_add_norm<float, float>(a, many, s);
+  else if (how->residual_dtype == ODMA_F32) launch_add_norm<unsigned short, float>(a, many, s);
+  else launch_add_norm<unsigned short, unsigned short>(a, many, s);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(where, e);
+  return ODMA_OK;
+}
+
+int odma_group_adapters(odma_pool_t* pool, int32_t n, const int32_t* adapter, int32_t n_adapters, const int64_t* row_start,
+                        int64_t max_rows, int32_t* row_order, int32_t max_items, int32_t* items, void* stream) {
+  const char* where = "odma_group_adapters";
+  int rc = device_ready(pool, where);
+  if (rc) return rc;
+  if (n < 0 || n > pool->cfg.max_requests || (n && !adapter) || max_rows < 0 || (max_rows && !row_order) || !items || !aligned(items, 16))
+    return refuse(where, "invalid argument");
+  if (n_adapters < 1 || n_adapters > ODMA_MAX_ADAPTERS) return refuse(where, "1 to ODMA_MAX_ADAPTERS adapters");
+  if (max_rows > MAX_LISTED) return refuse(where, "too many rows");
+  if (max_items < max_rows / ODMA_ADAPTER_ITEM_ROWS + std::min(n, n_adapters)) return refuse(where, "too few items for so many rows and adapters");
+  ListArgs a;
+  a.adapter = adapter;
+  a.row_start = row_start;
+  a.row_order = row_order;
+  a.items = (int4*)items;
+  a.max_rows = max_rows;
+  a.n = n;
+  a.n_adapters = n_adapters;
+  a.max_items = max_items;
+  a.per = std::max(1, (n + LIST_WG - 1) / LIST_WG);
+  const int64_t wg = std::max(1, (n + a.per - 1) / a.per), longest = row_start ? max_rows / wg : 1;
+  const int64_t split = std::max<int64_t>(1, std::min<int64_t>((longest + 1023) / 1024, LIST_WG / wg));
+  hipLaunchKernelGGL(group_adapters_kernel, dim3((unsigned)wg, (unsigned)split), dim3(256), (size_t)(n_adapters + 31) / 32 * 4, (hipStream_t)stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(where, e);
+  return ODMA_OK;
+}
+
+size_t odma_adapt_scratch_bytes(const odma_pool_t* pool, const odma_adapters_t* adapters, int32_t max_items) {
+  const char* where = "odma_adapt_scratch_bytes";
+  AdaptShape shape;
+  const char* why = pool ? adapt_shape(adapters, max_items, &shape) : "null pool";
+  if (why) {
+    refuse(where, why);
+    return 0;
+  }
+  return shape.scratch;
+}
+
+int odma_adapt_rows(odma_pool_t* pool, int64_t n_rows, const odma_adapters_t* adapters, int32_t max_items, const int32_t* items,
+                    const int32_t* row_order, const void* x, int64_t x_stride, const void* base, int64_t base_stride, void* y,
+                    int64_t y_stride, void* scratch, size_t scratch_bytes, void* stream) {
+  const char* where = "odma_adapt_rows";
+  int rc = device_ready(pool, where);
+  if (rc) return rc;
+  if (n_rows == 0 || max_items == 0) return ODMA_OK;
+  if (n_rows < 0 || !items || !row_order || !x || !base || !y || !scratch) return refuse(where, "invalid argument");
+  if (n_rows > MAX_LISTED) return refuse(where, "too many rows");
+  AdaptShape shape;
+  const char* why = adapt_shape(adapters, max_items, &shape);
+  if (why) return refuse(where, why);
+  const int unit = pool->elem_bytes == 4 ? 4 : 8;              // elements of 16 bytes
+  if (!aligned(x, 16) || !aligned(base, 16) || !aligned(y, 16) || x_stride < 0 || x_stride % unit || base_stride < 0 || base_stride % unit ||
+      y_stride < 0 || y_stride % unit)
+    return refuse(where, "rows must start on 16-byte boundaries");
+  const int32_t cols = adapters->part_start[adapters->n_parts];
+  if (n_rows > 1 && y_stride < cols) return refuse(where, "rows of y overlap");
+  if (y == base && y_stride != base_stride) return refuse(where, "y may be base only with the same stride");
+  if (!aligned(items, 16) || !aligned(scratch, 256)) return refuse(where, "items must be 16-byte aligned, scratch 256-byte aligned");
+  if (scratch_bytes < shape.scratch) return refuse(where, "scratch smaller than odma_adapt_scratch_bytes()");
+  AdaptArgs a;
+  a.down = adapters->down;
+  a.up = adapters->up;
+  a.scale = adapters->scale;
+  a.ranks = adapters->ranks;
+  a.items = (const int4*)items;
+  a.row_order = row_order;
+  a.x = x;
+  a.base = base;
+  a.y = y;
+  a.h = (float*)scratch;
+  a.x_stride = x_stride;
+  a.base_stride = base_stride;
+  a.y_stride = y_stride;
+  a.n_rows = n_rows;
+  a.n_adapters = adapters->n_adapters;
+  a.n_parts = adapters->n_parts;
+  a.rank = adapters->rank;
+  a.width = adapters->width;
+  a.max_items = max_items;
+  a.splits = shape.splits;
+  a.split_channels = shape.split_channels;
+  a.groups = shape.groups;
+  a.chunk_columns = shape.chunk_columns;
+  a.chunks = shape.chunks;
+  for (int p = 0; p <= ODMA_MAX_PARTS; ++p) a.part_start[p] = p <= a.n_parts ? adapters->part_start[p] : cols;
+  a.part_chunk[0] = 0;
+  for (int p = 0; p < ODMA_MAX_PARTS; ++p)
+    a.part_chunk[p + 1] = a.part_chunk[p] + (a.part_start[p + 1] - a.part_start[p] + a.chunk_columns - 1) / a.chunk_columns;
+  hipStream_t s = (hipStream_t)stream;
+  const bool f32 = pool->elem_bytes == 4;
+  if (f32) launch_adapt<float>(a, shape, s);
+  else launch_adapt<unsigned short>(a, shape, s);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(where, e);
+  const dim3 grid((unsigned)(shape.chunks * max_items));
+  const size_t lds = (size_t)4 * ((a.rank + 15) / 16) * 64 * 16;
+  if (f32) hipLaunchKernelGGL((adapt_up_kernel<float>), grid, dim3(256), lds, s, a);
+  else hipLaunchKernelGGL((adapt_up_kernel<unsigned short>), grid, dim3(256), lds, s, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(where, e);
+  return ODMA_OK;
+}
+
+}  // extern "C"

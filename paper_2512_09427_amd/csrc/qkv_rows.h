@@ -20,6 +20,7 @@
 
 #include "block_index.h"
 #include "kernels_common.h"
+#include "row_pieces.h"
 
 namespace {
 
@@ -79,12 +80,6 @@ __device__ __forceinline__ void store4(unsigned char* p, const float* x) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(x[0]), e4m3_range(x[1]), 0, false);
   w = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(x[2]), e4m3_range(x[3]), w, true);
   *(int*)p = w;
-}
-
-// 1 / sqrt(v); the instruction takes denormal numbers for 0
-__device__ __forceinline__ float root_of_inverse(float v) {
-  const bool tiny = v < 0x1p-96f;
-  return __builtin_amdgcn_rsqf(tiny ? v * 0x1p96f : v) * (tiny ? 0x1p48f : 1.f);
 }
 
 // The sum over the GROUP lanes that share a head's row, in all of them: moves inside quads, halves of rows and rows (each leaves its
