@@ -550,7 +550,7 @@ size_t odma_score_scratch_bytes(const odma_pool_t* pool, int64_t n_rows, int32_t
  * outside 0 .. vocab - 1 has log p -inf and rank vocab.
  *   logits       DEVICE rows of logits_dtype (ODMA_F32 or ODMA_BF16), row i at element i * logits_stride (vocab or more; rows
  *                may begin at any element)
- *   scale        1 / temperature, from 2^-64 to 2^64
+ *   scale        1 / temperature, from 2^-24 to 2^24
  *   tokens       DEVICE int32[n_rows]; NULL only with logprob and rank NULL
  *   top_id       DEVICE int32[n_rows][n_top]   top_logprob DEVICE float[n_rows][n_top]   0 <= n_top <= min(vocab, ODMA_MAX_ALTERNATIVES)
  *   scratch      DEVICE, odma_score_scratch_bytes() bytes or more, 256-byte aligned, any contents; calls that may overlap need

@@ -10,6 +10,7 @@
 
 #include "kernels_common.h"
 #include "row_pieces.h"
+#include "wave_reduce.h"
 
 namespace {
 
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void add_norm_kernel(AddNormA
   }
   // The sum over a row's lanes, in all of them; `turn`: sums that follow one another take turns at two places
   auto row_sum = [&](float x, int turn) {
-    x = wave_sum(x);
+    x = sum_over_wave(x);
     if (W == 1) return x;
     if (lane == 0) part[turn][mine][w] = x;
     __syncthreads();

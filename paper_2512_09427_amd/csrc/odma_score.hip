@@ -18,11 +18,11 @@ int refuse(const char* where, const char* why) {
 
 constexpr int64_t MAX_ROWS = (int64_t)1 << 22;   // (a launch has fewer than 2^32 threads)
 constexpr int32_t MAX_VOCAB = 1 << 24;
-constexpr int SCORE_WG = 1024;        // work-groups up to which rows are cut into parts
-constexpr int PART_UNIT = 2048;       // elements of the shortest part: a piece or two for every thread
+constexpr int PART_UNIT = 2048;       // elements of the shortest part: a piece or two for every thread of four waves
 
+constexpr int SCORE_ROWS_8 = 512, SCORE_ROWS_16 = 256, SCORE_W = 16, SCORE_WAVES = 4096;
 struct ScoreShape {
-  int parts, part_len;
+  int waves, parts, part_len;
   size_t states, scratch;
 };
 const char* score_shape(int64_t n_rows, int32_t vocab, int32_t n_top, ScoreShape* shape) {
@@ -30,12 +30,21 @@ const char* score_shape(int64_t n_rows, int32_t vocab, int32_t n_top, ScoreShape
   if (vocab < 1 || vocab > MAX_VOCAB) return "1 to 2^24 tokens";
   if (n_top < 0 || n_top > ODMA_MAX_ALTERNATIVES || n_top > vocab) return "0 to ODMA_MAX_ALTERNATIVES alternatives, of the vocabulary";
   const int64_t units = (vocab + PART_UNIT - 1) / PART_UNIT;
-  int64_t parts = std::max<int64_t>(1, std::min<int64_t>({units, SCORE_PARTS, SCORE_WG / std::max<int64_t>(n_rows, 1)}));
+  const int64_t rows = std::max<int64_t>(n_rows, 1);
+  shape->waves = rows > SCORE_ROWS_8 ? 4 : rows > SCORE_ROWS_16 ? 8 : rows * SCORE_PARTS >= 1024 ? SCORE_W : 4;
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({units, SCORE_PARTS, SCORE_WAVES / shape->waves / rows}));
   shape->part_len = (int)((units + parts - 1) / parts * PART_UNIT);
   shape->parts = (vocab + shape->part_len - 1) / shape->part_len;
   shape->states = ((size_t)n_rows * shape->parts * sizeof(float4) + 255) / 256 * 256;
   shape->scratch = shape->parts == 1 ? 256 : std::max<size_t>(shape->states + (size_t)n_rows * shape->parts * n_top * sizeof(u64), 256);
   return nullptr;
+}
+
+template <typename T>
+void launch_score(const ScoreArgs& a, int waves, dim3 grid, hipStream_t s) {
+  if (waves == 4) hipLaunchKernelGGL((score_kernel<T, 4>), grid, dim3(256), 0, s, a);
+  else if (waves == 8) hipLaunchKernelGGL((score_kernel<T, 8>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((score_kernel<T, 16>), grid, dim3(1024), 0, s, a);
 }
 
 }  // namespace
@@ -63,7 +72,7 @@ int odma_score_tokens(odma_pool_t* pool, int64_t n_rows, const void* logits, int
   if (!logits || (logits_dtype != ODMA_F32 && logits_dtype != ODMA_BF16)) return refuse(where, "logits in ODMA_F32 or ODMA_BF16");
   if (logits_stride < 0 || (n_rows > 1 && logits_stride < vocab) || (uintptr_t)logits % (logits_dtype == ODMA_F32 ? 4 : 2))
     return refuse(where, "rows of logits overlap or are not aligned to their elements");
-  if (!(scale >= 0x1p-64f && scale <= 0x1p64f)) return refuse(where, "the scale must lie between 2^-64 and 2^64");
+  if (!(scale >= 0x1p-24f && scale <= 0x1p24f)) return refuse(where, "the scale must lie between 2^-24 and 2^24");
   if (!tokens && (logprob || rank)) return refuse(where, "logprob and rank need tokens");
   if (!logprob && !rank && !entropy && !top_id && !top_logprob) return refuse(where, "nothing to compute");
   if (n_top == 0 && (top_id || top_logprob)) return refuse(where, "alternatives without their number");
@@ -93,8 +102,8 @@ int odma_score_tokens(odma_pool_t* pool, int64_t n_rows, const void* logits, int
   a.scale_log2 = scale * 1.4426950408889634f;
   hipStream_t s = (hipStream_t)stream;
   const dim3 grid((unsigned)(n_rows * shape.parts));
-  if (a.logits_f32) hipLaunchKernelGGL((score_kernel<float>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((score_kernel<unsigned short>), grid, dim3(256), 0, s, a);
+  if (a.logits_f32) launch_score<float>(a, shape.waves, grid, s);
+  else launch_score<unsigned short>(a, shape.waves, grid, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(where, e);
   if (shape.parts > 1) {
