@@ -2,12 +2,11 @@
 //   y[row, c] = base[row, c] + s_a sum_k up[a, c, k] h[row, k],   h[row, k] = sum_d down[a, k, d] x[row, d]
 // for the rows of every item (adapter_lists.h: up to 64 rows of one adapter), two launches.
 //
-// The first forms h: ranks are the rows of the matrix product, an item's rows its columns, x and down come straight from
-// memory in operand order (16 bytes a lane of both are neighbouring channels).  The channels are cut between the waves of a
+// The first forms h: ranks are the rows of the matrix product, an item's rows its columns.  The channels are cut between the waves of a
 // work-group, which add up in LDS, and, where a batch has few items, between work-groups, whose parts stay apart in scratch: nothing is
-// added up in an order that changes.  The second stages an item's h in LDS, parts added up and scaled, and takes 64
-// columns a wave at a time: base enters as the accumulators, y leaves as 16-byte pieces.  In bf16, h enters as two bf16 parts
-// (value and rest: 16 bits), which fill the contraction of 32 that a rank of 16 would half leave empty.
+// added up in an order that changes.  The second stages an item's h in LDS, parts added up and scaled, and takes 64 columns a wave at
+// a time.  In bf16, h enters as two bf16 parts (value and rest: 16 bits), which fill the contraction of 32 that a rank of 16 would
+// half leave empty.
 //
 // Both are bound by memory: adapters that occur once are the bytes of a decode step, x, base and y those of a prompt.
 #pragma once
@@ -62,34 +61,73 @@ struct AdaptOp<float> {
   }
 };
 
+// Rows that are more than a cache keeps pass by it.
+template <bool STREAM, typename T>
+__device__ __forceinline__ uint4v taken(const T* p) {
+  return STREAM ? __builtin_nontemporal_load((const uint4v*)p) : *(const uint4v*)p;
+}
+template <bool STREAM, typename T>
+__device__ __forceinline__ void put(T* p, uint4v v) {
+  if (STREAM) __builtin_nontemporal_store(v, (uint4v*)p);
+  else *(uint4v*)p = v;
+}
+
+// Ranks of h as the second product takes them: eight in bf16, value and rest (finite numbers stay finite: the value is cut off).
+__device__ __forceinline__ void split_ranks(const float* v, uint4v& hi, uint4v& lo) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float v0 = v[2 * e], v1 = v[2 * e + 1];
+    const unsigned h0 = __float_as_uint(v0) & 0xffff0000u, h1 = __float_as_uint(v1) & 0xffff0000u;
+    const float l0 = __builtin_isinf(v0) ? 0.f : v0 - __uint_as_float(h0), l1 = __builtin_isinf(v1) ? 0.f : v1 - __uint_as_float(h1);
+    hi[e] = h0 >> 16 | h1;
+    lo[e] = float_to_bf16_bits(l0) | (unsigned)float_to_bf16_bits(l1) << 16;
+  }
+}
+
+// A lane's part of a row's 64 columns: base and what the products add, rounded.  d: eight (fp32: four) sums.
+__device__ __forceinline__ uint4v added(const unsigned short*, uint4v base, const float* d) {
+  uint4v out;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    out[e] = float_to_bf16_bits(__uint_as_float(base[e] << 16) + d[2 * e]) | (unsigned)float_to_bf16_bits(__uint_as_float(base[e] & 0xffff0000u) + d[2 * e + 1]) << 16;
+  return out;
+}
+__device__ __forceinline__ uint4v added(const float*, uint4v base, const float* d) {
+  uint4v out;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[e] = __float_as_uint(__uint_as_float(base[e]) + d[e]);
+  return out;
+}
+
 // h of an item: grid items x groups of MT tiles of 16 ranks x splits.
-template <typename T, int MT>
+//
+// A wave takes 128 bytes of the item's rows and of the ranks' at a time: lanes load them as they lie, eight neighbouring lanes a line, and
+// pass them through LDS of the wave's own, where the pieces of a row are permuted by its number so that the 16 rows of an operand meet all banks.
+template <typename T, int MT, bool STREAM>
 __global__ __launch_bounds__(256) void adapt_down_kernel(AdaptArgs a) {
   using Op = AdaptOp<T>;
-  constexpr int X = Op::X, STEP = 4 * X, STEPS = 2;          // channels of a piece and of a step of four pieces; steps that a wave takes at a time
-  __shared__ __attribute__((aligned(16))) float4v parts[4][MT][64];
+  constexpr int X = Op::X, CHUNK = 8 * X;                    // channels of a piece, of 128 bytes
+  constexpr int WAVE = (64 + MT * 16) * 8;                   // pieces of a wave in LDS: rows, then ranks
+  __shared__ __attribute__((aligned(16))) uint4v stage[4 * WAVE];
   const int at = blockIdx.x / (a.splits * a.groups), cut = (int)blockIdx.x - at * a.splits * a.groups;
   const int4 item = a.items[at];
   const int adapter = item.x, first = item.y, count = min(item.z, ODMA_ADAPTER_ITEM_ROWS);
   if (count <= 0 || (unsigned)adapter >= (unsigned)a.n_adapters) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = rfl(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const int split = cut % a.splits, group = cut / a.splits;
   const int flat = a.n_parts * a.rank, rank_a = rank_of(a, adapter);
   const int k0 = split * a.split_channels, k1 = min(k0 + a.split_channels, a.width);
-  // ranks and rows that are not there repeat the first one: what they give is not used
-  const T* arow[MT];
+  const int subtiles = (count + 15) / 16, r0 = group * MT * 16;
+  uint4v* mine = stage + wave * WAVE;
+  // the lane's line of eight, and which of its pieces it loads
+  const int line = lane >> 3, piece = (lane & 7) ^ line;
+  // ranks: eight at a time are all there or not (flat and the adapter's rank are multiples of 8); what those that are not hold is not used
+  const T* arow = (const T*)a.down + ((int64_t)adapter * flat + r0 + line) * a.width + piece * X;
+  bool there[2 * MT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int r = (group * MT + t) * 16 + m;
-    arow[t] = (const T*)a.down + ((int64_t)adapter * flat + (r < flat && r % a.rank < rank_a ? r : 0)) * a.width + g * X;
-  }
-  const int subtiles = (count + 15) / 16;
-  const T* xrow[4];
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int j = u * 16 + m;
-    const int row = j < count ? a.row_order[first + j] : -1;
-    xrow[u] = (const T*)a.x + (row >= 0 && row < a.n_rows ? row : 0) * a.x_stride + g * X;
+  for (int i = 0; i < 2 * MT; ++i) {
+    const int r = r0 + 8 * i;
+    there[i] = r < flat && r % a.rank < rank_a;
   }
   float4v acc[MT][4];
 #pragma unroll
@@ -98,169 +136,394 @@ __global__ __launch_bounds__(256) void adapt_down_kernel(AdaptArgs a) {
     for (int u = 0; u < 4; ++u) acc[t][u] = float4v{0.f, 0.f, 0.f, 0.f};
   auto run = [&](auto subs) {
     constexpr int NS = decltype(subs)::value;
-    for (int k = k0 + wave * STEPS * STEP; k < k1; k += 4 * STEPS * STEP) {
-      uint4v av[STEPS][MT], xv[STEPS][NS];
+    const T* xrow[2 * NS];                                   // rows that are not there repeat one: what they give is not used
 #pragma unroll
-      for (int c = 0; c < STEPS; ++c) {
-        const bool in = k + c * STEP + g * X < k1;           // (a width is whole pieces)
+    for (int i = 0; i < 2 * NS; ++i) {
+      const int row = a.row_order[first + min(8 * i + line, count - 1)];
+      xrow[i] = (const T*)a.x + (row >= 0 && row < a.n_rows ? row : 0) * a.x_stride + piece * X;
+    }
+    uint4v av[2 * MT], xv[2 * NS];
+    auto load = [&](int k) {
+      const bool in = k + piece * X < k1;                    // (a width is whole pieces)
 #pragma unroll
-        for (int t = 0; t < MT; ++t) av[c][t] = in ? *(const uint4v*)(arow[t] + k + c * STEP) : uint4v{0, 0, 0, 0};
-#pragma unroll
-        for (int u = 0; u < NS; ++u) xv[c][u] = in ? *(const uint4v*)(xrow[u] + k + c * STEP) : uint4v{0, 0, 0, 0};
+      for (int i = 0; i < 2 * MT; ++i) {
+        av[i] = uint4v{0, 0, 0, 0};
+        if (there[i] && in) av[i] = *(const uint4v*)(arow + (int64_t)(8 * i) * a.width + k);
       }
 #pragma unroll
-      for (int c = 0; c < STEPS; ++c)
+      for (int i = 0; i < 2 * NS; ++i) {
+        xv[i] = uint4v{0, 0, 0, 0};
+        if (in) xv[i] = taken<STREAM>(xrow[i] + k);
+      }
+    };
+    int k = k0 + wave * CHUNK;
+    if (k < k1) load(k);
+    for (; k < k1; k += 4 * CHUNK) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+      for (int i = 0; i < 2 * NS; ++i) mine[i * 64 + lane] = xv[i];
 #pragma unroll
-          for (int u = 0; u < NS; ++u) acc[t][u] = Op::mma(av[c][t], xv[c][u], acc[t][u]);
+      for (int i = 0; i < 2 * MT; ++i) mine[(8 + i) * 64 + lane] = av[i];
+      if (k + 4 * CHUNK < k1) load(k + 4 * CHUNK);           // under way while these are multiplied
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint4v b[NS];
+#pragma unroll
+        for (int u = 0; u < NS; ++u) b[u] = mine[(u * 16 + m) * 8 + ((4 * c + g) ^ (m & 7))];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          const uint4v w = mine[(64 + t * 16 + m) * 8 + ((4 * c + g) ^ (m & 7))];
+#pragma unroll
+          for (int u = 0; u < NS; ++u) acc[t][u] = Op::mma(w, b[u], acc[t][u]);
+        }
+      }
     }
   };
   if (subtiles == 1) run(std::integral_constant<int, 1>{});
   else if (subtiles == 2) run(std::integral_constant<int, 2>{});
   else run(std::integral_constant<int, 4>{});
   // ---- the waves' sums; a lane holds ranks 4 g .. 4 g + 3 of row m
+  float4v* parts = (float4v*)stage;
   float* out = a.h + ((int64_t)split * a.max_items + at) * ODMA_ADAPTER_ITEM_ROWS * flat;
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     if (u >= subtiles) break;
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < MT; ++t) parts[wave][t][lane] = acc[t][u];
+    for (int t = 0; t < MT; ++t) parts[(wave * MT + t) * 64 + lane] = acc[t][u];
     __syncthreads();
     for (int t = wave; t < MT; t += 4) {
-      const int r = (group * MT + t) * 16 + 4 * g;
+      const int r = r0 + t * 16 + 4 * g;
       if (r >= flat) continue;
-      float4v s = parts[0][t][lane] + parts[1][t][lane] + parts[2][t][lane] + parts[3][t][lane];
+      float4v s = parts[t * 64 + lane] + parts[(MT + t) * 64 + lane] + parts[(2 * MT + t) * 64 + lane] + parts[(3 * MT + t) * 64 + lane];
       if (r % a.rank >= rank_a) s = float4v{0.f, 0.f, 0.f, 0.f};
       *(float4v*)(out + (int64_t)(u * 16 + m) * flat + r) = s;
     }
   }
 }
 
-// y of an item: grid items x chunks of columns.  LDS: h in operand order, [subtile][step][group][row] pieces of 16 bytes.
-template <typename T>
+// y of an item: grid items x chunks of columns.  SW: waves that share the rows of 64 columns where an item has so many.  LDS, dynamic: h in
+// operand order, [subtile][step][group][row] pieces of 16 bytes.
+//
+// A tile of 16 rows x 64 columns leaves the accumulators through LDS of the wave's own and is added to base and stored as the rows lie,
+// eight (fp32: 16) neighbouring lanes a line.
+template <typename T, int SW, bool STREAM>
 __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
   using Op = AdaptOp<T>;
-  constexpr int X = Op::X, NB = 16 / X;                      // pieces of a lane's 16 columns
+  constexpr int X = Op::X, SUBS = 4 / SW;                    // most subtiles of a wave
+  constexpr int LINE = 64 / X, LOADS = 16 * LINE / 64;       // lanes of a row's 64 columns; loads of a subtile
   extern __shared__ __attribute__((aligned(16))) uint4v hs[];
+  __shared__ __attribute__((aligned(16))) float4v turned[4][256];
   const int at = blockIdx.x / a.chunks, chunk = (int)blockIdx.x - at * a.chunks;
   const int4 item = a.items[at];
   const int adapter = item.x, first = item.y, count = min(item.z, ODMA_ADAPTER_ITEM_ROWS);
   if (count <= 0 || (unsigned)adapter >= (unsigned)a.n_adapters) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = rfl(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const int flat = a.n_parts * a.rank, rank_a = rank_of(a, adapter);
   int part = 0;
   while (part + 1 < a.n_parts && chunk >= a.part_chunk[part + 1]) ++part;
   const int c0 = a.part_start[part] + (chunk - a.part_chunk[part]) * a.chunk_columns;
   const int c1 = min(c0 + a.chunk_columns, a.part_start[part + 1]), cols = a.part_start[a.n_parts];
-  const int subtiles = (count + 15) / 16, steps = (a.rank + 15) / 16;
-  int row[4];
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int j = u * 16 + m;
-    row[u] = j < count ? a.row_order[first + j] : -1;
-    if (row[u] >= a.n_rows) row[u] = -1;
-  }
-  // ---- h: the splits' sums, scaled
+  const int steps = (a.rank + 15) / 16, eights = steps * 2;  // (eights of ranks)
+  const int line = lane / LINE, piece = lane % LINE;
   const float scale = a.scale ? a.scale[adapter] : 1.f;
-  const int eights = steps * 2;                              // of ranks
-  for (int i = threadIdx.x; i < subtiles * 16 * eights; i += 256) {
-    const int j = i / eights, p = i - j * eights;
+  const T* up = (const T*)a.up + (int64_t)adapter * cols * a.rank;
+  float4v* turn = turned[wave];
+  // h of up to 64 rows is staged at a time, of 32 where ranks are more than 128
+  const int most_rows = steps > 8 ? 32 : 64;
+  for (int j0 = 0; j0 < count; j0 += most_rows) {
+    const int rows = min(count - j0, most_rows), subtiles = (rows + 15) / 16;
+    // this wave's subtiles and columns
+    const int sw = subtiles == 1 ? 1 : min(SW, subtiles == 3 ? 4 : subtiles), u0 = wave % sw, column_waves = 4 / sw;
+    int row[SUBS][LOADS];
+#pragma unroll
+    for (int v = 0; v < SUBS; ++v)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int j = (u0 + v * sw) * 16 + i * (64 / LINE) + line;
+        row[v][i] = j < rows ? a.row_order[first + j0 + j] : -1;
+        if (row[v][i] >= a.n_rows) row[v][i] = -1;
+      }
+    uint4v in[SUBS][LOADS];
+    auto load = [&](int cs) {
+      const int c = cs + piece * X;
+#pragma unroll
+      for (int v = 0; v < SUBS; ++v)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          if (row[v][i] >= 0 && c < c1) in[v][i] = taken<STREAM>((const T*)a.base + row[v][i] * a.base_stride + c);
+    };
+    auto weights = [&](uint4v (&av)[4], int cs, int s) {       // operand s of 64 columns
+      const int q = 4 * s + g, p = X == 8 && q >= eights ? q - eights : q;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int c = cs + t * 16 + m;
+        av[t] = uint4v{0, 0, 0, 0};
+        if (p * X < rank_a && c < c1) av[t] = *(const uint4v*)(up + (int64_t)c * a.rank + p * X);
+      }
+    };
+    int cs = c0 + wave / sw * 64;
+    uint4v av[4];
+    if (cs < c1) {                                             // under way while h is staged
+      weights(av, cs, 0);
+      load(cs);
+    }
+    // ---- h: the splits' sums, scaled
+    for (int i = threadIdx.x; i < subtiles * 16 * eights; i += 256) {
+      const int j = i / eights, p = i - j * eights;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = 0.f;
+      if (8 * p < rank_a && j < rows) {
+        const float* src = a.h + ((int64_t)at * ODMA_ADAPTER_ITEM_ROWS + j0 + j) * flat + part * a.rank + 8 * p;
+#pragma unroll 4
+        for (int s = 0; s < a.splits; ++s) {
+          const float* from = src + (int64_t)s * a.max_items * ODMA_ADAPTER_ITEM_ROWS * flat;
+          const float4v lo = *(const float4v*)from, hi = *(const float4v*)(from + 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] += lo[e];
+            v[4 + e] += hi[e];
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= scale;
+      }
+      uint4v* to = hs + (j >> 4) * steps * 64 + (j & 15);
+      if constexpr (X == 8) {                                  // value and rest
+        uint4v hi, lo;
+        split_ranks(v, hi, lo);
+        to[p * 16] = hi;
+        to[(eights + p) * 16] = lo;
+      } else {
+        to[2 * p * 16] = __builtin_bit_cast(uint4v, float4v{v[0], v[1], v[2], v[3]});
+        to[(2 * p + 1) * 16] = __builtin_bit_cast(uint4v, float4v{v[4], v[5], v[6], v[7]});
+      }
+    }
+    __syncthreads();
+    while (cs < c1) {
+      float4v acc[SUBS][4];
+#pragma unroll
+      for (int v = 0; v < SUBS; ++v)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[v][t] = float4v{0.f, 0.f, 0.f, 0.f};
+      for (int s = 0; s < steps; ++s) {
+        if (s > 0) weights(av, cs, s);
+#pragma unroll
+        for (int v = 0; v < SUBS; ++v) {
+          if (u0 + v * sw >= subtiles) break;
+          const uint4v b = hs[((u0 + v * sw) * steps + s) * 64 + lane];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) acc[v][t] = Op::mma(av[t], b, acc[v][t]);
+        }
+      }
+      const int now = cs + piece * X;
+      cs += 64 * column_waves;
+      uint4v old[SUBS][LOADS];
+#pragma unroll
+      for (int v = 0; v < SUBS; ++v)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) old[v][i] = in[v][i];
+      if (cs < c1) {                                           // the next columns
+        weights(av, cs, 0);
+        load(cs);
+      }
+#pragma unroll
+      for (int v = 0; v < SUBS; ++v) {
+        if (u0 + v * sw >= subtiles) break;
+        // a row's 16 pieces of four columns are permuted by its number
+#pragma unroll
+        for (int t = 0; t < 4; ++t) turn[m * 16 + ((4 * t + g) ^ m)] = acc[v][t];
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          const int n = i * (64 / LINE) + line;
+          float d[X];
+#pragma unroll
+          for (int e = 0; e < X / 4; ++e) {
+            const float4v four = turn[n * 16 + ((piece * (X / 4) + e) ^ n)];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) d[4 * e + k] = four[k];
+          }
+          const uint4v out = added((const T*)nullptr, old[v][i], d);
+          if (row[v][i] >= 0 && now < c1) put<STREAM>((T*)a.y + row[v][i] * a.y_stride + now, out);
+        }
+      }
+    }
+    if (j0 + most_rows < count) __syncthreads();             // (h has been read)
+  }
+}
+
+// Both products of 16 rows in one launch, for batches of few rows and ranks up to 16: a work-group for every run of columns and 16 rows of an
+// item, which forms what it needs of h for itself, from the caches where others do too.  Which 16 rows a work-group has it counts
+// from all items (most have fewer than 16, and work-groups for rows that are not there would wait for a place all the same);
+// eight of them stand side by side, so that those with the same rows are on one XCD.
+template <typename T>
+__global__ __launch_bounds__(512, 4) void adapt_few_kernel(AdaptArgs a) {
+  using Op = AdaptOp<T>;
+  constexpr int X = Op::X, CHUNK = 8 * X, WAVES = 8, AHEAD = 3;   // (AHEAD: runs of channels that a wave has under way)
+  constexpr int LINE = 64 / X, LOADS = 16 * LINE / 64;
+  __shared__ __attribute__((aligned(16))) uint4v stage[WAVES * 256];   // of a wave: 16 rows and 16 ranks of 128 bytes
+  __shared__ __attribute__((aligned(16))) uint4v hs[64];
+  const int eight = blockIdx.x / (8 * a.chunks), in_eight = (int)blockIdx.x - eight * 8 * a.chunks, chunk = in_eight / 8;
+  const int lane = threadIdx.x & 63, wave = rfl(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
+  int left = eight * 8 + in_eight % 8, adapter = ODMA_ADAPTER_NONE, first = 0, count = 0;
+  for (int i0 = 0; i0 < a.max_items; i0 += 64) {
+    int4 item = make_int4(ODMA_ADAPTER_NONE, 0, 0, 0);
+    if (i0 + lane < a.max_items) item = a.items[i0 + lane];
+    if ((unsigned)item.x >= (unsigned)a.n_adapters) item.z = 0;
+    const int subs = (min(max(item.z, 0), ODMA_ADAPTER_ITEM_ROWS) + 15) / 16;
+    // runs of the items in front of this one (0 to 4 each), summed by their binary digits
+    int before = 0, all = 0;
+#pragma unroll
+    for (int bit = 0; bit < 3; ++bit) {
+      const unsigned long long set = __builtin_amdgcn_ballot_w64(subs >> bit & 1);
+      before += (int)__builtin_amdgcn_mbcnt_hi((unsigned)(set >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)set, 0)) << bit;
+      all += __builtin_popcountll(set) << bit;
+    }
+    if (left < all) {
+      const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(left < before + subs));
+      const int sub = left - __builtin_amdgcn_readlane(before, l);
+      adapter = __builtin_amdgcn_readlane(item.x, l);
+      first = __builtin_amdgcn_readlane(item.y, l) + sub * 16;
+      count = min(min(__builtin_amdgcn_readlane(item.z, l), ODMA_ADAPTER_ITEM_ROWS) - sub * 16, 16);
+      break;
+    }
+    left -= all;
+  }
+  if (count <= 0) return;
+  const int flat = a.n_parts * a.rank, rank_a = rank_of(a, adapter);
+  int part = 0;
+  while (part + 1 < a.n_parts && chunk >= a.part_chunk[part + 1]) ++part;
+  const int c0 = a.part_start[part] + (chunk - a.part_chunk[part]) * a.chunk_columns;
+  const int c1 = min(c0 + a.chunk_columns, a.part_start[part + 1]), cols = a.part_start[a.n_parts];
+  uint4v* mine = stage + wave * 256;
+  const int line8 = lane >> 3, piece8 = (lane & 7) ^ line8;
+  const T* arow = (const T*)a.down + ((int64_t)adapter * flat + part * a.rank + line8) * a.width + piece8 * X;
+  const int line = lane / LINE, piece = lane % LINE;
+  // one round of loads for the rows' numbers, beside down and up; then x and base
+  int xnumber[2], row[LOADS];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) xnumber[i] = a.row_order[first + min(8 * i + line8, count - 1)];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) row[i] = a.row_order[first + min(i * (64 / LINE) + line, count - 1)];
+  uint4v av[AHEAD][2], xv[AHEAD][2], in[LOADS], uv[4];
+  auto load_ranks = [&](int j, int k) {
+    const bool there = k + piece8 * X < a.width;             // (a width is whole pieces)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      av[j][i] = uint4v{0, 0, 0, 0};
+      if (8 * i < rank_a && there) av[j][i] = *(const uint4v*)(arow + (int64_t)(8 * i) * a.width + k);
+    }
+  };
+  auto load_up = [&](int cs) {
+    const int p = X == 8 ? g & 1 : g;                        // (bf16: two pieces of ranks, for the value and for the rest of h)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      uv[t] = uint4v{0, 0, 0, 0};
+      if (p * X < rank_a && cs + t * 16 + m < c1) uv[t] = *(const uint4v*)((const T*)a.up + ((int64_t)adapter * cols + cs + t * 16 + m) * a.rank + p * X);
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j) load_ranks(j, (j * WAVES + wave) * CHUNK);
+  int cs = c0 + wave * 64;
+  if (cs < c1) load_up(cs);
+  __builtin_amdgcn_sched_barrier(0);
+  const T* xrow[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) xrow[i] = (const T*)a.x + (xnumber[i] >= 0 && xnumber[i] < a.n_rows ? xnumber[i] : 0) * a.x_stride + piece8 * X;
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i)
+    if (i * (64 / LINE) + line >= count || row[i] >= a.n_rows) row[i] = -1;
+  auto load_x = [&](int j, int k) {
+    const bool there = k + piece8 * X < a.width;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      xv[j][i] = uint4v{0, 0, 0, 0};
+      if (8 * i < count && there) xv[j][i] = *(const uint4v*)(xrow[i] + k);
+    }
+  };
+  auto load_base = [&](int cs) {
+    const int c = cs + piece * X;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+      if (row[i] >= 0 && c < c1) in[i] = *(const uint4v*)((const T*)a.base + row[i] * a.base_stride + c);
+  };
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j) load_x(j, (j * WAVES + wave) * CHUNK);
+  if (cs < c1) load_base(cs);
+  const float scale = a.scale ? a.scale[adapter] : 1.f;
+  float4v acc = {0.f, 0.f, 0.f, 0.f};
+  for (int k = wave * CHUNK; k < a.width;) {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (k >= a.width) break;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        mine[i * 64 + lane] = xv[j][i];
+        mine[(2 + i) * 64 + lane] = av[j][i];
+      }
+      if (k + AHEAD * WAVES * CHUNK < a.width) {
+        load_ranks(j, k + AHEAD * WAVES * CHUNK);
+        load_x(j, k + AHEAD * WAVES * CHUNK);
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) acc = Op::mma(mine[(16 + m) * 8 + ((4 * c + g) ^ (m & 7))], mine[m * 8 + ((4 * c + g) ^ (m & 7))], acc);
+      k += WAVES * CHUNK;
+    }
+  }
+  // ---- the waves' sums, scaled, as the second product takes them; a lane holds ranks 4 g .. 4 g + 3 of row m
+  float4v* parts = (float4v*)stage;
+  __syncthreads();
+  parts[wave * 64 + lane] = acc;
+  __syncthreads();
+  if (wave == 0) {
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) acc += parts[w * 64 + lane];
     float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    if (8 * p < rank_a && j < count) {
-      const float* src = a.h + ((int64_t)at * ODMA_ADAPTER_ITEM_ROWS + j) * flat + part * a.rank + 8 * p;
-      for (int s = 0; s < a.splits; ++s) {
-        const float4v lo = *(const float4v*)src, hi = *(const float4v*)(src + 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] += lo[e];
-          v[4 + e] += hi[e];
-        }
-        src += (int64_t)a.max_items * ODMA_ADAPTER_ITEM_ROWS * flat;
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= scale;
+    for (int e = 0; e < 4; ++e) {
+      v[e] = 4 * g < rank_a ? acc[e] * scale : 0.f;
+      v[4 + e] = 0.f;
     }
-    uint4v* to = hs + (j >> 4) * steps * 64 + (j & 15);
-    if constexpr (X == 8) {                                  // value and rest
+    if constexpr (X == 8) {
       uint4v hi, lo;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float v0 = v[2 * e], v1 = v[2 * e + 1];
-        const unsigned h0 = __float_as_uint(v0) & 0xffff0000u, h1 = __float_as_uint(v1) & 0xffff0000u;   // cut off: finite stays finite
-        const float l0 = __builtin_isinf(v0) ? 0.f : v0 - __uint_as_float(h0), l1 = __builtin_isinf(v1) ? 0.f : v1 - __uint_as_float(h1);
-        hi[e] = h0 >> 16 | h1;
-        lo[e] = float_to_bf16_bits(l0) | (unsigned)float_to_bf16_bits(l1) << 16;
-      }
-      to[p * 16] = hi;
-      to[(eights + p) * 16] = lo;
+      split_ranks(v, hi, lo);
+      uint2v* to = (uint2v*)hs + ((g >> 1) * 16 + m) * 2 + (g & 1);
+      *to = uint2v{hi[0], hi[1]};
+      to[64] = uint2v{lo[0], lo[1]};
     } else {
-      to[2 * p * 16] = __builtin_bit_cast(uint4v, float4v{v[0], v[1], v[2], v[3]});
-      to[(2 * p + 1) * 16] = __builtin_bit_cast(uint4v, float4v{v[4], v[5], v[6], v[7]});
+      hs[g * 16 + m] = __builtin_bit_cast(uint4v, float4v{v[0], v[1], v[2], v[3]});
     }
   }
   __syncthreads();
-  // ---- 64 columns a wave: four tiles whose rows are dealt out so that a lane's columns make pieces of 16 bytes, neighbouring lanes'
-  // pieces 64
-  for (int cs = c0 + wave * 64; cs < c1; cs += 256) {
-    uint4v in[4][NB];
+  const uint4v h = hs[lane];
+  float4v* turn = (float4v*)mine;                            // (the parts have been read)
+  while (cs < c1) {
+    float4v sum[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int t = 0; t < 4; ++t) sum[t] = Op::mma(uv[t], h, float4v{0.f, 0.f, 0.f, 0.f});
+    uint4v old[LOADS];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const int c = cs + (b * 4 + g) * X;
-        in[u][b] = row[u] >= 0 && c < c1 ? *(const uint4v*)((const T*)a.base + row[u] * a.base_stride + c) : uint4v{0, 0, 0, 0};
-      }
-    float4v acc[4][4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (X == 8) {
-            const unsigned w = in[u][t / 2][(t % 2) * 2 + i / 2];
-            acc[u][t][i] = __uint_as_float(i % 2 ? w & 0xffff0000u : w << 16);
-          } else {
-            acc[u][t][i] = __uint_as_float(in[u][t][i]);
-          }
-        }
-    for (int s = 0; s < steps; ++s) {
-      const int q = 4 * s + g, p = X == 8 && q >= eights ? q - eights : q;
-      const bool real = p * X < rank_a;
-      uint4v av[4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int c = X == 8 ? cs + (t / 2) * 32 + (m / 4) * 8 + (t % 2) * 4 + m % 4 : cs + t * 16 + m;
-        av[t] = real && c < c1 ? *(const uint4v*)((const T*)a.up + ((int64_t)adapter * cols + c) * a.rank + p * X) : uint4v{0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (u >= subtiles) break;
-        const uint4v bv = hs[(u * steps + s) * 64 + lane];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) acc[u][t] = Op::mma(av[t], bv, acc[u][t]);
-      }
+    for (int i = 0; i < LOADS; ++i) old[i] = in[i];
+    const int now = cs + piece * X;
+    cs += WAVES * 64;
+    if (cs < c1) {
+      load_up(cs);
+      load_base(cs);
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int t = 0; t < 4; ++t) turn[m * 16 + ((4 * t + g) ^ m)] = sum[t];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const int c = cs + (b * 4 + g) * X;
-        if (row[u] < 0 || c >= c1) continue;
-        uint4v out;
+    for (int i = 0; i < LOADS; ++i) {
+      const int n = i * (64 / LINE) + line;
+      float d[X];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (X == 8)
-            out[i] = float_to_bf16_bits(acc[u][2 * b + i / 2][2 * (i % 2)]) | (unsigned)float_to_bf16_bits(acc[u][2 * b + i / 2][2 * (i % 2) + 1]) << 16;
-          else
-            out[i] = __float_as_uint(acc[u][b][i]);
-        }
-        *(uint4v*)((T*)a.y + row[u] * a.y_stride + c) = out;
+      for (int e = 0; e < X / 4; ++e) {
+        const float4v four = turn[n * 16 + ((piece * (X / 4) + e) ^ n)];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) d[4 * e + k] = four[k];
       }
+      if (row[i] >= 0 && now < c1) *(uint4v*)((T*)a.y + row[i] * a.y_stride + now) = added((const T*)nullptr, old[i], d);
+    }
   }
 }
 

@@ -54,12 +54,18 @@ void launch_add_norm(const AddNormArgs& a, bool many, hipStream_t s) {
   else launch_add_norm<T, R, 16, 4>(a, s);
 }
 
-// What the adapters' launches look like, or why they are refused
+constexpr int ADAPT_FEW = 4096, ADAPT_FEW_WG = 360, ADAPT_SPLIT = 256, ADAPT_WG = 1024, ADAPT_UP_WG = 1024;
+
+// Runs of 16 rows of items, at most, in eights
+inline int64_t few_sixteens(int64_t n_rows, int64_t items) { return (n_rows / 16 + std::min(items, n_rows) + 7) / 8 * 8; }
+
+// What the adapters' launches look like, or why they are refused.  n_rows < 0: for the scratch of any number of rows.
 struct AdaptShape {
   int flat, tiles, groups, splits, split_channels, chunk_columns, chunks;
+  bool few, stream;
   size_t scratch;
 };
-const char* adapt_shape(const odma_adapters_t* ad, int64_t max_items, AdaptShape* shape) {
+const char* adapt_shape(const odma_adapters_t* ad, int elem_bytes, int64_t n_rows, int64_t max_items, AdaptShape* shape) {
   if (!ad || !ad->down || !ad->up) return "adapters without weights";
   if (ad->n_adapters < 1 || ad->n_adapters > ODMA_MAX_ADAPTERS) return "1 to ODMA_MAX_ADAPTERS adapters";
   if (ad->rank < 8 || ad->rank > ODMA_MAX_RANK || ad->rank % 8) return "the rank must be a multiple of 8 up to ODMA_MAX_RANK";
@@ -70,30 +76,62 @@ const char* adapt_shape(const odma_adapters_t* ad, int64_t max_items, AdaptShape
     if (ad->part_start[p + 1] <= ad->part_start[p] || ad->part_start[p + 1] % 16) return "parts must ascend by multiples of 16 columns";
   if (max_items < 0) return "invalid argument";
   if (!aligned(ad->down, 16) || !aligned(ad->up, 16)) return "weights must start on 16-byte boundaries";
+  const int64_t items = std::max<int64_t>(max_items, 1);
+  const int cols = ad->part_start[ad->n_parts];
   shape->flat = ad->n_parts * ad->rank;
   const int all = (shape->flat + 15) / 16;
   shape->tiles = all <= 4 ? all : 4;
   shape->groups = (all + shape->tiles - 1) / shape->tiles;
-  // Channels are cut between work-groups where items are few: 512 each at least, and no more work-groups than the chip holds a few times.
-  const int most = (ad->width + 511) / 512;
-  shape->splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 4096 / std::max<int64_t>(max_items, 1)));
+  // Channels are cut between work-groups where items are few
+  const int fewest = elem_bytes == 4 ? ADAPT_SPLIT / 2 : ADAPT_SPLIT;
+  shape->splits = (int)std::max<int64_t>(1, std::min<int64_t>((ad->width + fewest - 1) / fewest, ADAPT_WG / (items * shape->groups)));
   shape->split_channels = ((ad->width + shape->splits - 1) / shape->splits + 63) / 64 * 64;
   shape->splits = (ad->width + shape->split_channels - 1) / shape->split_channels;
   shape->scratch = std::max<size_t>((size_t)max_items * ODMA_ADAPTER_ITEM_ROWS * shape->flat * sizeof(float) * shape->splits, 256);
-  shape->chunk_columns = 512;
-  shape->chunks = 0;
-  for (int p = 0; p < ad->n_parts; ++p) shape->chunks += (ad->part_start[p + 1] - ad->part_start[p] + shape->chunk_columns - 1) / shape->chunk_columns;
-  if ((int64_t)max_items * std::max(shape->chunks, shape->splits * shape->groups) > MAX_WG) return "too many items";
+  auto chunks_of = [&](int columns) {
+    int64_t n = 0;
+    for (int p = 0; p < ad->n_parts; ++p) n += (ad->part_start[p + 1] - ad->part_start[p] + columns - 1) / columns;
+    return n;
+  };
+  shape->few = n_rows >= 0 && n_rows <= ADAPT_FEW && ad->rank <= 16 && items <= 1024 && cols <= 1 << 17;
+  shape->stream = n_rows * cols * elem_bytes > (int64_t)4 << 20 && items * cols / 512 >= ADAPT_UP_WG;
+  shape->chunk_columns = shape->few ? 512 : 64;
+  if (shape->few)
+    while (shape->chunk_columns < 4096 && (std::min(items, n_rows) + n_rows / 64) * chunks_of(shape->chunk_columns) > ADAPT_FEW_WG) shape->chunk_columns *= 2;
+  else
+    while (shape->chunk_columns < 512 && items * cols / shape->chunk_columns > ADAPT_UP_WG) shape->chunk_columns *= 2;
+  if (items * std::max<int64_t>(chunks_of(shape->chunk_columns), shape->splits * shape->groups) > MAX_WG) return "too many items";
+  shape->chunks = (int)chunks_of(shape->chunk_columns);
   return nullptr;
 }
 
-template <typename T>
-void launch_adapt(const AdaptArgs& a, const AdaptShape& shape, hipStream_t s) {
+template <typename T, bool STREAM>
+void launch_adapt_down(const AdaptArgs& a, const AdaptShape& shape, hipStream_t s) {
   const dim3 grid((unsigned)(shape.splits * shape.groups * a.max_items));
-  if (shape.tiles == 1) hipLaunchKernelGGL((adapt_down_kernel<T, 1>), grid, dim3(256), 0, s, a);
-  else if (shape.tiles == 2) hipLaunchKernelGGL((adapt_down_kernel<T, 2>), grid, dim3(256), 0, s, a);
-  else if (shape.tiles == 3) hipLaunchKernelGGL((adapt_down_kernel<T, 3>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((adapt_down_kernel<T, 4>), grid, dim3(256), 0, s, a);
+  if (shape.tiles == 1) hipLaunchKernelGGL((adapt_down_kernel<T, 1, STREAM>), grid, dim3(256), 0, s, a);
+  else if (shape.tiles == 2) hipLaunchKernelGGL((adapt_down_kernel<T, 2, STREAM>), grid, dim3(256), 0, s, a);
+  else if (shape.tiles == 3) hipLaunchKernelGGL((adapt_down_kernel<T, 3, STREAM>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((adapt_down_kernel<T, 4, STREAM>), grid, dim3(256), 0, s, a);
+}
+
+template <typename T>
+int launch_adapt(const char* where, const AdaptArgs& a, const AdaptShape& shape, hipStream_t s) {
+  hipError_t e;
+  if (shape.few) {
+    hipLaunchKernelGGL((adapt_few_kernel<T>), dim3((unsigned)(few_sixteens(a.n_rows, a.max_items) * shape.chunks)), dim3(512), 0, s, a);
+    e = hipGetLastError();
+    return e == hipSuccess ? ODMA_OK : hip_fail(where, e);
+  }
+  if (shape.stream && shape.groups == 1) launch_adapt_down<T, true>(a, shape, s);
+  else launch_adapt_down<T, false>(a, shape, s);
+  e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(where, e);
+  const dim3 grid((unsigned)(shape.chunks * a.max_items));
+  const size_t lds = (size_t)(a.rank > 128 ? 2 : 4) * ((a.rank + 15) / 16) * 64 * 16;
+  if (shape.stream) hipLaunchKernelGGL((adapt_up_kernel<T, 2, true>), grid, dim3(256), lds, s, a);
+  else hipLaunchKernelGGL((adapt_up_kernel<T, 4, false>), grid, dim3(256), lds, s, a);
+  e = hipGetLastError();
+  return e == hipSuccess ? ODMA_OK : hip_fail(where, e);
 }
 
 }  // namespace
@@ -186,7 +224,7 @@ int odma_group_adapters(odma_pool_t* pool, int32_t n, const int32_t* adapter, in
 size_t odma_adapt_scratch_bytes(const odma_pool_t* pool, const odma_adapters_t* adapters, int32_t max_items) {
   const char* where = "odma_adapt_scratch_bytes";
   AdaptShape shape;
-  const char* why = pool ? adapt_shape(adapters, max_items, &shape) : "null pool";
+  const char* why = pool ? adapt_shape(adapters, (int)pool->elem_bytes, -1, max_items, &shape) : "null pool";
   if (why) {
     refuse(where, why);
     return 0;
@@ -204,7 +242,7 @@ int odma_adapt_rows(odma_pool_t* pool, int64_t n_rows, const odma_adapters_t* ad
   if (n_rows < 0 || !items || !row_order || !x || !base || !y || !scratch) return refuse(where, "invalid argument");
   if (n_rows > MAX_LISTED) return refuse(where, "too many rows");
   AdaptShape shape;
-  const char* why = adapt_shape(adapters, max_items, &shape);
+  const char* why = adapt_shape(adapters, (int)pool->elem_bytes, n_rows, max_items, &shape);
   if (why) return refuse(where, why);
   const int unit = pool->elem_bytes == 4 ? 4 : 8;              // elements of 16 bytes
   if (!aligned(x, 16) || !aligned(base, 16) || !aligned(y, 16) || x_stride < 0 || x_stride % unit || base_stride < 0 || base_stride % unit ||
@@ -245,18 +283,7 @@ int odma_adapt_rows(odma_pool_t* pool, int64_t n_rows, const odma_adapters_t* ad
   for (int p = 0; p < ODMA_MAX_PARTS; ++p)
     a.part_chunk[p + 1] = a.part_chunk[p] + (a.part_start[p + 1] - a.part_start[p] + a.chunk_columns - 1) / a.chunk_columns;
   hipStream_t s = (hipStream_t)stream;
-  const bool f32 = pool->elem_bytes == 4;
-  if (f32) launch_adapt<float>(a, shape, s);
-  else launch_adapt<unsigned short>(a, shape, s);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return hip_fail(where, e);
-  const dim3 grid((unsigned)(shape.chunks * max_items));
-  const size_t lds = (size_t)4 * ((a.rank + 15) / 16) * 64 * 16;
-  if (f32) hipLaunchKernelGGL((adapt_up_kernel<float>), grid, dim3(256), lds, s, a);
-  else hipLaunchKernelGGL((adapt_up_kernel<unsigned short>), grid, dim3(256), lds, s, a);
-  e = hipGetLastError();
-  if (e != hipSuccess) return hip_fail(where, e);
-  return ODMA_OK;
+  return pool->elem_bytes == 4 ? launch_adapt<float>(where, a, shape, s) : launch_adapt<unsigned short>(where, a, shape, s);
 }
 
 }  // extern "C"

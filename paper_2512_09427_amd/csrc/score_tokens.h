@@ -153,7 +153,7 @@ __global__ __launch_bounds__(W * 64) void score_kernel(ScoreArgs a) {
   __shared__ u64 best;                                       // of the waves' bounds
   __shared__ float tops[W];
   __shared__ int larger_of[W], held_of[W], listed;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = rfl(threadIdx.x >> 6);
   const int64_t row = (int64_t)blockIdx.x / a.parts;
   const int part = (int)((int64_t)blockIdx.x - row * a.parts);
   if (!row_there(a, row)) return;
@@ -163,13 +163,12 @@ __global__ __launch_bounds__(W * 64) void score_kernel(ScoreArgs a) {
   // whole pieces, and up to 2 V - 2 elements in front of and behind them
   const int lead = min((int)((16 - ((uintptr_t)(p + e0) & 15)) & 15) / (int)sizeof(T), e1 - e0);
   const int pieces = (e1 - e0 - lead) / V, body = e0 + lead, tail = body + pieces * V;
-  uint4v w[U];
+  uint4v w[U] = {};
   auto load = [&](int g) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = g + u * N + lane;
-      w[u] = uint4v{0, 0, 0, 0};
-      if (i < pieces) w[u] = __builtin_nontemporal_load((const uint4v*)(p + body + i * V));
+      if (g + u * N >= pieces) continue;
+      w[u] = __builtin_nontemporal_load((const uint4v*)(p + body) + min(g + u * N + lane, pieces - 1));
     }
   };
   load(wave * 64);                                           // under way while the given token's logit is looked up
@@ -278,7 +277,7 @@ __global__ __launch_bounds__(W * 64) void score_kernel(ScoreArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       score_piece((const T*)nullptr, w[u], x[u]);
-      if (g + u * N + lane >= pieces)
+      if (g + u * N + 64 > pieces && g + u * N + lane >= pieces)
 #pragma unroll
         for (int i = 0; i < V; ++i) x[u][i] = -INFINITY;
     }

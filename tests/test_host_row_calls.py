@@ -142,7 +142,7 @@ def test_adapt_rows(runtime):  # noqa: F811
         assert refused(adapt, p, size=size - 1)
         adapt(p, y=K, ys=96), adapt(f, xs=516, bs=100, ys=100), adapt(p, xs=0, bs=0)
         two = launched(lambda: adapt(p, ys=256, ad=make(rank=256, part_cols=(64, 64, 64, 64), width=32768)))
-        assert ["down" in two[0][0], "up" in two[1][0]] == [True, True] and len(two) == 2 and two[1][2] == 65536
+        assert ["down" in two[0][0], "up" in two[1][0]] == [True, True] and len(two) == 2 and two[1][2] == 32768
         for at in (0, 1):
             hip.fake_fail_launch(at)
             assert fails(lambda: adapt(p))
@@ -155,8 +155,8 @@ def test_score_tokens(runtime):  # noqa: F811
         nan, inf = float("nan"), float("inf")
         for bad in (dict(n=-1), dict(n=(1 << 22) + 1), dict(logits=None), dict(dtype=B.FP8), dict(dtype=-1), dict(vocab=0), dict(vocab=-4),
                     dict(vocab=(1 << 24) + 1, stride=1 << 25), dict(stride=31999), dict(stride=-32000), dict(logits=Q + 1),
-                    dict(logits=Q + 2, dtype=B.F32), dict(scale=0.0), dict(scale=-1.0), dict(scale=nan), dict(scale=inf), dict(scale=1e-20),
-                    dict(scale=1e20), dict(tokens=None), dict(tokens=None, lp=None), dict(tokens=None, rank=None), dict(top=-1), dict(top=65),
+                    dict(logits=Q + 2, dtype=B.F32), dict(scale=0.0), dict(scale=-1.0), dict(scale=nan), dict(scale=inf), dict(scale=1e-8),
+                    dict(scale=1e8), dict(tokens=None), dict(tokens=None, lp=None), dict(tokens=None, rank=None), dict(top=-1), dict(top=65),
                     dict(vocab=4), dict(top=0), dict(top=0, ids=None), dict(top=0, lps=None), dict(ids=None, lps=None),
                     dict(top=0, ids=None, lps=None, lp=None, rank=None, ent=None), dict(scratch=None), dict(scratch=SCRATCH + 128), dict(size=0)):
             assert refused(score, p, **bad), bad
@@ -169,7 +169,7 @@ def test_score_tokens(runtime):  # noqa: F811
         assert refused(score, p, size=size - 1)
         # results that nobody asks for
         score(p, tokens=None, lp=None, rank=None), score(p, top=0, ids=None, lps=None), score(p, ids=None), score(p, lps=None, ent=None)
-        score(p, n=1, stride=0), score(p, logits=Q + 2, stride=32001), score(p, logits=Q + 4, stride=32001, dtype=B.F32, scale=2.0 ** -64)
+        score(p, n=1, stride=0), score(p, logits=Q + 2, stride=32001), score(p, logits=Q + 4, stride=32001, dtype=B.F32, scale=2.0 ** -24)
         # few rows are cut into parts of 2048 tokens or more, 64 at most, up to 1024 work-groups, which a second launch joins
         for n, vocab, wg in ((1, 2048, 1), (1, 2049, 2), (1, 32000, 16), (1, 1 << 24, 64), (64, 32000, 1024), (100, 32000, 800), (513, 32000, 513),
                              (4096, 1 << 20, 4096), (1 << 22, 5, 1 << 22)):
