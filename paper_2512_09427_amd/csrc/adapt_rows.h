@@ -61,6 +61,13 @@ struct AdaptOp<float> {
   }
 };
 
+// Which item a work-group has, of `pieces` each: eight items side by side, so that an item's work-groups share an XCD's L2.
+__device__ __forceinline__ void item_of(int pieces, int& at, int& piece) {
+  const int eight = blockIdx.x / (8 * pieces), rest = (int)blockIdx.x - eight * 8 * pieces;
+  at = eight * 8 + rest % 8;
+  piece = rest / 8;
+}
+
 // Rows that are more than a cache keeps pass by it.
 template <bool STREAM, typename T>
 __device__ __forceinline__ uint4v taken(const T* p) {
@@ -115,12 +122,16 @@ __global__ __launch_bounds__(256) void adapt_down_kernel(AdaptArgs a) {
   if (count <= 0 || (unsigned)adapter >= (unsigned)a.n_adapters) return;
   const int lane = threadIdx.x & 63, wave = rfl(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const int split = cut % a.splits, group = cut / a.splits;
+  // the lane's line of eight, and which of its pieces it loads
+  const int line = lane >> 3, piece = (lane & 7) ^ line;
+  // the rows' numbers, in one round with the adapter's rank; rows that are not there repeat one: what they give is not used
+  int number[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) number[i] = a.row_order[first + min(8 * i + line, count - 1)];
   const int flat = a.n_parts * a.rank, rank_a = rank_of(a, adapter);
   const int k0 = split * a.split_channels, k1 = min(k0 + a.split_channels, a.width);
   const int subtiles = (count + 15) / 16, r0 = group * MT * 16;
   uint4v* mine = stage + wave * WAVE;
-  // the lane's line of eight, and which of its pieces it loads
-  const int line = lane >> 3, piece = (lane & 7) ^ line;
   // ranks: eight at a time are all there or not (flat and the adapter's rank are multiples of 8); what those that are not hold is not used
   const T* arow = (const T*)a.down + ((int64_t)adapter * flat + r0 + line) * a.width + piece * X;
   bool there[2 * MT];
@@ -136,12 +147,9 @@ __global__ __launch_bounds__(256) void adapt_down_kernel(AdaptArgs a) {
     for (int u = 0; u < 4; ++u) acc[t][u] = float4v{0.f, 0.f, 0.f, 0.f};
   auto run = [&](auto subs) {
     constexpr int NS = decltype(subs)::value;
-    const T* xrow[2 * NS];                                   // rows that are not there repeat one: what they give is not used
+    const T* xrow[2 * NS];
 #pragma unroll
-    for (int i = 0; i < 2 * NS; ++i) {
-      const int row = a.row_order[first + min(8 * i + line, count - 1)];
-      xrow[i] = (const T*)a.x + (row >= 0 && row < a.n_rows ? row : 0) * a.x_stride + piece * X;
-    }
+    for (int i = 0; i < 2 * NS; ++i) xrow[i] = (const T*)a.x + (number[i] >= 0 && number[i] < a.n_rows ? number[i] : 0) * a.x_stride + piece * X;
     uint4v av[2 * MT], xv[2 * NS];
     auto load = [&](int k) {
       const bool in = k + piece * X < k1;                    // (a width is whole pieces)
@@ -238,11 +246,7 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
 #pragma unroll
     for (int v = 0; v < SUBS; ++v)
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int j = (u0 + v * sw) * 16 + i * (64 / LINE) + line;
-        row[v][i] = j < rows ? a.row_order[first + j0 + j] : -1;
-        if (row[v][i] >= a.n_rows) row[v][i] = -1;
-      }
+      for (int i = 0; i < LOADS; ++i) row[v][i] = a.row_order[first + j0 + min((u0 + v * sw) * 16 + i * (64 / LINE) + line, rows - 1)];
     uint4v in[SUBS][LOADS];
     auto load = [&](int cs) {
       const int c = cs + piece * X;
@@ -258,22 +262,25 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
       for (int t = 0; t < 4; ++t) {
         const int c = cs + t * 16 + m;
         av[t] = uint4v{0, 0, 0, 0};
-        if (p * X < rank_a && c < c1) av[t] = *(const uint4v*)(up + (int64_t)c * a.rank + p * X);
+        if (p * X < a.rank && c < c1) av[t] = *(const uint4v*)(up + (int64_t)c * a.rank + p * X);
       }
     };
     int cs = c0 + wave / sw * 64;
     uint4v av[4];
-    if (cs < c1) {                                             // under way while h is staged
-      weights(av, cs, 0);
-      load(cs);
-    }
-    // ---- h: the splits' sums, scaled
+    if (cs < c1) weights(av, cs, 0);                           // under way while h is staged
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int v = 0; v < SUBS; ++v)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        if ((u0 + v * sw) * 16 + i * (64 / LINE) + line >= rows || row[v][i] >= a.n_rows) row[v][i] = -1;
+    if (cs < c1) load(cs);
     for (int i = threadIdx.x; i < subtiles * 16 * eights; i += 256) {
       const int j = i / eights, p = i - j * eights;
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = 0.f;
-      if (8 * p < rank_a && j < rows) {
+      if (8 * p < a.rank && j < rows) {                      // (behind the adapter's rank h is 0)
         const float* src = a.h + ((int64_t)at * ODMA_ADAPTER_ITEM_ROWS + j0 + j) * flat + part * a.rank + 8 * p;
 #pragma unroll 4
         for (int s = 0; s < a.splits; ++s) {
@@ -308,6 +315,9 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
         for (int t = 0; t < 4; ++t) acc[v][t] = float4v{0.f, 0.f, 0.f, 0.f};
       for (int s = 0; s < steps; ++s) {
         if (s > 0) weights(av, cs, s);
+        if ((X == 8 ? (4 * s + g) % eights : 4 * s + g) * X >= rank_a)      // (what lies behind the adapter's rank may be anything)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) av[t] = uint4v{0, 0, 0, 0};
 #pragma unroll
         for (int v = 0; v < SUBS; ++v) {
           if (u0 + v * sw >= subtiles) break;
@@ -352,20 +362,22 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
   }
 }
 
-// Both products of 16 rows in one launch, for batches of few rows and ranks up to 16: a work-group for every run of columns and 16 rows of an
+// Both products of 16 rows in one launch, for batches of few rows and ranks up to 64 (PT: tiles of 16): a work-group for every run of columns and 16 rows of an
 // item, which forms what it needs of h for itself, from the caches where others do too.  Which 16 rows a work-group has it counts
 // from all items (most have fewer than 16, and work-groups for rows that are not there would wait for a place all the same);
 // eight of them stand side by side, so that those with the same rows are on one XCD.
-template <typename T>
-__global__ __launch_bounds__(512, 4) void adapt_few_kernel(AdaptArgs a) {
+template <typename T, int PT>
+__global__ __launch_bounds__(512, PT == 1 ? 4 : 2) void adapt_few_kernel(AdaptArgs a) {
   using Op = AdaptOp<T>;
-  constexpr int X = Op::X, CHUNK = 8 * X, WAVES = 8, AHEAD = 3;   // (AHEAD: runs of channels that a wave has under way)
+  constexpr int X = Op::X, CHUNK = 8 * X, WAVES = 8, AHEAD = PT == 4 ? 2 : 3;   // (AHEAD: runs of channels that a wave has under way)
   constexpr int LINE = 64 / X, LOADS = 16 * LINE / 64;
-  __shared__ __attribute__((aligned(16))) uint4v stage[WAVES * 256];   // of a wave: 16 rows and 16 ranks of 128 bytes
-  __shared__ __attribute__((aligned(16))) uint4v hs[64];
-  const int eight = blockIdx.x / (8 * a.chunks), in_eight = (int)blockIdx.x - eight * 8 * a.chunks, chunk = in_eight / 8;
+  constexpr int TWO = PT < 2 ? PT : 2, WAVE = (16 + TWO * 16) * 8;   // of a wave in LDS: 16 rows and 16 or 32 ranks of 128 bytes, in pieces
+  __shared__ __attribute__((aligned(16))) uint4v stage[WAVES * WAVE];
+  __shared__ __attribute__((aligned(16))) uint4v hs[PT * 64];
+  int left, chunk;
+  item_of(a.chunks, left, chunk);
   const int lane = threadIdx.x & 63, wave = rfl(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
-  int left = eight * 8 + in_eight % 8, adapter = ODMA_ADAPTER_NONE, first = 0, count = 0;
+  int adapter = ODMA_ADAPTER_NONE, first = 0, count = 0;
   for (int i0 = 0; i0 < a.max_items; i0 += 64) {
     int4 item = make_int4(ODMA_ADAPTER_NONE, 0, 0, 0);
     if (i0 + lane < a.max_items) item = a.items[i0 + lane];
@@ -395,7 +407,7 @@ __global__ __launch_bounds__(512, 4) void adapt_few_kernel(AdaptArgs a) {
   while (part + 1 < a.n_parts && chunk >= a.part_chunk[part + 1]) ++part;
   const int c0 = a.part_start[part] + (chunk - a.part_chunk[part]) * a.chunk_columns;
   const int c1 = min(c0 + a.chunk_columns, a.part_start[part + 1]), cols = a.part_start[a.n_parts];
-  uint4v* mine = stage + wave * 256;
+  uint4v* mine = stage + wave * WAVE;
   const int line8 = lane >> 3, piece8 = (lane & 7) ^ line8;
   const T* arow = (const T*)a.down + ((int64_t)adapter * flat + part * a.rank + line8) * a.width + piece8 * X;
   const int line = lane / LINE, piece = lane % LINE;
@@ -405,27 +417,30 @@ __global__ __launch_bounds__(512, 4) void adapt_few_kernel(AdaptArgs a) {
   for (int i = 0; i < 2; ++i) xnumber[i] = a.row_order[first + min(8 * i + line8, count - 1)];
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) row[i] = a.row_order[first + min(i * (64 / LINE) + line, count - 1)];
-  uint4v av[AHEAD][2], xv[AHEAD][2], in[LOADS], uv[4];
+  uint4v av[AHEAD][2 * PT], xv[AHEAD][2], in[LOADS], uv[PT][4];
   auto load_ranks = [&](int j, int k) {
     const bool there = k + piece8 * X < a.width;             // (a width is whole pieces)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 2 * PT; ++i) {
       av[j][i] = uint4v{0, 0, 0, 0};
       if (8 * i < rank_a && there) av[j][i] = *(const uint4v*)(arow + (int64_t)(8 * i) * a.width + k);
     }
   };
   auto load_up = [&](int cs) {
-    const int p = X == 8 ? g & 1 : g;                        // (bf16: two pieces of ranks, for the value and for the rest of h)
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      uv[t] = uint4v{0, 0, 0, 0};
-      if (p * X < rank_a && cs + t * 16 + m < c1) uv[t] = *(const uint4v*)((const T*)a.up + ((int64_t)adapter * cols + cs + t * 16 + m) * a.rank + p * X);
+    for (int s = 0; s < PT; ++s) {
+      const int q = 4 * s + g, p = X == 8 && q >= 2 * PT ? q - 2 * PT : q;   // (bf16: pieces of ranks for the value and for the rest of h)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        uv[s][t] = uint4v{0, 0, 0, 0};
+        if (p * X < rank_a && cs + t * 16 + m < c1) uv[s][t] = *(const uint4v*)((const T*)a.up + ((int64_t)adapter * cols + cs + t * 16 + m) * a.rank + p * X);
+      }
     }
   };
 #pragma unroll
   for (int j = 0; j < AHEAD; ++j) load_ranks(j, (j * WAVES + wave) * CHUNK);
   int cs = c0 + wave * 64;
-  if (cs < c1) load_up(cs);
+  if (PT == 1 && cs < c1) load_up(cs);
   __builtin_amdgcn_sched_barrier(0);
   const T* xrow[2];
 #pragma unroll
@@ -451,56 +466,70 @@ __global__ __launch_bounds__(512, 4) void adapt_few_kernel(AdaptArgs a) {
   for (int j = 0; j < AHEAD; ++j) load_x(j, (j * WAVES + wave) * CHUNK);
   if (cs < c1) load_base(cs);
   const float scale = a.scale ? a.scale[adapter] : 1.f;
-  float4v acc = {0.f, 0.f, 0.f, 0.f};
+  float4v acc[PT];
+#pragma unroll
+  for (int t = 0; t < PT; ++t) acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
   for (int k = wave * CHUNK; k < a.width;) {
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
       if (k >= a.width) break;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        mine[i * 64 + lane] = xv[j][i];
-        mine[(2 + i) * 64 + lane] = av[j][i];
-      }
-      if (k + AHEAD * WAVES * CHUNK < a.width) {
-        load_ranks(j, k + AHEAD * WAVES * CHUNK);
-        load_x(j, k + AHEAD * WAVES * CHUNK);
-      }
+      for (int i = 0; i < 2; ++i) mine[i * 64 + lane] = xv[j][i];
 #pragma unroll
-      for (int c = 0; c < 2; ++c) acc = Op::mma(mine[(16 + m) * 8 + ((4 * c + g) ^ (m & 7))], mine[m * 8 + ((4 * c + g) ^ (m & 7))], acc);
+      for (int t0 = 0; t0 < PT; t0 += TWO) {
+#pragma unroll
+        for (int i = 0; i < 2 * TWO; ++i) mine[(2 + i) * 64 + lane] = av[j][2 * t0 + i];
+        if (t0 + TWO >= PT && k + AHEAD * WAVES * CHUNK < a.width) {
+          load_ranks(j, k + AHEAD * WAVES * CHUNK);
+          load_x(j, k + AHEAD * WAVES * CHUNK);
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const uint4v b = mine[m * 8 + ((4 * c + g) ^ (m & 7))];
+#pragma unroll
+          for (int t = 0; t < TWO; ++t) acc[t0 + t] = Op::mma(mine[(16 + t * 16 + m) * 8 + ((4 * c + g) ^ (m & 7))], b, acc[t0 + t]);
+        }
+      }
       k += WAVES * CHUNK;
     }
   }
   // ---- the waves' sums, scaled, as the second product takes them; a lane holds ranks 4 g .. 4 g + 3 of row m
   float4v* parts = (float4v*)stage;
+  if (PT > 1 && cs < c1) load_up(cs);
   __syncthreads();
-  parts[wave * 64 + lane] = acc;
-  __syncthreads();
-  if (wave == 0) {
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) acc += parts[w * 64 + lane];
+  for (int t = 0; t < PT; ++t) parts[(wave * PT + t) * 64 + lane] = acc[t];
+  __syncthreads();
+  if (wave < PT) {
+    float4v sum = parts[wave * 64 + lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += parts[(w * PT + wave) * 64 + lane];
     float v[8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      v[e] = 4 * g < rank_a ? acc[e] * scale : 0.f;
+      v[e] = 16 * wave + 4 * g < rank_a ? sum[e] * scale : 0.f;
       v[4 + e] = 0.f;
     }
     if constexpr (X == 8) {
       uint4v hi, lo;
       split_ranks(v, hi, lo);
-      uint2v* to = (uint2v*)hs + ((g >> 1) * 16 + m) * 2 + (g & 1);
+      uint2v* to = (uint2v*)hs + ((2 * wave + (g >> 1)) * 16 + m) * 2 + (g & 1);
       *to = uint2v{hi[0], hi[1]};
-      to[64] = uint2v{lo[0], lo[1]};
+      to[PT * 64] = uint2v{lo[0], lo[1]};
     } else {
-      hs[g * 16 + m] = __builtin_bit_cast(uint4v, float4v{v[0], v[1], v[2], v[3]});
+      hs[(4 * wave + g) * 16 + m] = __builtin_bit_cast(uint4v, float4v{v[0], v[1], v[2], v[3]});
     }
   }
   __syncthreads();
-  const uint4v h = hs[lane];
   float4v* turn = (float4v*)mine;                            // (the parts have been read)
   while (cs < c1) {
     float4v sum[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) sum[t] = Op::mma(uv[t], h, float4v{0.f, 0.f, 0.f, 0.f});
+    for (int t = 0; t < 4; ++t) {
+      sum[t] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < PT; ++s) sum[t] = Op::mma(uv[s][t], hs[s * 64 + lane], sum[t]);
+    }
     uint4v old[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) old[i] = in[i];

@@ -39,7 +39,8 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void add_norm_kernel(AddNormA
     there = slot != ODMA_SLOT_NONE && slot < a.pool_tokens;
   }
   if (W == 1 && !there) return;                            // (no barrier where a wave has a row of its own)
-  Piece<T> b[P], g[P];
+  constexpr bool EARLY = P <= 2;                           // weights too are loaded in the first round, where registers are plenty
+  Piece<T> b[P], g[P], wb[P], wn[P];
   Piece<R> r[P];
   bool in[P];
 #pragma unroll
@@ -53,6 +54,8 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void add_norm_kernel(AddNormA
       if (a.block) b[p] = take8((const T*)a.block + row * a.block_stride + at);
       r[p] = take8((const R*)a.residual + row * a.residual_stride + at);
       if (a.gate) g[p] = take8((const T*)a.gate + row * a.gate_stride + at);
+      if (EARLY && a.block_weight) wb[p] = take8((const T*)a.block_weight + at);
+      if (EARLY && a.next_weight) wn[p] = take8((const T*)a.next_weight + at);
     }
   }
   // The sum over a row's lanes, in all of them; `turn`: sums that follow one another take turns at two places
@@ -87,7 +90,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void add_norm_kernel(AddNormA
     widen8(r[p], old);
     if (a.block_weight && in[p]) {
       float weight[8];
-      widen8(take8((const T*)a.block_weight + at), weight);
+      widen8(EARLY ? wb[p] : take8((const T*)a.block_weight + at), weight);
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = x[i] * inv * weight[i];
     }
@@ -112,7 +115,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void add_norm_kernel(AddNormA
     const int at = ((p * W + w) * 64 + lane) * 8;
     if (!in[p]) continue;
     float weight[8];
-    widen8(take8((const T*)a.next_weight + at), weight);
+    widen8(EARLY ? wn[p] : take8((const T*)a.next_weight + at), weight);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[p][i] = v[p][i] * inv * weight[i];
     put8((T*)a.x_out + row * a.width + at, v[p]);

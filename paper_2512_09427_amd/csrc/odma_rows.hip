@@ -54,7 +54,20 @@ void launch_add_norm(const AddNormArgs& a, bool many, hipStream_t s) {
   else launch_add_norm<T, R, 16, 4>(a, s);
 }
 
-constexpr int ADAPT_FEW = 4096, ADAPT_FEW_WG = 360, ADAPT_SPLIT = 256, ADAPT_WG = 1024, ADAPT_UP_WG = 1024;
+// Up to so many rows, both products in one launch (adapt_few_kernel), by the bytes of a channel of an adapter's ranks, which every work-group of
+// it reads: 32 (bf16, rank 16), 64, more.  Against the two launches, us a call, 3584 channels, 4608 columns in three parts, requests / adapters:
+//   32: 1 / 4 6.5 and 8.9, 64 / 64 11.2 and 18.3, 1 024 / 32 17.2 and 22.7, 4 096 / 32 42.9 and 50.4, 8 192 / 32 72.3 and 64.2
+//   64 (rank 32): 64 / 16 9.7 and 12.2, 256 / 32 11.4 and 20.4, 1 024 / 32 28.6 and 27.5;  fp32, rank 16: 64 / 64 18 and 23
+//   128 (rank 64): 1 / 4 14.2 and 10.7, 64 / 16 15.2 and 15.2, 256 / 32 16.5 and 29.7, 1 024 / 32 54.9 and 46.0;  fp32 28.6 and 12.3, 30 and 19, 33 and 46, 100 and 93
+constexpr int ADAPT_FEW = 4096;
+// Work-groups that it is cut into, by the adapters that a batch may have.  64 / 64 as above 11.0 us with 260 and 12.3 with 390; 256 / 32 9.1 with 360
+// and 11.4 with 160.
+constexpr int ADAPT_FEW_WG = 360;
+// The first of two launches: fewest channels of a cut, and work-groups up to which channels are cut: every cut is one more array for the second
+// launch to add up.  256 / 32 of rank 64 29.7 us with 512 and 32.8 with 256; 24 fp32 prompts of 2 300 rows 24.7 with 512 and 27.5 with 1024.
+constexpr int ADAPT_SPLIT = 512, ADAPT_WG = 512;
+// The second: work-groups up to which columns are cut, down to 64.  1 024 / 32 of rank 64 46 us with 1024 and 60 with 512.
+constexpr int ADAPT_UP_WG = 1024;
 
 // Runs of 16 rows of items, at most, in eights
 inline int64_t few_sixteens(int64_t n_rows, int64_t items) { return (n_rows / 16 + std::min(items, n_rows) + 7) / 8 * 8; }
@@ -80,11 +93,9 @@ const char* adapt_shape(const odma_adapters_t* ad, int elem_bytes, int64_t n_row
   const int cols = ad->part_start[ad->n_parts];
   shape->flat = ad->n_parts * ad->rank;
   const int all = (shape->flat + 15) / 16;
-  shape->tiles = all <= 4 ? all : 4;
+  shape->tiles = std::min(all, 4);
   shape->groups = (all + shape->tiles - 1) / shape->tiles;
-  // Channels are cut between work-groups where items are few
-  const int fewest = elem_bytes == 4 ? ADAPT_SPLIT / 2 : ADAPT_SPLIT;
-  shape->splits = (int)std::max<int64_t>(1, std::min<int64_t>((ad->width + fewest - 1) / fewest, ADAPT_WG / (items * shape->groups)));
+  shape->splits = (int)std::max<int64_t>(1, std::min<int64_t>((ad->width + ADAPT_SPLIT - 1) / ADAPT_SPLIT, ADAPT_WG / (items * shape->groups)));
   shape->split_channels = ((ad->width + shape->splits - 1) / shape->splits + 63) / 64 * 64;
   shape->splits = (ad->width + shape->split_channels - 1) / shape->split_channels;
   shape->scratch = std::max<size_t>((size_t)max_items * ODMA_ADAPTER_ITEM_ROWS * shape->flat * sizeof(float) * shape->splits, 256);
@@ -93,7 +104,9 @@ const char* adapt_shape(const odma_adapters_t* ad, int elem_bytes, int64_t n_row
     for (int p = 0; p < ad->n_parts; ++p) n += (ad->part_start[p + 1] - ad->part_start[p] + columns - 1) / columns;
     return n;
   };
-  shape->few = n_rows >= 0 && n_rows <= ADAPT_FEW && ad->rank <= 16 && items <= 1024 && cols <= 1 << 17;
+  const int rank_bytes = ad->rank * elem_bytes;
+  shape->few = items <= 1024 && cols <= 1 << 17 && (rank_bytes <= 32 ? n_rows >= 0 && n_rows <= ADAPT_FEW : rank_bytes <= 64 ? n_rows >= 0 && n_rows <= ADAPT_FEW / 8
+               : ad->rank <= 64 && n_rows >= ADAPT_FEW / 32 && n_rows <= ADAPT_FEW / 8);
   shape->stream = n_rows * cols * elem_bytes > (int64_t)4 << 20 && items * cols / 512 >= ADAPT_UP_WG;
   shape->chunk_columns = shape->few ? 512 : 64;
   if (shape->few)
@@ -118,7 +131,10 @@ template <typename T>
 int launch_adapt(const char* where, const AdaptArgs& a, const AdaptShape& shape, hipStream_t s) {
   hipError_t e;
   if (shape.few) {
-    hipLaunchKernelGGL((adapt_few_kernel<T>), dim3((unsigned)(few_sixteens(a.n_rows, a.max_items) * shape.chunks)), dim3(512), 0, s, a);
+    const dim3 grid((unsigned)(few_sixteens(a.n_rows, a.max_items) * shape.chunks));
+    if (a.rank <= 16) hipLaunchKernelGGL((adapt_few_kernel<T, 1>), grid, dim3(512), 0, s, a);
+    else if (a.rank <= 32) hipLaunchKernelGGL((adapt_few_kernel<T, 2>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((adapt_few_kernel<T, 4>), grid, dim3(512), 0, s, a);
     e = hipGetLastError();
     return e == hipSuccess ? ODMA_OK : hip_fail(where, e);
   }

@@ -20,7 +20,14 @@ constexpr int64_t MAX_ROWS = (int64_t)1 << 22;   // (a launch has fewer than 2^3
 constexpr int32_t MAX_VOCAB = 1 << 24;
 constexpr int PART_UNIT = 2048;       // elements of the shortest part: a piece or two for every thread of four waves
 
-constexpr int SCORE_ROWS_8 = 512, SCORE_ROWS_16 = 256, SCORE_W = 16, SCORE_WAVES = 4096;
+// Waves of a work-group and parts of a row: as many waves as a chip that has few rows can hold, in one work-group for each compute unit where
+// there are about as many rows (16 waves), two (8), or more (4).  Rows of fewer tokens than SCORE_WHOLE stay whole, others are cut where
+// rows are fewer than work-groups.  us a call, 20 alternatives, bf16: 256 rows x 128 000 22 with 16 waves, 27 with 8 or 16 in
+// two parts, 33 with 4 in four; 300 x 128 000 33 (8), 36 (4); 512 x 128 000 34 (8), 41 (16), 45 (4); 8 rows x 128 000 11.5 in 63 parts of 4 waves, 12.3 of 8;
+// whole against cut: 1 x 32 003 9.1 and 9.9, fp32 11.0 and 10.0; 100 x 32 003 10.5 and 13.5; 1 x 3 001 7.2 and 9.7; 1 x 65 003 12.4 and 9.9.
+constexpr int SCORE_ROWS_4 = 512, SCORE_ROWS_8 = 256, SCORE_ROWS_16 = 16, SCORE_WHOLE = 32768;
+constexpr int SCORE_WAVES = 4096;     // of a launch, where rows are cut
+
 struct ScoreShape {
   int waves, parts, part_len;
   size_t states, scratch;
@@ -31,8 +38,9 @@ const char* score_shape(int64_t n_rows, int32_t vocab, int32_t n_top, ScoreShape
   if (n_top < 0 || n_top > ODMA_MAX_ALTERNATIVES || n_top > vocab) return "0 to ODMA_MAX_ALTERNATIVES alternatives, of the vocabulary";
   const int64_t units = (vocab + PART_UNIT - 1) / PART_UNIT;
   const int64_t rows = std::max<int64_t>(n_rows, 1);
-  shape->waves = rows > SCORE_ROWS_8 ? 4 : rows > SCORE_ROWS_16 ? 8 : rows * SCORE_PARTS >= 1024 ? SCORE_W : 4;
-  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({units, SCORE_PARTS, SCORE_WAVES / shape->waves / rows}));
+  const bool whole = vocab <= SCORE_WHOLE;
+  shape->waves = rows > SCORE_ROWS_4 ? 4 : rows > SCORE_ROWS_8 ? 8 : rows >= SCORE_ROWS_16 || whole ? 16 : 4;
+  const int64_t parts = whole ? 1 : std::max<int64_t>(1, std::min<int64_t>({units, SCORE_PARTS, SCORE_WAVES / shape->waves / rows}));
   shape->part_len = (int)((units + parts - 1) / parts * PART_UNIT);
   shape->parts = (vocab + shape->part_len - 1) / shape->part_len;
   shape->states = ((size_t)n_rows * shape->parts * sizeof(float4) + 255) / 256 * 256;

@@ -171,6 +171,11 @@ SHAPES = [
     ([33, 90], 3, 136, [208], 128),
     ([5, 70], 2, 264, [96], 256),
     ([1, 2, 3, 0, 5], 4, 8, [16, 32], 8),
+    # items of several runs of 16 rows, and more items than a wave has lanes, in the launch for few rows
+    ([17, 40, 64, 65, 1, 200, 33], 4, 520, [1104, 64], 16),
+    ([1, 2, 3] * 70, 200, 264, [64, 4112], 8),
+    ([2] * 100, 9, 2056, [528, 32], 32),
+    ([3] * 50, 60, 1032, [1040], 64),
 ]
 
 
@@ -196,11 +201,22 @@ def test_many_items(typ):
 
 
 @pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("rank", [8, 48])
+def test_long_calls(rank, typ):
+    """Rows that pass by the caches, in whole chunks of columns."""
+    rng = np.random.default_rng(4)
+    rows = rng.integers(0, 150, 300)
+    c = Case(typ, rng.integers(-1, 6, 300), rows, 6, 264, [1040, 512], rank, pads=(8, 16, 24))
+    assert c.total > 10000 and len(c.items) * 1552 / 512 >= 1024
+    c.run().check()
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
 def test_ragged_ranks(typ):
     """Weights behind an adapter's rank are NaN and infinities here, and are not there."""
     for rank, ranks in ((16, [16, 8, 0, -3, 99, 9]), (64, [8, 64, 40, 1, 24, 33])):
-        for whole in (True, False):
-            Case(typ, np.arange(12) % 6, [3, 1, 70, 2, 9, 20] * 2, 6, 328, [64, 48], rank, ranks=ranks, whole=whole).run().check()
+        for whole, more in ((True, 1), (False, 1), (True, 60)):
+            Case(typ, np.arange(12) % 6, [3 * more, 1, 70, 2, 9, 20] * 2, 6, 328, [64, 48], rank, ranks=ranks, whole=whole).run().check()
 
 
 @pytest.mark.parametrize("typ", ["bf16", "f32"])

@@ -111,7 +111,8 @@ def test_small_vocabularies(vocab, typ):
 
 @pytest.mark.parametrize("typ", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,vocab,top,scale", [(1, 128000, 20, 1.0), (2, 50001, 64, 0.7), (5, 32003, 5, 1.6), (17, 131072, 20, 1.0),
-                                                  (300, 9001, 20, 1.0), (700, 3001, 64, 2.5), (1025, 2500, 3, 1.0), (2, 262147, 1, 1.0)])
+                                                  (300, 9001, 20, 1.0), (300, 40001, 20, 1.0), (1, 32768, 64, 1.0),
+                                                  (16, 32769, 20, 1.0), (256, 20001, 20, 1.0), (700, 3001, 64, 2.5), (1025, 2500, 3, 1.0), (2, 262147, 1, 1.0)])
 def test_parts_and_whole_rows(rows, vocab, top, scale, typ):
     x = some(rows, vocab + vocab % 2, typ, seed=rows)
     gen = torch.Generator().manual_seed(7)
@@ -124,7 +125,7 @@ def test_parts_and_whole_rows(rows, vocab, top, scale, typ):
 @pytest.mark.parametrize("rows", [1, 1024])                      # cut into parts, whole
 @pytest.mark.parametrize("order", ["up", "down", "equal", "two values", "zeros of both signs", "low", "steps"])
 def test_ordered_and_equal_logits(order, rows, typ):
-    vocab = 20011 if rows == 1 else 5003
+    vocab = 40011 if rows == 1 else 5003
     i = torch.arange(vocab, dtype=torch.float64)
     x = {"up": i / 128, "down": -i / 128, "equal": torch.full_like(i, -2.5), "two values": (i % 3 == 1).double(),
          "zeros of both signs": torch.where(i % 2 == 0, -0.0, 0.0), "low": torch.where(i % 7 == 3, i / 1000, FULL),

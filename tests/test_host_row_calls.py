@@ -143,9 +143,19 @@ def test_adapt_rows(runtime):  # noqa: F811
         adapt(p, y=K, ys=96), adapt(f, xs=516, bs=100, ys=100), adapt(p, xs=0, bs=0)
         two = launched(lambda: adapt(p, ys=256, ad=make(rank=256, part_cols=(64, 64, 64, 64), width=32768)))
         assert ["down" in two[0][0], "up" in two[1][0]] == [True, True] and len(two) == 2 and two[1][2] == 32768
-        for at in (0, 1):
+        # few rows take one launch, by the bytes of a channel of the ranks: up to 4096 rows of 32, 512 of 64, from 128 on for more up to rank 64
+        for pool, n, rank, few in ((p, 1, 16, True), (p, 4096, 16, True), (p, 4097, 16, False), (p, 512, 32, True), (p, 513, 32, False), (p, 127, 64, False),
+                                   (p, 128, 64, True), (p, 512, 40, True), (p, 513, 64, False), (p, 200, 72, False), (f, 512, 16, True), (f, 513, 16, False),
+                                   (f, 127, 32, False), (f, 128, 32, True), (f, 128, 64, True), (f, 128, 72, False)):
+            got = launched(lambda: adapt(pool, n=n, ad=make(rank=rank)))
+            assert len(got) == (1 if few else 2) and ("few" in got[0][0]) == few, (n, rank, got)
+        assert len(launched(lambda: adapt(p, max_items=1025))) == 2
+        assert launched(lambda: adapt(p, n=100))[0][1] == (2 * 16, 1, 1)       # 6 + 6 runs of 16 rows, in eights; two parts of a chunk of columns each
+        # long calls pass rows by the caches
+        assert "Lb1E" in launched(lambda: adapt(p, n=100000, max_items=1600, ys=4608, bs=4608, ad=make(part_cols=(3584, 512, 512))))[1][0]
+        for at, kw in ((0, {}), (0, dict(n=5000)), (1, dict(n=5000))):
             hip.fake_fail_launch(at)
-            assert fails(lambda: adapt(p))
+            assert fails(lambda: adapt(p, **kw))
     """)
 
 
@@ -170,13 +180,15 @@ def test_score_tokens(runtime):  # noqa: F811
         # results that nobody asks for
         score(p, tokens=None, lp=None, rank=None), score(p, top=0, ids=None, lps=None), score(p, ids=None), score(p, lps=None, ent=None)
         score(p, n=1, stride=0), score(p, logits=Q + 2, stride=32001), score(p, logits=Q + 4, stride=32001, dtype=B.F32, scale=2.0 ** -24)
-        # few rows are cut into parts of 2048 tokens or more, 64 at most, up to 1024 work-groups, which a second launch joins
-        for n, vocab, wg in ((1, 2048, 1), (1, 2049, 2), (1, 32000, 16), (1, 1 << 24, 64), (64, 32000, 1024), (100, 32000, 800), (513, 32000, 513),
-                             (4096, 1 << 20, 4096), (1 << 22, 5, 1 << 22)):
+        # rows of up to 32 768 tokens are whole; longer ones of few rows are cut into parts of 2048 or more, 64 at most, which a second launch
+        # joins.  Waves of a work-group: 4, of 16 to 256 rows (and of short rows up to there) 16, up to 512 rows 8
+        for n, vocab, wg, waves in ((1, 5, 1, 16), (1, 32768, 1, 16), (1, 32769, 17, 4), (1, 1 << 24, 64, 4), (15, 128000, 945, 4), (16, 128000, 256, 16),
+                                    (100, 128000, 200, 16), (256, 128000, 256, 16), (256, 300, 256, 16), (257, 300, 257, 8), (512, 128000, 512, 8),
+                                    (513, 128000, 513, 4), (1 << 22, 5, 1 << 22, 4)):
             got = launched(lambda: score(p, n=n, vocab=vocab, stride=vocab))
-            assert "score_kernel" in got[0][0] and got[0][1] == (wg, 1, 1), (n, vocab, got)
+            assert "score_kernel" in got[0][0] and f"Li{waves}E" in got[0][0] and got[0][1] == (wg, 1, 1), (n, vocab, got)
             assert len(got) == (2 if wg > n else 1) and (wg == n or (got[1][1] == (n, 1, 1) and "join" in got[1][0]))
         for at in (0, 1):
             hip.fake_fail_launch(at)
-            assert fails(lambda: score(p))
+            assert fails(lambda: score(p, vocab=128000, stride=128000))
     """)
