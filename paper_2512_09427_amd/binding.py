@@ -203,7 +203,7 @@ def _rows(t) -> Optional[int]:
         return t
     if not t.is_cuda:
         raise TypeError("DEVICE argument must be a CUDA tensor")
-    if t.dim() and t.stride(-1) != 1:
+    if not t.is_contiguous() and t.dim() and t.stride(-1) != 1:
         raise ValueError("the last dimension of a DEVICE argument must be contiguous")
     return t.data_ptr()
 

@@ -54,15 +54,18 @@ void launch_add_norm(const AddNormArgs& a, bool many, hipStream_t s) {
   else launch_add_norm<T, R, 16, 4>(a, s);
 }
 
-// Up to so many rows, both products in one launch (adapt_few_kernel), by the bytes of a channel of an adapter's ranks, which every work-group of
-// it reads: 32 (bf16, rank 16), 64, more.  Against the two launches, us a call, 3584 channels, 4608 columns in three parts, requests / adapters:
-//   32: 1 / 4 6.5 and 8.9, 64 / 64 11.2 and 18.3, 1 024 / 32 17.2 and 22.7, 4 096 / 32 42.9 and 50.4, 8 192 / 32 72.3 and 64.2
-//   64 (rank 32): 64 / 16 9.7 and 12.2, 256 / 32 11.4 and 20.4, 1 024 / 32 28.6 and 27.5;  fp32, rank 16: 64 / 64 18 and 23
-//   128 (rank 64): 1 / 4 14.2 and 10.7, 64 / 16 15.2 and 15.2, 256 / 32 16.5 and 29.7, 1 024 / 32 54.9 and 46.0;  fp32 28.6 and 12.3, 30 and 19, 33 and 46, 100 and 93
-constexpr int ADAPT_FEW = 4096;
-// Work-groups that it is cut into, by the adapters that a batch may have.  64 / 64 as above 11.0 us with 260 and 12.3 with 390; 256 / 32 9.1 with 360
-// and 11.4 with 160.
-constexpr int ADAPT_FEW_WG = 360;
+// Both products in one launch (adapt_few_kernel) or in two, by the rows and by the bytes of a channel of an adapter's ranks, which every work-group
+// of the one launch reads.  One and two, us a call, 3584 channels, 4608 columns in three parts (or 1024 in one), requests / adapters:
+//   32 bytes (bf16, rank 16): 1 / 4 6.5 and 8.9, 64 / 64 11.0 and 18.3, 1 024 / 32 17.2 and 22.7, 4 096 / 32 42.9 and 50.4, 8 192 / 32 72.3 and 64.2
+//   64 (bf16, rank 32): 1 / 4 8.4 and 10.0, 64 / 16 9.8 and 12.1, 256 / 32 11.5 and 20.1, 1 024 / 32 23.5 and 27.6, 4 096 / 32 59.6 and 57.6
+//   128 (bf16, rank 64): 1 / 4 14.1 and 10.8, 64 / 16 15.1 and 14.9, 256 / 32 16.2 and 28.8, 1 024 / 32 38.6 and 45.7, 4 096 / 32 109 and 99
+//   256 (fp32, rank 64): 1 / 4 28.5 and 14.2, 64 / 16 30 and 20, 256 / 32 32 and 47, 1 024 / 32 79 and 94 (31.6 and 30.7), 4 096 / 32 179 and 184 (75 and 68)
+constexpr int ADAPT_FEW = 4096, ADAPT_FEW_WIDE = 2560, ADAPT_FEW_FROM = 128;
+// Work-groups that it is cut into, as far as the adapters that a batch may have let it be known.  Two share a compute unit with ranks up to 16: 64 / 64 as above
+// 11.0 us with 260 and 12.3 with 390, 256 / 32 9.1 with 360 and 11.4 with 160.  With more it is one; parts narrower than the others' runs of columns
+// leave short work-groups that fill in: 1 024 / 32 of rank 64 38.6 us with 384 and 55 with 256, but 2 300 fp32 rows beside 1024 columns
+// 26.8 with 286 and 22.8 with 143.
+constexpr int ADAPT_FEW_WG = 360, ADAPT_FEW_WG_PARTS = 400, ADAPT_FEW_WG_WIDE = 256;
 // The first of two launches: fewest channels of a cut, and work-groups up to which channels are cut: every cut is one more array for the second
 // launch to add up.  256 / 32 of rank 64 29.7 us with 512 and 32.8 with 256; 24 fp32 prompts of 2 300 rows 24.7 with 512 and 27.5 with 1024.
 constexpr int ADAPT_SPLIT = 512, ADAPT_WG = 512;
@@ -105,12 +108,13 @@ const char* adapt_shape(const odma_adapters_t* ad, int elem_bytes, int64_t n_row
     return n;
   };
   const int rank_bytes = ad->rank * elem_bytes;
-  shape->few = items <= 1024 && cols <= 1 << 17 && (rank_bytes <= 32 ? n_rows >= 0 && n_rows <= ADAPT_FEW : rank_bytes <= 64 ? n_rows >= 0 && n_rows <= ADAPT_FEW / 8
-               : ad->rank <= 64 && n_rows >= ADAPT_FEW / 32 && n_rows <= ADAPT_FEW / 8);
+  const int64_t fewest = rank_bytes <= 64 ? 0 : ADAPT_FEW_FROM, most = rank_bytes <= 32 ? ADAPT_FEW : ADAPT_FEW_WIDE;
+  shape->few = ad->rank <= 64 && n_rows >= fewest && n_rows <= most && items <= 1024 && cols <= 1 << 17;
   shape->stream = n_rows * cols * elem_bytes > (int64_t)4 << 20 && items * cols / 512 >= ADAPT_UP_WG;
   shape->chunk_columns = shape->few ? 512 : 64;
   if (shape->few)
-    while (shape->chunk_columns < 4096 && (std::min(items, n_rows) + n_rows / 64) * chunks_of(shape->chunk_columns) > ADAPT_FEW_WG) shape->chunk_columns *= 2;
+    while (shape->chunk_columns < 4096 && std::max(std::min(items, n_rows) + n_rows / 64, n_rows / 16) * chunks_of(shape->chunk_columns) >
+           (ad->rank <= 16 ? ADAPT_FEW_WG : ad->n_parts > 1 ? ADAPT_FEW_WG_PARTS : ADAPT_FEW_WG_WIDE)) shape->chunk_columns *= 2;
   else
     while (shape->chunk_columns < 512 && items * cols / shape->chunk_columns > ADAPT_UP_WG) shape->chunk_columns *= 2;
   if (items * std::max<int64_t>(chunks_of(shape->chunk_columns), shape->splits * shape->groups) > MAX_WG) return "too many items";

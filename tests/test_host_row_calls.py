@@ -143,10 +143,11 @@ def test_adapt_rows(runtime):  # noqa: F811
         adapt(p, y=K, ys=96), adapt(f, xs=516, bs=100, ys=100), adapt(p, xs=0, bs=0)
         two = launched(lambda: adapt(p, ys=256, ad=make(rank=256, part_cols=(64, 64, 64, 64), width=32768)))
         assert ["down" in two[0][0], "up" in two[1][0]] == [True, True] and len(two) == 2 and two[1][2] == 32768
-        # few rows take one launch, by the bytes of a channel of the ranks: up to 4096 rows of 32, 512 of 64, from 128 on for more up to rank 64
-        for pool, n, rank, few in ((p, 1, 16, True), (p, 4096, 16, True), (p, 4097, 16, False), (p, 512, 32, True), (p, 513, 32, False), (p, 127, 64, False),
-                                   (p, 128, 64, True), (p, 512, 40, True), (p, 513, 64, False), (p, 200, 72, False), (f, 512, 16, True), (f, 513, 16, False),
-                                   (f, 127, 32, False), (f, 128, 32, True), (f, 128, 64, True), (f, 128, 72, False)):
+        # few rows take one launch, by the bytes of a channel of the ranks: up to 4096 rows of 32, 2560 of 64, from 128 on for more up to rank 64
+        for pool, n, rank, few in ((p, 1, 16, True), (p, 4096, 16, True), (p, 4097, 16, False), (p, 1, 32, True), (p, 2560, 32, True), (p, 2561, 32, False),
+                                   (p, 127, 64, False), (p, 128, 64, True), (p, 2560, 40, True), (p, 2561, 64, False), (p, 200, 72, False),
+                                   (f, 1, 16, True), (f, 2560, 16, True), (f, 2561, 16, False), (f, 127, 32, False), (f, 128, 32, True), (f, 128, 64, True),
+                                   (f, 128, 72, False)):
             got = launched(lambda: adapt(pool, n=n, ad=make(rank=rank)))
             assert len(got) == (1 if few else 2) and ("few" in got[0][0]) == few, (n, rank, got)
         assert len(launched(lambda: adapt(p, max_items=1025))) == 2
