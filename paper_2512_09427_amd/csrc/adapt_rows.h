@@ -1,8 +1,8 @@
 // Low-rank adapters of many requests beside a shared projection:
 //   y[row, c] = base[row, c] + s_a sum_k up[a, c, k] h[row, k],   h[row, k] = sum_d down[a, k, d] x[row, d]
-// for the rows of every item (adapter_lists.h: up to 64 rows of one adapter), two launches.
+// for the rows of every item (adapter_lists.h: up to 64 rows of one adapter), in two launches, or in one where rows are few.
 //
-// The first forms h: ranks are the rows of the matrix product, an item's rows its columns.  The channels are cut between the waves of a
+// The first of two forms h: ranks are the rows of the matrix product, an item's rows its columns.  The channels are cut between the waves of a
 // work-group, which add up in LDS, and, where a batch has few items, between work-groups, whose parts stay apart in scratch: nothing is
 // added up in an order that changes.  The second stages an item's h in LDS, parts added up and scaled, and takes 64 columns a wave at
 // a time.  In bf16, h enters as two bf16 parts (value and rest: 16 bits), which fill the contraction of 32 that a rank of 16 would
@@ -32,6 +32,7 @@ struct AdaptArgs {
   int32_t part_start[ODMA_MAX_PARTS + 1];
   int32_t part_chunk[ODMA_MAX_PARTS + 1];   // second launch: chunks of columns in front of a part
   int32_t chunk_columns, chunks;
+  int32_t runs;                      // the one launch for few rows: runs of 16 rows of the grid
 };
 
 // An adapter's rank: a multiple of 8, up to that of the arrays.
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(256) void adapt_down_kernel(AdaptArgs a) {
   const int at = blockIdx.x / (a.splits * a.groups), cut = (int)blockIdx.x - at * a.splits * a.groups;
   const int4 item = a.items[at];
   const int adapter = item.x, first = item.y, count = min(item.z, ODMA_ADAPTER_ITEM_ROWS);
-  if (count <= 0 || (unsigned)adapter >= (unsigned)a.n_adapters) return;
+  if (count <= 0 || first < 0 || (unsigned)adapter >= (unsigned)a.n_adapters) return;
   const int lane = threadIdx.x & 63, wave = rfl(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const int split = cut % a.splits, group = cut / a.splits;
   // the lane's line of eight, and which of its pieces it loads
@@ -224,7 +225,7 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
   const int at = blockIdx.x / a.chunks, chunk = (int)blockIdx.x - at * a.chunks;
   const int4 item = a.items[at];
   const int adapter = item.x, first = item.y, count = min(item.z, ODMA_ADAPTER_ITEM_ROWS);
-  if (count <= 0 || (unsigned)adapter >= (unsigned)a.n_adapters) return;
+  if (count <= 0 || first < 0 || (unsigned)adapter >= (unsigned)a.n_adapters) return;
   const int lane = threadIdx.x & 63, wave = rfl(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const int flat = a.n_parts * a.rank, rank_a = rank_of(a, adapter);
   int part = 0;
@@ -374,185 +375,201 @@ __global__ __launch_bounds__(512, PT == 1 ? 4 : 2) void adapt_few_kernel(AdaptAr
   constexpr int TWO = PT < 2 ? PT : 2, WAVE = (16 + TWO * 16) * 8;   // of a wave in LDS: 16 rows and 16 or 32 ranks of 128 bytes, in pieces
   __shared__ __attribute__((aligned(16))) uint4v stage[WAVES * WAVE];
   __shared__ __attribute__((aligned(16))) uint4v hs[PT * 64];
-  int left, chunk;
-  item_of(a.chunks, left, chunk);
-  const int lane = threadIdx.x & 63, wave = rfl(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
-  int adapter = ODMA_ADAPTER_NONE, first = 0, count = 0;
-  for (int i0 = 0; i0 < a.max_items; i0 += 64) {
-    int4 item = make_int4(ODMA_ADAPTER_NONE, 0, 0, 0);
-    if (i0 + lane < a.max_items) item = a.items[i0 + lane];
-    if ((unsigned)item.x >= (unsigned)a.n_adapters) item.z = 0;
-    const int subs = (min(max(item.z, 0), ODMA_ADAPTER_ITEM_ROWS) + 15) / 16;
-    // runs of the items in front of this one (0 to 4 each), summed by their binary digits
-    int before = 0, all = 0;
+  int run, chunk;
+  item_of(a.chunks, run, chunk);
+  const int wave = rfl(threadIdx.x >> 6);
+  for (;; run += a.runs) {                                   // (lists of more rows than there are go on behind the grid's)
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));                           // (what follows from it is formed anew: nothing of it waits in registers for a second turn)
+    const int m = lane & 15, g = lane >> 4;
+    // ---- the run's item: 256 items a round
+    int adapter = ODMA_ADAPTER_NONE, first = 0, count = 0, left = run;
+    bool last = false;                                       // no run of the next round
+    for (int i0 = 0; i0 < a.max_items && count == 0; i0 += 256) {
+      int4 item[4];
 #pragma unroll
-    for (int bit = 0; bit < 3; ++bit) {
-      const unsigned long long set = __builtin_amdgcn_ballot_w64(subs >> bit & 1);
-      before += (int)__builtin_amdgcn_mbcnt_hi((unsigned)(set >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)set, 0)) << bit;
-      all += __builtin_popcountll(set) << bit;
-    }
-    if (left < all) {
-      const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(left < before + subs));
-      const int sub = left - __builtin_amdgcn_readlane(before, l);
-      adapter = __builtin_amdgcn_readlane(item.x, l);
-      first = __builtin_amdgcn_readlane(item.y, l) + sub * 16;
-      count = min(min(__builtin_amdgcn_readlane(item.z, l), ODMA_ADAPTER_ITEM_ROWS) - sub * 16, 16);
-      break;
-    }
-    left -= all;
-  }
-  if (count <= 0) return;
-  const int flat = a.n_parts * a.rank, rank_a = rank_of(a, adapter);
-  int part = 0;
-  while (part + 1 < a.n_parts && chunk >= a.part_chunk[part + 1]) ++part;
-  const int c0 = a.part_start[part] + (chunk - a.part_chunk[part]) * a.chunk_columns;
-  const int c1 = min(c0 + a.chunk_columns, a.part_start[part + 1]), cols = a.part_start[a.n_parts];
-  uint4v* mine = stage + wave * WAVE;
-  const int line8 = lane >> 3, piece8 = (lane & 7) ^ line8;
-  const T* arow = (const T*)a.down + ((int64_t)adapter * flat + part * a.rank + line8) * a.width + piece8 * X;
-  const int line = lane / LINE, piece = lane % LINE;
-  // one round of loads for the rows' numbers, beside down and up; then x and base
-  int xnumber[2], row[LOADS];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) xnumber[i] = a.row_order[first + min(8 * i + line8, count - 1)];
-#pragma unroll
-  for (int i = 0; i < LOADS; ++i) row[i] = a.row_order[first + min(i * (64 / LINE) + line, count - 1)];
-  uint4v av[AHEAD][2 * PT], xv[AHEAD][2], in[LOADS], uv[PT][4];
-  auto load_ranks = [&](int j, int k) {
-    const bool there = k + piece8 * X < a.width;             // (a width is whole pieces)
-#pragma unroll
-    for (int i = 0; i < 2 * PT; ++i) {
-      av[j][i] = uint4v{0, 0, 0, 0};
-      if (8 * i < rank_a && there) av[j][i] = *(const uint4v*)(arow + (int64_t)(8 * i) * a.width + k);
-    }
-  };
-  auto load_up = [&](int cs) {
-#pragma unroll
-    for (int s = 0; s < PT; ++s) {
-      const int q = 4 * s + g, p = X == 8 && q >= 2 * PT ? q - 2 * PT : q;   // (bf16: pieces of ranks for the value and for the rest of h)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        uv[s][t] = uint4v{0, 0, 0, 0};
-        if (p * X < rank_a && cs + t * 16 + m < c1) uv[s][t] = *(const uint4v*)((const T*)a.up + ((int64_t)adapter * cols + cs + t * 16 + m) * a.rank + p * X);
+      for (int j = 0; j < 4; ++j) {
+        item[j] = make_int4(ODMA_ADAPTER_NONE, 0, 0, 0);
+        if (i0 + j * 64 + lane < a.max_items) item[j] = a.items[i0 + j * 64 + lane];
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int rows = (unsigned)item[j].x < (unsigned)a.n_adapters && item[j].y >= 0 ? min(max(item[j].z, 0), ODMA_ADAPTER_ITEM_ROWS) : 0;
+        const int subs = (rows + 15) / 16;
+        // runs of the items in front of this one (0 to 4 each), summed by their binary digits
+        int before = 0, all = 0;
+#pragma unroll
+        for (int bit = 0; bit < 3; ++bit) {
+          const unsigned long long set = __builtin_amdgcn_ballot_w64(subs >> bit & 1);
+          before += (int)__builtin_amdgcn_mbcnt_hi((unsigned)(set >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)set, 0)) << bit;
+          all += __builtin_popcountll(set) << bit;
+        }
+        if (count == 0 && left < all) {
+          const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(left < before + subs));
+          const int sub = left - __builtin_amdgcn_readlane(before, l);
+          adapter = __builtin_amdgcn_readlane(item[j].x, l);
+          first = __builtin_amdgcn_readlane(item[j].y, l) + sub * 16;
+          count = min(__builtin_amdgcn_readlane(rows, l) - sub * 16, 16);
+        }
+        left -= all;
+      }
+      last = i0 + 256 >= a.max_items && left + a.runs >= 0;  // (left: this run behind all that there are)
     }
-  };
+    if (count == 0) return;
+    const int flat = a.n_parts * a.rank, rank_a = rank_of(a, adapter);
+    int part = 0;
+    while (part + 1 < a.n_parts && chunk >= a.part_chunk[part + 1]) ++part;
+    const int c0 = a.part_start[part] + (chunk - a.part_chunk[part]) * a.chunk_columns;
+    const int c1 = min(c0 + a.chunk_columns, a.part_start[part + 1]), cols = a.part_start[a.n_parts];
+    uint4v* mine = stage + wave * WAVE;
+    const int line8 = lane >> 3, piece8 = (lane & 7) ^ line8;
+    const T* arow = (const T*)a.down + ((int64_t)adapter * flat + part * a.rank + line8) * a.width + piece8 * X;
+    const int line = lane / LINE, piece = lane % LINE;
+    // one round of loads for the rows' numbers, beside down and up; then x and base
+    int xnumber[2], row[LOADS];
 #pragma unroll
-  for (int j = 0; j < AHEAD; ++j) load_ranks(j, (j * WAVES + wave) * CHUNK);
-  int cs = c0 + wave * 64;
-  if (PT == 1 && cs < c1) load_up(cs);
-  __builtin_amdgcn_sched_barrier(0);
-  const T* xrow[2];
+    for (int i = 0; i < 2; ++i) xnumber[i] = a.row_order[first + min(8 * i + line8, count - 1)];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) xrow[i] = (const T*)a.x + (xnumber[i] >= 0 && xnumber[i] < a.n_rows ? xnumber[i] : 0) * a.x_stride + piece8 * X;
+    for (int i = 0; i < LOADS; ++i) row[i] = a.row_order[first + min(i * (64 / LINE) + line, count - 1)];
+    uint4v av[AHEAD][2 * PT], xv[AHEAD][2], in[LOADS], uv[PT][4];
+    auto load_ranks = [&](int j, int k) {
+      const bool there = k + piece8 * X < a.width;             // (a width is whole pieces)
 #pragma unroll
-  for (int i = 0; i < LOADS; ++i)
-    if (i * (64 / LINE) + line >= count || row[i] >= a.n_rows) row[i] = -1;
-  auto load_x = [&](int j, int k) {
-    const bool there = k + piece8 * X < a.width;
+      for (int i = 0; i < 2 * PT; ++i) {
+        av[j][i] = uint4v{0, 0, 0, 0};
+        if (8 * i < rank_a && there) av[j][i] = *(const uint4v*)(arow + (int64_t)(8 * i) * a.width + k);
+      }
+    };
+    auto load_up = [&](int cs) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      xv[j][i] = uint4v{0, 0, 0, 0};
-      if (8 * i < count && there) xv[j][i] = *(const uint4v*)(xrow[i] + k);
-    }
-  };
-  auto load_base = [&](int cs) {
-    const int c = cs + piece * X;
+      for (int s = 0; s < PT; ++s) {
+        const int q = 4 * s + g, p = X == 8 && q >= 2 * PT ? q - 2 * PT : q;   // (bf16: pieces of ranks for the value and for the rest of h)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          uv[s][t] = uint4v{0, 0, 0, 0};
+          if (p * X < rank_a && cs + t * 16 + m < c1) uv[s][t] = *(const uint4v*)((const T*)a.up + ((int64_t)adapter * cols + cs + t * 16 + m) * a.rank + p * X);
+        }
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) load_ranks(j, (j * WAVES + wave) * CHUNK);
+    int cs = c0 + wave * 64;
+    if (PT == 1 && cs < c1) load_up(cs);
+    __builtin_amdgcn_sched_barrier(0);
+    const T* xrow[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) xrow[i] = (const T*)a.x + (xnumber[i] >= 0 && xnumber[i] < a.n_rows ? xnumber[i] : 0) * a.x_stride + piece8 * X;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
-      if (row[i] >= 0 && c < c1) in[i] = *(const uint4v*)((const T*)a.base + row[i] * a.base_stride + c);
-  };
+      if (i * (64 / LINE) + line >= count || row[i] >= a.n_rows) row[i] = -1;
+    auto load_x = [&](int j, int k) {
+      const bool there = k + piece8 * X < a.width;
 #pragma unroll
-  for (int j = 0; j < AHEAD; ++j) load_x(j, (j * WAVES + wave) * CHUNK);
-  if (cs < c1) load_base(cs);
-  const float scale = a.scale ? a.scale[adapter] : 1.f;
-  float4v acc[PT];
-#pragma unroll
-  for (int t = 0; t < PT; ++t) acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
-  for (int k = wave * CHUNK; k < a.width;) {
-#pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      if (k >= a.width) break;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) mine[i * 64 + lane] = xv[j][i];
-#pragma unroll
-      for (int t0 = 0; t0 < PT; t0 += TWO) {
-#pragma unroll
-        for (int i = 0; i < 2 * TWO; ++i) mine[(2 + i) * 64 + lane] = av[j][2 * t0 + i];
-        if (t0 + TWO >= PT && k + AHEAD * WAVES * CHUNK < a.width) {
-          load_ranks(j, k + AHEAD * WAVES * CHUNK);
-          load_x(j, k + AHEAD * WAVES * CHUNK);
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const uint4v b = mine[m * 8 + ((4 * c + g) ^ (m & 7))];
-#pragma unroll
-          for (int t = 0; t < TWO; ++t) acc[t0 + t] = Op::mma(mine[(16 + t * 16 + m) * 8 + ((4 * c + g) ^ (m & 7))], b, acc[t0 + t]);
-        }
+      for (int i = 0; i < 2; ++i) {
+        xv[j][i] = uint4v{0, 0, 0, 0};
+        if (8 * i < count && there) xv[j][i] = *(const uint4v*)(xrow[i] + k);
       }
-      k += WAVES * CHUNK;
-    }
-  }
-  // ---- the waves' sums, scaled, as the second product takes them; a lane holds ranks 4 g .. 4 g + 3 of row m
-  float4v* parts = (float4v*)stage;
-  if (PT > 1 && cs < c1) load_up(cs);
-  __syncthreads();
+    };
+    auto load_base = [&](int cs) {
+      const int c = cs + piece * X;
 #pragma unroll
-  for (int t = 0; t < PT; ++t) parts[(wave * PT + t) * 64 + lane] = acc[t];
-  __syncthreads();
-  if (wave < PT) {
-    float4v sum = parts[wave * 64 + lane];
+      for (int i = 0; i < LOADS; ++i)
+        if (row[i] >= 0 && c < c1) in[i] = *(const uint4v*)((const T*)a.base + row[i] * a.base_stride + c);
+    };
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) sum += parts[(w * PT + wave) * 64 + lane];
-    float v[8];
+    for (int j = 0; j < AHEAD; ++j) load_x(j, (j * WAVES + wave) * CHUNK);
+    if (cs < c1) load_base(cs);
+    const float scale = a.scale ? a.scale[adapter] : 1.f;
+    float4v acc[PT];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[e] = 16 * wave + 4 * g < rank_a ? sum[e] * scale : 0.f;
-      v[4 + e] = 0.f;
-    }
-    if constexpr (X == 8) {
-      uint4v hi, lo;
-      split_ranks(v, hi, lo);
-      uint2v* to = (uint2v*)hs + ((2 * wave + (g >> 1)) * 16 + m) * 2 + (g & 1);
-      *to = uint2v{hi[0], hi[1]};
-      to[PT * 64] = uint2v{lo[0], lo[1]};
-    } else {
-      hs[(4 * wave + g) * 16 + m] = __builtin_bit_cast(uint4v, float4v{v[0], v[1], v[2], v[3]});
-    }
-  }
-  __syncthreads();
-  float4v* turn = (float4v*)mine;                            // (the parts have been read)
-  while (cs < c1) {
-    float4v sum[4];
+    for (int t = 0; t < PT; ++t) acc[t] = float4v{0.f, 0.f, 0.f, 0.f};
+    for (int k = wave * CHUNK; k < a.width;) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      sum[t] = float4v{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < AHEAD; ++j) {
+        if (k >= a.width) break;
 #pragma unroll
-      for (int s = 0; s < PT; ++s) sum[t] = Op::mma(uv[s][t], hs[s * 64 + lane], sum[t]);
-    }
-    uint4v old[LOADS];
+        for (int i = 0; i < 2; ++i) mine[i * 64 + lane] = xv[j][i];
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) old[i] = in[i];
-    const int now = cs + piece * X;
-    cs += WAVES * 64;
-    if (cs < c1) {
-      load_up(cs);
-      load_base(cs);
-    }
+        for (int t0 = 0; t0 < PT; t0 += TWO) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) turn[m * 16 + ((4 * t + g) ^ m)] = sum[t];
+          for (int i = 0; i < 2 * TWO; ++i) mine[(2 + i) * 64 + lane] = av[j][2 * t0 + i];
+          if (t0 + TWO >= PT && k + AHEAD * WAVES * CHUNK < a.width) {
+            load_ranks(j, k + AHEAD * WAVES * CHUNK);
+            load_x(j, k + AHEAD * WAVES * CHUNK);
+          }
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int n = i * (64 / LINE) + line;
-      float d[X];
+          for (int c = 0; c < 2; ++c) {
+            const uint4v b = mine[m * 8 + ((4 * c + g) ^ (m & 7))];
 #pragma unroll
-      for (int e = 0; e < X / 4; ++e) {
-        const float4v four = turn[n * 16 + ((piece * (X / 4) + e) ^ n)];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) d[4 * e + k] = four[k];
+            for (int t = 0; t < TWO; ++t) acc[t0 + t] = Op::mma(mine[(16 + t * 16 + m) * 8 + ((4 * c + g) ^ (m & 7))], b, acc[t0 + t]);
+          }
+        }
+        k += WAVES * CHUNK;
       }
-      if (row[i] >= 0 && now < c1) *(uint4v*)((T*)a.y + row[i] * a.y_stride + now) = added((const T*)nullptr, old[i], d);
     }
+    // ---- the waves' sums, scaled, as the second product takes them; a lane holds ranks 4 g .. 4 g + 3 of row m
+    float4v* parts = (float4v*)stage;
+    if (PT > 1 && cs < c1) load_up(cs);
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < PT; ++t) parts[(wave * PT + t) * 64 + lane] = acc[t];
+    __syncthreads();
+    if (wave < PT) {
+      float4v sum = parts[wave * 64 + lane];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) sum += parts[(w * PT + wave) * 64 + lane];
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = 16 * wave + 4 * g < rank_a ? sum[e] * scale : 0.f;
+        v[4 + e] = 0.f;
+      }
+      if constexpr (X == 8) {
+        uint4v hi, lo;
+        split_ranks(v, hi, lo);
+        uint2v* to = (uint2v*)hs + ((2 * wave + (g >> 1)) * 16 + m) * 2 + (g & 1);
+        *to = uint2v{hi[0], hi[1]};
+        to[PT * 64] = uint2v{lo[0], lo[1]};
+      } else {
+        hs[(4 * wave + g) * 16 + m] = __builtin_bit_cast(uint4v, float4v{v[0], v[1], v[2], v[3]});
+      }
+    }
+    __syncthreads();
+    float4v* turn = (float4v*)mine;                            // (the parts have been read)
+    while (cs < c1) {
+      float4v sum[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        sum[t] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < PT; ++s) sum[t] = Op::mma(uv[s][t], hs[s * 64 + lane], sum[t]);
+      }
+      uint4v old[LOADS];
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) old[i] = in[i];
+      const int now = cs + piece * X;
+      cs += WAVES * 64;
+      if (cs < c1) {
+        load_up(cs);
+        load_base(cs);
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) turn[m * 16 + ((4 * t + g) ^ m)] = sum[t];
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int n = i * (64 / LINE) + line;
+        float d[X];
+#pragma unroll
+        for (int e = 0; e < X / 4; ++e) {
+          const float4v four = turn[n * 16 + ((piece * (X / 4) + e) ^ n)];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) d[4 * e + k] = four[k];
+        }
+        if (row[i] >= 0 && now < c1) *(uint4v*)((T*)a.y + row[i] * a.y_stride + now) = added((const T*)nullptr, old[i], d);
+      }
+    }
+    if (last) return;
+    __syncthreads();                                         // (LDS has been read)
   }
 }
 

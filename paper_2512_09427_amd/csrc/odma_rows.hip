@@ -72,8 +72,8 @@ constexpr int ADAPT_SPLIT = 512, ADAPT_WG = 512;
 // The second: work-groups up to which columns are cut, down to 64.  1 024 / 32 of rank 64 46 us with 1024 and 60 with 512.
 constexpr int ADAPT_UP_WG = 1024;
 
-// Runs of 16 rows of items, at most, in eights
-inline int64_t few_sixteens(int64_t n_rows, int64_t items) { return (n_rows / 16 + std::min(items, n_rows) + 7) / 8 * 8; }
+// Runs of 16 rows of the items, as many as there can be if the lists are of these rows, in eights
+inline int64_t few_runs(int64_t n_rows, int64_t items) { return (n_rows / 16 + std::min(items, n_rows) + 7) / 8 * 8; }
 
 // What the adapters' launches look like, or why they are refused.  n_rows < 0: for the scratch of any number of rows.
 struct AdaptShape {
@@ -135,7 +135,7 @@ template <typename T>
 int launch_adapt(const char* where, const AdaptArgs& a, const AdaptShape& shape, hipStream_t s) {
   hipError_t e;
   if (shape.few) {
-    const dim3 grid((unsigned)(few_sixteens(a.n_rows, a.max_items) * shape.chunks));
+    const dim3 grid((unsigned)(a.runs * shape.chunks));
     if (a.rank <= 16) hipLaunchKernelGGL((adapt_few_kernel<T, 1>), grid, dim3(512), 0, s, a);
     else if (a.rank <= 32) hipLaunchKernelGGL((adapt_few_kernel<T, 2>), grid, dim3(512), 0, s, a);
     else hipLaunchKernelGGL((adapt_few_kernel<T, 4>), grid, dim3(512), 0, s, a);
@@ -171,6 +171,7 @@ int odma_add_norm(odma_pool_t* pool, int64_t n_rows, const odma_add_norm_t* how,
   const bool f32 = pool->elem_bytes == 4;
   if (how->residual_dtype != ODMA_F32 && (f32 || how->residual_dtype != ODMA_BF16))
     return refuse(where, "the residual has the rows' type or ODMA_F32");
+  if (x_out && x_out == block && block_stride != how->width) return refuse(where, "x_out may be block only where block_stride is width");
   if (!x_out != !how->next_weight) return refuse(where, "x_out and next_weight go together");
   if (!block && (how->block_weight || how->gate)) return refuse(where, "weights or a gate without a block");
   if (how->gate_kind < ODMA_GATE_NONE || how->gate_kind > ODMA_GATE_SIGMOID || (how->gate_kind == ODMA_GATE_NONE) != !how->gate)
@@ -298,6 +299,7 @@ int odma_adapt_rows(odma_pool_t* pool, int64_t n_rows, const odma_adapters_t* ad
   a.groups = shape.groups;
   a.chunk_columns = shape.chunk_columns;
   a.chunks = shape.chunks;
+  a.runs = (int32_t)std::min<int64_t>(few_runs(n_rows, max_items), 1 << 20);
   for (int p = 0; p <= ODMA_MAX_PARTS; ++p) a.part_start[p] = p <= a.n_parts ? adapters->part_start[p] : cols;
   a.part_chunk[0] = 0;
   for (int p = 0; p < ODMA_MAX_PARTS; ++p)

@@ -260,6 +260,21 @@ def test_lists_that_name_nothing():
     assert (torch.isinf(c.y[66]) == (c.up[0, :, 0] != 0)).all()
 
 
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("rank", [16, 72])
+def test_lists_of_more_rows(rank, typ):
+    """Lists made for more rows than a call has: those that it has are adapted, wherever in the lists they stand."""
+    n = 400
+    adapter = np.arange(n)[::-1] % 350
+    c = Case(typ, adapter, [1] * n, 350, 264, [64, 48], rank)
+    whole = c.run().check().y.clone()
+    for rows in (1, 17, 100):
+        c.y.fill_(-7)
+        c.pool.odma_adapt_rows(rows, c.ad, len(c.items), c.items, c.order, c.x, c.x.stride(0), c.base, c.base.stride(0), c.y, c.y.stride(0), c.scratch)
+        torch.cuda.synchronize()
+        assert torch.equal(c.y[:rows], whole[:rows]) and (c.y[rows:] == -7).all()
+
+
 def test_far_rows():
     """Rows whose elements lie past 2^31."""
     c = Case("bf16", [0, 1], [2, 3], 2, 64, [32], 8)

@@ -61,7 +61,7 @@ def test_add_norm(runtime):  # noqa: F811
         p, f = make_pool(), make_pool(kv_dtype=B.F32)
         nan, inf = float("nan"), float("inf")
         for bad in (dict(n=-1), dict(n=(1 << 22) + 1), dict(res=None), dict(out=None, x=None, next_weight=None), dict(width=0), dict(width=-8),
-                    dict(width=1020), dict(width=32776), dict(residual_dtype=B.FP8), dict(residual_dtype=7), dict(x=None), dict(next_weight=None),
+                    dict(width=1020), dict(width=32776), dict(residual_dtype=B.FP8), dict(residual_dtype=7), dict(x=None), dict(next_weight=None), dict(x=Q, bs=2048),
                     dict(block=None, block_weight=WB), dict(block=None, gate=GATE), dict(gate=GATE, gate_kind=B.GATE_NONE),
                     dict(gate_kind=B.GATE_VALUE), dict(gate=GATE, gate_kind=3), dict(gate=GATE, gate_kind=-1), dict(eps=-1e-6), dict(eps=nan),
                     dict(eps=inf), dict(residual_scale=inf), dict(block_scale=nan), dict(block=Q + 8), dict(res=RES + 4), dict(out=OUT + 8),
@@ -75,7 +75,7 @@ def test_add_norm(runtime):  # noqa: F811
         # a row for all; rows that stand apart; one residual for all, not kept
         norm(p, rs=0, n=1), norm(p, bs=0), norm(p, bs=4096, rs=2048, gate=GATE, gate_stride=0), norm(p, rs=0, out=None)
         norm(p, residual_dtype=B.F32, rs=1028), norm(f, residual_dtype=B.F32, bs=1028, rs=1028), norm(p, block=None, out=None)
-        norm(make_pool(kv_dtype=B.FP8), slot=SLOT)
+        norm(make_pool(kv_dtype=B.FP8), slot=SLOT), norm(p, x=Q)
         # few rows: a wave for every 512 channels, rows of up to four waves side by side; many: waves with rows of their own
         for n, width, wg in ((1, 512, 1), (5, 512, 2), (5, 1024, 3), (5, 2048, 5), (5, 4096, 5), (5, 32768, 5), (1023, 2048, 1023), (1024, 512, 256),
                              (1025, 2048, 257), (1025, 3584, 513), (1025, 8192, 1025), (1025, 32768, 1025), (1 << 22, 32768, 1 << 22)):
