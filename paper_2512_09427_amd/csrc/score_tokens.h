@@ -25,6 +25,7 @@ constexpr int SCORE_PARTS = 64;             // most parts of a row: a lane each 
 constexpr int SCORE_KEPT = 128;             // keys that a wave keeps: a list that is cut down, and what 64 lanes may add
 constexpr int SCORE_RANKED = 128;           // keys that are ranked without another bound
 constexpr float SCORE_FAR = 0x1p100f;
+constexpr float SCORE_SLACK = 8.f;
 typedef unsigned long long u64;
 
 struct ScoreArgs {
@@ -180,8 +181,9 @@ __global__ __launch_bounds__(W * 64) void score_kernel(ScoreArgs a) {
   const float given = token >= 0 && token < a.vocab ? score_element(p + token) : __builtin_nanf("");
   // The lane's state, in powers of two and with a rounded reference: l = sum 2^(c x - r), t = sum 2^(c x - r) (c x - r), c x - r in one rounding.
   // The reference starts at a logit of -SCORE_FAR; rows whose largest logit is not between it and SCORE_FAR are taken again below.
-  const float c = a.scale_log2;
-  float m = -SCORE_FAR, r = rounded_product(m, c), l = 0.f, t = 0.f, top = -INFINITY;    // (top: the largest as it is)
+  // It moves when a logit is 2^SCORE_SLACK times likelier: of 64 lanes one finds a new largest logit in nearly every piece.
+  const float c = a.scale_log2, slack = SCORE_SLACK / c;
+  float m = -SCORE_FAR, raise = m, r = rounded_product(m, c), l = 0.f, t = 0.f, top = -INFINITY;    // (top: the largest as it is)
   int larger = 0, held = 0, round = 0;
   u64 bound = (u64)ORDERED_OFF << 32 | 0xffffffffu;          // keys above it are kept
   float least = -INFINITY;                                   // what is not above it cannot be among them
@@ -222,8 +224,9 @@ __global__ __launch_bounds__(W * 64) void score_kernel(ScoreArgs a) {
   auto add = [&](const float* x, int n) {
     float most = x[0];
     for (int i = 1; i < n; ++i) most = fmaxf(most, x[i]);
-    if (most > m) {
+    if (most > raise) {
       m = most;
+      raise = most + slack;
       const float now = rounded_product(m, c), d = r - now, f = __builtin_amdgcn_exp2f(d);
       t = f == 0.f ? 0.f : f * __builtin_fmaf(l, d, t);
       l *= f;
@@ -234,12 +237,12 @@ __global__ __launch_bounds__(W * 64) void score_kernel(ScoreArgs a) {
       l += e;
       t = __builtin_fmaf(e, fmaxf(d, LOWEST_REF), t);        // (0 x -inf)
     }
-    top = fmaxf(top, most);
+    top = most > top ? most : top;
     return most;
   };
-  auto count = [&](const float* x, int n, float most) {
-    if (most > given)
-      for (int i = 0; i < n; ++i) larger += x[i] > given;
+  auto count = [&](const float* x, int n, float most) {       // (of the whole wave)
+    if (!__builtin_amdgcn_ballot_w64(most > given)) return;
+    for (int i = 0; i < n; ++i) larger += count_of(__builtin_amdgcn_ballot_w64(x[i] > given));
   };
   auto collect = [&](const float* x, int n, float most, int at) {
     if (!__builtin_amdgcn_ballot_w64(most > least)) return;
@@ -278,9 +281,12 @@ __global__ __launch_bounds__(W * 64) void score_kernel(ScoreArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       score_piece((const T*)nullptr, w[u], x[u]);
-      if (g + u * N + 64 > pieces && g + u * N + lane >= pieces)
+      if (g + u * N + 64 > pieces) {                         // (the whole wave)
+        asm volatile("" ::: "memory");                       // (or the compiler makes 8 moves of it that every piece goes through)
+        if (g + u * N + lane >= pieces)
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[u][i] = -INFINITY;
+          for (int i = 0; i < V; ++i) x[u][i] = -INFINITY;
+      }
     }
     load(g + N * U);                                         // under way while these are taken in
 #pragma unroll
@@ -313,7 +319,6 @@ __global__ __launch_bounds__(W * 64) void score_kernel(ScoreArgs a) {
   ScoreState s = join_lanes(ScoreState{m, l * f, f * __builtin_fmaf(-d, l, t) / c}, c);
   publish();
   top = max_over_wave(top);
-  larger = (int)sum_over_wave((unsigned)larger);
   if (lane == 0) {
     states[wave] = s;
     tops[wave] = top;
