@@ -210,6 +210,12 @@ __global__ __launch_bounds__(256) void adapt_down_kernel(AdaptArgs a) {
   }
 }
 
+// Operands of h for 16 rows: in bf16 value and rest of 32 ranks each, of up to 16 ranks side by side in one; in fp32 16 ranks each.
+template <typename T>
+__host__ __device__ constexpr int up_steps(int rank) {
+  return sizeof(T) == 4 ? (rank + 15) / 16 : rank <= 16 ? 1 : (rank + 31) / 32 * 2;
+}
+
 // y of an item: grid items x chunks of columns.  SW: waves that share the rows of 64 columns where an item has so many.  LDS, dynamic: h in
 // operand order, [subtile][step][group][row] pieces of 16 bytes.
 //
@@ -232,7 +238,8 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
   while (part + 1 < a.n_parts && chunk >= a.part_chunk[part + 1]) ++part;
   const int c0 = a.part_start[part] + (chunk - a.part_chunk[part]) * a.chunk_columns;
   const int c1 = min(c0 + a.chunk_columns, a.part_start[part + 1]), cols = a.part_start[a.n_parts];
-  const int steps = (a.rank + 15) / 16, eights = steps * 2;  // (eights of ranks)
+  const int steps = up_steps<T>(a.rank), eights = X == 8 ? steps * 2 : (a.rank + 15) / 16 * 2;   // (eights of ranks)
+  const int units = X == 8 && steps > 1 ? steps / 2 : steps; // operands of weights: from 32 ranks of them on one serves value and rest of h
   const int line = lane / LINE, piece = lane % LINE;
   const float scale = a.scale ? a.scale[adapter] : 1.f;
   const T* up = (const T*)a.up + (int64_t)adapter * cols * a.rank;
@@ -257,8 +264,9 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
         for (int i = 0; i < LOADS; ++i)
           if (row[v][i] >= 0 && c < c1) in[v][i] = taken<STREAM>((const T*)a.base + row[v][i] * a.base_stride + c);
     };
-    auto weights = [&](uint4v (&av)[4], int cs, int s) {       // operand s of 64 columns
-      const int q = 4 * s + g, p = X == 8 && q >= eights ? q - eights : q;
+    auto piece_of = [&](int unit) { return X == 8 && steps == 1 ? g & 1 : 4 * unit + g; };   // ranks of a lane's operand
+    auto weights = [&](uint4v (&av)[4], int cs, int unit) {    // of 64 columns
+      const int p = piece_of(unit);
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int c = cs + t * 16 + m;
@@ -314,17 +322,20 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
       for (int v = 0; v < SUBS; ++v)
 #pragma unroll
         for (int t = 0; t < 4; ++t) acc[v][t] = float4v{0.f, 0.f, 0.f, 0.f};
-      for (int s = 0; s < steps; ++s) {
-        if (s > 0) weights(av, cs, s);
-        if ((X == 8 ? (4 * s + g) % eights : 4 * s + g) * X >= rank_a)      // (what lies behind the adapter's rank may be anything)
+      for (int unit = 0; unit < units; ++unit) {
+        if (unit > 0) weights(av, cs, unit);
+        if (piece_of(unit) * X >= rank_a)                      // (what lies behind the adapter's rank may be anything)
 #pragma unroll
           for (int t = 0; t < 4; ++t) av[t] = uint4v{0, 0, 0, 0};
 #pragma unroll
         for (int v = 0; v < SUBS; ++v) {
           if (u0 + v * sw >= subtiles) break;
-          const uint4v b = hs[((u0 + v * sw) * steps + s) * 64 + lane];
+          const uint4v* b = hs + ((u0 + v * sw) * steps + unit) * 64 + lane;
 #pragma unroll
-          for (int t = 0; t < 4; ++t) acc[v][t] = Op::mma(av[t], b, acc[v][t]);
+          for (int t = 0; t < 4; ++t) acc[v][t] = Op::mma(av[t], b[0], acc[v][t]);
+          if (units < steps)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[v][t] = Op::mma(av[t], b[units * 64], acc[v][t]);
         }
       }
       const int now = cs + piece * X;
@@ -372,6 +383,7 @@ __global__ __launch_bounds__(512, PT == 1 ? 4 : 2) void adapt_few_kernel(AdaptAr
   using Op = AdaptOp<T>;
   constexpr int X = Op::X, CHUNK = 8 * X, WAVES = 8, AHEAD = PT == 4 ? 2 : 3;   // (AHEAD: runs of channels that a wave has under way)
   constexpr int LINE = 64 / X, LOADS = 16 * LINE / 64;
+  constexpr int UNITS = X == 8 && PT > 1 ? PT / 2 : PT;      // operands of up, as in the second of two launches
   constexpr int TWO = PT < 2 ? PT : 2, WAVE = (16 + TWO * 16) * 8;   // of a wave in LDS: 16 rows and 16 or 32 ranks of 128 bytes, in pieces
   __shared__ __attribute__((aligned(16))) uint4v stage[WAVES * WAVE];
   __shared__ __attribute__((aligned(16))) uint4v hs[PT * 64];
@@ -431,7 +443,7 @@ __global__ __launch_bounds__(512, PT == 1 ? 4 : 2) void adapt_few_kernel(AdaptAr
     for (int i = 0; i < 2; ++i) xnumber[i] = a.row_order[first + min(8 * i + line8, count - 1)];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) row[i] = a.row_order[first + min(i * (64 / LINE) + line, count - 1)];
-    uint4v av[AHEAD][2 * PT], xv[AHEAD][2], in[LOADS], uv[PT][4];
+    uint4v av[AHEAD][2 * PT], xv[AHEAD][2], in[LOADS], uv[UNITS][4];
     auto load_ranks = [&](int j, int k) {
       const bool there = k + piece8 * X < a.width;             // (a width is whole pieces)
 #pragma unroll
@@ -442,8 +454,8 @@ __global__ __launch_bounds__(512, PT == 1 ? 4 : 2) void adapt_few_kernel(AdaptAr
     };
     auto load_up = [&](int cs) {
 #pragma unroll
-      for (int s = 0; s < PT; ++s) {
-        const int q = 4 * s + g, p = X == 8 && q >= 2 * PT ? q - 2 * PT : q;   // (bf16: pieces of ranks for the value and for the rest of h)
+      for (int s = 0; s < UNITS; ++s) {
+        const int p = X == 8 && PT == 1 ? g & 1 : 4 * s + g;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           uv[s][t] = uint4v{0, 0, 0, 0};
@@ -542,7 +554,7 @@ __global__ __launch_bounds__(512, PT == 1 ? 4 : 2) void adapt_few_kernel(AdaptAr
       for (int t = 0; t < 4; ++t) {
         sum[t] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < PT; ++s) sum[t] = Op::mma(uv[s][t], hs[s * 64 + lane], sum[t]);
+        for (int s = 0; s < PT; ++s) sum[t] = Op::mma(uv[s % UNITS][t], hs[s * 64 + lane], sum[t]);
       }
       uint4v old[LOADS];
 #pragma unroll

@@ -378,7 +378,7 @@ __global__ __launch_bounds__(W * 64) void score_kernel(ScoreArgs a) {
 
 // The parts of a row together: a work-group for each row.
 __global__ __launch_bounds__(256) void score_join_kernel(ScoreArgs a) {
-  constexpr int HELD = 4;                                    // keys of a thread that are loaded ahead
+  constexpr int HELD = SCORE_PARTS * ODMA_MAX_ALTERNATIVES / 256;   // keys of a thread
   __shared__ u64 list[SCORE_PARTS * ODMA_MAX_ALTERNATIVES];
   __shared__ int listed;
   const int lane = threadIdx.x & 63;
@@ -394,6 +394,7 @@ __global__ __launch_bounds__(256) void score_join_kernel(ScoreArgs a) {
   u64 held[HELD];
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
+    if (i * 256 >= n) break;
     const int at = i * 256 + threadIdx.x;
     held[i] = at < n ? keys[at] : 0;
   }
@@ -422,8 +423,10 @@ __global__ __launch_bounds__(256) void score_join_kernel(ScoreArgs a) {
     if (key > bound) list[atomicAdd(&listed, 1)] = key;      // (a bound has no token behind it: keys that reach it are above it)
   };
 #pragma unroll
-  for (int i = 0; i < HELD; ++i) add(held[i]);
-  for (int i = HELD * 256 + threadIdx.x; i < n; i += 256) add(keys[i]);
+  for (int i = 0; i < HELD; ++i) {
+    if (i * 256 >= n) break;
+    add(held[i]);
+  }
   __syncthreads();
   const float log_l = log_of(s.l);
   rank_keys<256>(list, listed, a.n_top, [&](int r, u64 key) { put_top(a, row, s, log_l, r, key); });
