@@ -32,6 +32,7 @@ struct AdaptArgs {
   int32_t part_start[ODMA_MAX_PARTS + 1];
   int32_t part_chunk[ODMA_MAX_PARTS + 1];   // second launch: chunks of columns in front of a part
   int32_t chunk_columns, chunks;
+  int32_t neighbours;                // first launch: items by fours (neighbours_of)
   int32_t runs;                      // the one launch for few rows: runs of 16 rows of the grid
 };
 
@@ -67,6 +68,13 @@ __device__ __forceinline__ void item_of(int pieces, int& at, int& piece) {
   const int eight = blockIdx.x / (8 * pieces), rest = (int)blockIdx.x - eight * 8 * pieces;
   at = eight * 8 + rest % 8;
   piece = rest / 8;
+}
+
+// The same for many items: four neighbours, mostly of one adapter, share an XCD's L2 for their rows, which every group of ranks reads, and the ranks.
+__device__ __forceinline__ void neighbours_of(int pieces, int& at, int& piece) {
+  const int block = blockIdx.x / (32 * pieces), rest = (int)blockIdx.x - block * 32 * pieces, j = rest / 8;
+  piece = j / 4;
+  at = block * 32 + rest % 8 * 4 + j % 4;
 }
 
 // Rows that are more than a cache keeps pass by it.
@@ -117,7 +125,9 @@ __global__ __launch_bounds__(256) void adapt_down_kernel(AdaptArgs a) {
   constexpr int X = Op::X, CHUNK = 8 * X;                    // channels of a piece, of 128 bytes
   constexpr int WAVE = (64 + MT * 16) * 8;                   // pieces of a wave in LDS: rows, then ranks
   __shared__ __attribute__((aligned(16))) uint4v stage[4 * WAVE];
-  const int at = blockIdx.x / (a.splits * a.groups), cut = (int)blockIdx.x - at * a.splits * a.groups;
+  int at = blockIdx.x / (a.splits * a.groups), cut = (int)blockIdx.x - at * a.splits * a.groups;
+  if (a.neighbours) neighbours_of(a.splits * a.groups, at, cut);
+  if (at >= a.max_items) return;
   const int4 item = a.items[at];
   const int adapter = item.x, first = item.y, count = min(item.z, ODMA_ADAPTER_ITEM_ROWS);
   if (count <= 0 || first < 0 || (unsigned)adapter >= (unsigned)a.n_adapters) return;

@@ -71,6 +71,11 @@ constexpr int ADAPT_FEW_WG = 360, ADAPT_FEW_WG_PARTS = 400, ADAPT_FEW_WG_WIDE = 
 constexpr int ADAPT_SPLIT = 512, ADAPT_WG = 512;
 // The second: work-groups up to which columns are cut, down to 64.  1 024 / 32 of rank 64 46 us with 1024 and 60 with 512.
 constexpr int ADAPT_UP_WG = 1024;
+// Two of its waves share the rows of 64 columns, four where a work-group has no more columns than that: 14 123 fp32 rows of 24 prompts
+// beside 1024 columns 132 us with two and 153 with four.  Rows past the caches (shape.stream) where lines are whole, since two halves of a line that are
+// stored one by one cross the memory twice: 93 308 rows of 80 + 2 000 columns, rank 64, 434 us past them and 324 through them, of 64 + 2 048 columns
+// 263 and 277; 41 423 rows of 4 608 columns, rank 16, 219 and 245.
+// Of the first, groups of ranks of four neighbouring items on one XCD: 41 423 rows, three parts of rank 64, 332 us and 360 without.
 
 // Runs of 16 rows of the items, as many as there can be if the lists are of these rows, in eights
 inline int64_t few_runs(int64_t n_rows, int64_t items) { return (n_rows / 16 + std::min(items, n_rows) + 7) / 8 * 8; }
@@ -78,7 +83,7 @@ inline int64_t few_runs(int64_t n_rows, int64_t items) { return (n_rows / 16 + s
 // What the adapters' launches look like, or why they are refused.  n_rows < 0: for the scratch of any number of rows.
 struct AdaptShape {
   int flat, tiles, groups, splits, split_channels, chunk_columns, chunks;
-  bool few, stream;
+  bool few, stream, lines;
   size_t scratch;
 };
 const char* adapt_shape(const odma_adapters_t* ad, int elem_bytes, int64_t n_rows, int64_t max_items, AdaptShape* shape) {
@@ -117,14 +122,14 @@ const char* adapt_shape(const odma_adapters_t* ad, int elem_bytes, int64_t n_row
            (ad->rank <= 16 ? ADAPT_FEW_WG : ad->n_parts > 1 ? ADAPT_FEW_WG_PARTS : ADAPT_FEW_WG_WIDE)) shape->chunk_columns *= 2;
   else
     while (shape->chunk_columns < 512 && items * cols / shape->chunk_columns > ADAPT_UP_WG) shape->chunk_columns *= 2;
-  if (items * std::max<int64_t>(chunks_of(shape->chunk_columns), shape->splits * shape->groups) > MAX_WG) return "too many items";
+  if ((items + 31) / 32 * 32 * std::max<int64_t>(chunks_of(shape->chunk_columns), shape->splits * shape->groups) > MAX_WG) return "too many items";
   shape->chunks = (int)chunks_of(shape->chunk_columns);
   return nullptr;
 }
 
 template <typename T, bool STREAM>
 void launch_adapt_down(const AdaptArgs& a, const AdaptShape& shape, hipStream_t s) {
-  const dim3 grid((unsigned)(shape.splits * shape.groups * a.max_items));
+  const dim3 grid((unsigned)(shape.splits * shape.groups * (a.neighbours ? (a.max_items + 31) / 32 * 32 : a.max_items)));
   if (shape.tiles == 1) hipLaunchKernelGGL((adapt_down_kernel<T, 1, STREAM>), grid, dim3(256), 0, s, a);
   else if (shape.tiles == 2) hipLaunchKernelGGL((adapt_down_kernel<T, 2, STREAM>), grid, dim3(256), 0, s, a);
   else if (shape.tiles == 3) hipLaunchKernelGGL((adapt_down_kernel<T, 3, STREAM>), grid, dim3(256), 0, s, a);
@@ -148,7 +153,8 @@ int launch_adapt(const char* where, const AdaptArgs& a, const AdaptShape& shape,
   if (e != hipSuccess) return hip_fail(where, e);
   const dim3 grid((unsigned)(shape.chunks * a.max_items));
   const size_t lds = (size_t)(a.rank > 128 ? 2 : 4) * up_steps<T>(a.rank) * 64 * 16;
-  if (shape.stream) hipLaunchKernelGGL((adapt_up_kernel<T, 2, true>), grid, dim3(256), lds, s, a);
+  if (shape.stream && shape.lines) hipLaunchKernelGGL((adapt_up_kernel<T, 2, true>), grid, dim3(256), lds, s, a);
+  else if (shape.chunk_columns > 64) hipLaunchKernelGGL((adapt_up_kernel<T, 2, false>), grid, dim3(256), lds, s, a);
   else hipLaunchKernelGGL((adapt_up_kernel<T, 4, false>), grid, dim3(256), lds, s, a);
   e = hipGetLastError();
   return e == hipSuccess ? ODMA_OK : hip_fail(where, e);
@@ -274,6 +280,9 @@ int odma_adapt_rows(odma_pool_t* pool, int64_t n_rows, const odma_adapters_t* ad
   if (y == base && y_stride != base_stride) return refuse(where, "y may be base only with the same stride");
   if (!aligned(items, 16) || !aligned(scratch, 256)) return refuse(where, "items must be 16-byte aligned, scratch 256-byte aligned");
   if (scratch_bytes < shape.scratch) return refuse(where, "scratch smaller than odma_adapt_scratch_bytes()");
+  // whole lines of base and y in every work-group's columns
+  shape.lines = aligned(base, 128) && aligned(y, 128) && base_stride * pool->elem_bytes % 128 == 0 && y_stride * pool->elem_bytes % 128 == 0;
+  for (int p = 1; p < adapters->n_parts; ++p) shape.lines = shape.lines && adapters->part_start[p] * pool->elem_bytes % 128 == 0;
   AdaptArgs a;
   a.down = adapters->down;
   a.up = adapters->up;
@@ -299,6 +308,7 @@ int odma_adapt_rows(odma_pool_t* pool, int64_t n_rows, const odma_adapters_t* ad
   a.groups = shape.groups;
   a.chunk_columns = shape.chunk_columns;
   a.chunks = shape.chunks;
+  a.neighbours = shape.stream && shape.groups > 1;
   a.runs = (int32_t)std::min<int64_t>(few_runs(n_rows, max_items), 1 << 20);
   for (int p = 0; p <= ODMA_MAX_PARTS; ++p) a.part_start[p] = p <= a.n_parts ? adapters->part_start[p] : cols;
   a.part_chunk[0] = 0;

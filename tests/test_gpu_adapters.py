@@ -212,6 +212,28 @@ def test_long_calls(rank, typ):
 
 
 @pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("cols,rank,pads", [((1024, 512), 8, (8, 0, 64)), ((1024, 512), 48, (0, 64, 0)), ((64, 2048), 64, (0, 0, 0)), ((80, 2000), 64, (0, 0, 0)),
+                                            ((64, 1984), 160, (16, 128, 64))])
+def test_long_calls_of_groups(cols, rank, pads, typ):
+    """The same in whole lines and not, with ranks of one group and of several, which neighbouring items share; the last block of them is not whole."""
+    rng = np.random.default_rng(5)
+    rows = rng.integers(0, 150, 320)
+    c = Case(typ, rng.integers(-1, 7, 320), rows, 7, 72, list(cols), rank, pads=pads)
+    assert c.total > 10000 and len(c.items) * sum(cols) / 512 >= 1024 and len(c.items) % 32
+    c.run().check()
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 40, 56, 64, 72, 96, 120, 128, 136, 256])
+def test_ranks(rank, typ):
+    """Every way in which ranks fill operands, with few rows and many."""
+    for rows in ([3, 20, 1, 64, 70], [300, 1, 2900, 33, 129]):
+        c = Case(typ, [2, 0, 3, 2, 1], rows, 4, 136, [48, 144], rank, seed=rank)
+        c.run().check()
+    Case(typ, [2, 0, 3, 2, 1], [3, 20, 1, 64, 70], 4, 136, [48, 144], rank, seed=rank, whole=False).run().check()
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
 def test_ragged_ranks(typ):
     """Weights behind an adapter's rank are NaN and infinities here, and are not there."""
     for rank, ranks in ((16, [16, 8, 0, -3, 99, 9]), (64, [8, 64, 40, 1, 24, 33])):

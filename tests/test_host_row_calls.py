@@ -152,8 +152,12 @@ def test_adapt_rows(runtime):  # noqa: F811
             assert len(got) == (1 if few else 2) and ("few" in got[0][0]) == few, (n, rank, got)
         assert len(launched(lambda: adapt(p, max_items=1025))) == 2
         assert launched(lambda: adapt(p, n=100))[0][1] == (2 * 16, 1, 1)       # 6 + 6 runs of 16 rows, in eights; two parts of a chunk of columns each
-        # long calls pass rows by the caches
+        # long calls pass rows by the caches, where their lines are whole; groups of ranks take items in 32s
         assert "Lb1E" in launched(lambda: adapt(p, n=100000, max_items=1600, ys=4608, bs=4608, ad=make(part_cols=(3584, 512, 512))))[1][0]
+        for part_cols, ys, rank, stream, first in (((3584, 512, 512), 4608, 16, True, 1590), ((3584, 512, 512), 4616, 16, False, 1590),
+                                                   ((3600, 496, 512), 4608, 16, False, 1590), ((3584, 512, 512), 4672, 64, True, 1600 * 3)):
+            got = launched(lambda: adapt(p, n=100000, max_items=1590, ys=ys, bs=4608, ad=make(part_cols=part_cols, rank=rank)))
+            assert ("Lb1E" in got[1][0]) == stream and got[0][1][0] == first, got
         for at, kw in ((0, {}), (0, dict(n=5000)), (1, dict(n=5000))):
             hip.fake_fail_launch(at)
             assert fails(lambda: adapt(p, **kw))
