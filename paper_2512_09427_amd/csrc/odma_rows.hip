@@ -54,17 +54,18 @@ void launch_add_norm(const AddNormArgs& a, bool many, hipStream_t s) {
   else launch_add_norm<T, R, 16, 4>(a, s);
 }
 
-// Both products in one launch (adapt_few_kernel) or in two, by the rows and by the bytes of a channel of an adapter's ranks, which every work-group
-// of the one launch reads.  One and two, us a call, 3584 channels, 4608 columns in three parts (or 1024 in one), requests / adapters:
-//   32 bytes (bf16, rank 16): 1 / 4 6.5 and 8.9, 64 / 64 11.0 and 18.3, 1 024 / 32 17.2 and 22.7, 4 096 / 32 42.9 and 50.4, 8 192 / 32 72.3 and 64.2
-//   64 (bf16, rank 32): 1 / 4 8.4 and 10.0, 64 / 16 9.8 and 12.1, 256 / 32 11.5 and 20.1, 1 024 / 32 23.5 and 27.6, 4 096 / 32 59.6 and 57.6
-//   128 (bf16, rank 64): 1 / 4 14.1 and 10.8, 64 / 16 15.1 and 14.9, 256 / 32 16.2 and 28.8, 1 024 / 32 38.6 and 45.7, 4 096 / 32 109 and 99
-//   256 (fp32, rank 64): 1 / 4 28.5 and 14.2, 64 / 16 30 and 20, 256 / 32 32 and 47, 1 024 / 32 79 and 94 (31.6 and 30.7), 4 096 / 32 179 and 184 (75 and 68)
-constexpr int ADAPT_FEW = 4096, ADAPT_FEW_WIDE = 2560, ADAPT_FEW_FROM = 128;
+// Both products in one launch (adapt_few_kernel) or in two.  Every work-group of the one forms h for itself: its matrix instructions (counted as bytes of
+// the ranks in bf16, in whole tiles of 16, four times as many for fp32) times the rounds of work-groups that the chip goes through must stay within what two launches
+// cost more, which grows with the rows, and within a most.  One and two, us a call, 3584 channels, 4608 columns in three parts (1024 in one), requests of one row / adapters:
+//   bf16, rank 16: 1 / 4 6.6 and 8.9, 64 / 64 11.0 and 15.8, 1 024 / 32 16.5 and 19.4, 4 096 / 32 42.3 and 43.4, 8 192 / 32 71 and 58
+//   bf16, rank 32: 1 / 4 7.7 and 9.4, 256 / 32 16.9 and 17.3, 2 048 / 32 29.4 and 30.3, 4 096 / 32 55.5 and 51.4
+//   bf16, rank 64: 1 / 4 12.1 and 10.0, 256 / 32 24.1 and 22.3 (13.4 and 16.2), 1 024 / 32 32.6 and 32.8 (14.4 and 18.9), 4 096 / 32 85 and 74 (32 and 31)
+//   fp32, rank 64: 1 / 4 28 and 14, 256 / 32 58 and 46 (30 and 26), 1 024 / 32 77 and 90 (30.7 and 31.3), 4 096 / 32 180 and 191, 8 192 / 32 322 and 266
+// other channels: bf16 208 / 3 of rank 64, 8 160 to 816 23.0 and 17.1; 15 / 15, 992 to 320 6.1 and 9.3; 4 132 rows of rank 16, 128 to 1072 8.0 and 13.4.
+constexpr int64_t ADAPT_FEW = 8192, ADAPT_FEW_WORK = 320 << 10, ADAPT_FEW_ROW = 3 << 10, ADAPT_FEW_MOST = 560 << 10, ADAPT_FEW_MOST_F32 = 6 << 20, ADAPT_FEW_CU = 256;
 // Work-groups that it is cut into, as far as the adapters that a batch may have let it be known.  Two share a compute unit with ranks up to 16: 64 / 64 as above
 // 11.0 us with 260 and 12.3 with 390, 256 / 32 9.1 with 360 and 11.4 with 160.  With more it is one; parts narrower than the others' runs of columns
-// leave short work-groups that fill in: 1 024 / 32 of rank 64 38.6 us with 384 and 55 with 256, but 2 300 fp32 rows beside 1024 columns
-// 26.8 with 286 and 22.8 with 143.
+// leave short work-groups that fill in: fp32 1 024 / 32 of rank 64 77 us with 384 and 101 with 240, but beside 1024 columns 2 048 / 32 57 with 288 and 37 with 144.
 constexpr int ADAPT_FEW_WG = 360, ADAPT_FEW_WG_PARTS = 400, ADAPT_FEW_WG_WIDE = 256;
 // The first of two launches: fewest channels of a cut, and work-groups up to which channels are cut: every cut is one more array for the second
 // launch to add up.  256 / 32 of rank 64 29.7 us with 512 and 32.8 with 256; 24 fp32 prompts of 2 300 rows 24.7 with 512 and 27.5 with 1024.
@@ -112,16 +113,19 @@ const char* adapt_shape(const odma_adapters_t* ad, int elem_bytes, int64_t n_row
     for (int p = 0; p < ad->n_parts; ++p) n += (ad->part_start[p + 1] - ad->part_start[p] + columns - 1) / columns;
     return n;
   };
-  const int rank_bytes = ad->rank * elem_bytes;
-  const int64_t fewest = rank_bytes <= 64 ? 0 : ADAPT_FEW_FROM, most = rank_bytes <= 32 ? ADAPT_FEW : ADAPT_FEW_WIDE;
-  shape->few = ad->rank <= 64 && n_rows >= fewest && n_rows <= most && items <= 1024 && cols <= 1 << 17;
+  // One launch: its work-groups with the fewest chunks of columns that make enough of them, and how many rounds of them the chip goes through
+  const int64_t listed = std::min(items, n_rows), least = n_rows / 16;
+  const int64_t runs = ad->n_parts > 1 ? std::max(listed + n_rows / 64, least) : std::max(listed, least + (items - n_rows / 64) / 2);
+  const int few_wg = ad->rank <= 16 ? ADAPT_FEW_WG : ad->n_parts > 1 ? ADAPT_FEW_WG_PARTS : ADAPT_FEW_WG_WIDE;
+  int few_columns = 512;
+  while (few_columns < 4096 && runs * chunks_of(few_columns) > few_wg) few_columns *= 2;
+  const int64_t work = (int64_t)(ad->rank + 15) / 16 * 16 * ad->width * (elem_bytes == 4 ? 8 : 2);
+  const int64_t bound = std::min<int64_t>(ADAPT_FEW_WORK + ADAPT_FEW_ROW * n_rows, elem_bytes == 4 ? ADAPT_FEW_MOST_F32 : ADAPT_FEW_MOST);
+  shape->few = ad->rank <= 64 && n_rows >= 0 && n_rows <= ADAPT_FEW && items <= 1024 && cols <= 1 << 17 &&
+               work * std::max<int64_t>(runs * chunks_of(few_columns), ADAPT_FEW_CU) <= bound * ADAPT_FEW_CU;
   shape->stream = n_rows * cols * elem_bytes > (int64_t)4 << 20 && items * cols / 512 >= ADAPT_UP_WG;
-  shape->chunk_columns = shape->few ? 512 : 64;
-  if (shape->few)
-    while (shape->chunk_columns < 4096 && std::max(std::min(items, n_rows) + n_rows / 64, n_rows / 16) * chunks_of(shape->chunk_columns) >
-           (ad->rank <= 16 ? ADAPT_FEW_WG : ad->n_parts > 1 ? ADAPT_FEW_WG_PARTS : ADAPT_FEW_WG_WIDE)) shape->chunk_columns *= 2;
-  else
-    while (shape->chunk_columns < 512 && items * cols / shape->chunk_columns > ADAPT_UP_WG) shape->chunk_columns *= 2;
+  shape->chunk_columns = shape->few ? few_columns : 64;
+  while (!shape->few && shape->chunk_columns < 512 && items * cols / shape->chunk_columns > ADAPT_UP_WG) shape->chunk_columns *= 2;
   if ((items + 31) / 32 * 32 * std::max<int64_t>(chunks_of(shape->chunk_columns), shape->splits * shape->groups) > MAX_WG) return "too many items";
   shape->chunks = (int)chunks_of(shape->chunk_columns);
   return nullptr;

@@ -224,6 +224,15 @@ def test_long_calls_of_groups(cols, rank, pads, typ):
 
 
 @pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("rank,width,rows", [(64, 8200, [3, 20, 1, 64, 70]), (40, 8200, [1, 0, 2, 7, 100]), (8, 2056, [5000, 1, 3000, 130, 900]), (16, 1544, [5000, 1, 3000, 130, 900]),
+                                             (24, 1544, [9000, 63, 64, 65, 1])])
+def test_cut_channels(rank, width, rows, typ):
+    """Two launches, of which the first cuts the channels between work-groups."""
+    for whole in (True, False):
+        Case(typ, [2, 0, 3, 2, 1], rows, 4, width, [48, 80], rank, seed=rank, whole=whole).run().check()
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
 @pytest.mark.parametrize("rank", [8, 16, 24, 32, 40, 56, 64, 72, 96, 120, 128, 136, 256])
 def test_ranks(rank, typ):
     """Every way in which ranks fill operands, with few rows and many."""

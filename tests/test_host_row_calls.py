@@ -143,13 +143,13 @@ def test_adapt_rows(runtime):  # noqa: F811
         adapt(p, y=K, ys=96), adapt(f, xs=516, bs=100, ys=100), adapt(p, xs=0, bs=0)
         two = launched(lambda: adapt(p, ys=256, ad=make(rank=256, part_cols=(64, 64, 64, 64), width=32768)))
         assert ["down" in two[0][0], "up" in two[1][0]] == [True, True] and len(two) == 2 and two[1][2] == 32768
-        # few rows take one launch, by the bytes of a channel of the ranks: up to 4096 rows of 32, 2560 of 64, from 128 on for more up to rank 64
-        for pool, n, rank, few in ((p, 1, 16, True), (p, 4096, 16, True), (p, 4097, 16, False), (p, 1, 32, True), (p, 2560, 32, True), (p, 2561, 32, False),
-                                   (p, 127, 64, False), (p, 128, 64, True), (p, 2560, 40, True), (p, 2561, 64, False), (p, 200, 72, False),
-                                   (f, 1, 16, True), (f, 2560, 16, True), (f, 2561, 16, False), (f, 127, 32, False), (f, 128, 32, True), (f, 128, 64, True),
-                                   (f, 128, 72, False)):
-            got = launched(lambda: adapt(pool, n=n, ad=make(rank=rank)))
-            assert len(got) == (1 if few else 2) and ("few" in got[0][0]) == few, (n, rank, got)
+        # few rows take one launch, by the matrix instructions of a work-group and the rounds of them
+        for pool, n, rank, width, few in ((p, 1, 16, 3584, True), (p, 8192, 16, 512, True), (p, 8193, 16, 512, False), (p, 1, 32, 3584, True), (p, 1, 64, 3584, False),
+                                          (p, 100, 64, 3584, True), (p, 100, 64, 8192, False), (p, 8192, 64, 512, True), (p, 8192, 64, 3584, False),
+                                          (p, 200, 72, 512, False), (f, 1, 16, 3584, False), (f, 1, 16, 1024, True), (f, 200, 64, 3584, False), (f, 800, 64, 3584, True),
+                                          (f, 1, 8, 1024, True), (f, 8192, 64, 8192, False), (f, 128, 72, 512, False)):
+            got = launched(lambda: adapt(pool, n=n, ad=make(rank=rank, width=width), xs=width))
+            assert len(got) == (1 if few else 2) and ("few" in got[0][0]) == few, (n, rank, width, got)
         assert len(launched(lambda: adapt(p, max_items=1025))) == 2
         assert launched(lambda: adapt(p, n=100))[0][1] == (2 * 16, 1, 1)       # 6 + 6 runs of 16 rows, in eights; two parts of a chunk of columns each
         # long calls pass rows by the caches, where their lines are whole; groups of ranks take items in 32s
@@ -158,7 +158,7 @@ def test_adapt_rows(runtime):  # noqa: F811
                                                    ((3600, 496, 512), 4608, 16, False, 1590), ((3584, 512, 512), 4672, 64, True, 1600 * 3)):
             got = launched(lambda: adapt(p, n=100000, max_items=1590, ys=ys, bs=4608, ad=make(part_cols=part_cols, rank=rank)))
             assert ("Lb1E" in got[1][0]) == stream and got[0][1][0] == first, got
-        for at, kw in ((0, {}), (0, dict(n=5000)), (1, dict(n=5000))):
+        for at, kw in ((0, {}), (0, dict(n=9000)), (1, dict(n=9000))):
             hip.fake_fail_launch(at)
             assert fails(lambda: adapt(p, **kw))
     """)
