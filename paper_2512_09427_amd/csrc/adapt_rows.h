@@ -6,9 +6,13 @@
 // work-group, which add up in LDS, and, where a batch has few items, between work-groups, whose parts stay apart in scratch: nothing is
 // added up in an order that changes.  The second stages an item's h in LDS, parts added up and scaled, and takes 64 columns a wave at
 // a time.  In bf16, h enters as two bf16 parts (value and rest: 16 bits), which fill the contraction of 32 that a rank of 16 would
-// half leave empty.
+// half leave empty; from 32 ranks on one operand of up is multiplied by both.
 //
-// Both are bound by memory: adapters that occur once are the bytes of a decode step, x, base and y those of a prompt.
+// Both are bound by memory: adapters that occur once are the bytes of a decode step, x, base and y those of a prompt.  3584 channels, 4608 columns, rank 16 in
+// bf16: 43 340 rows of prompts 211 us (65 + 150 traced), 5.3 TB/s; 64 rows of as many adapters 11 us, a chain of loads that depend on one another (items, row
+// numbers, x, columns) around 33 MB.  Larger ranks are not: 41 423 rows of rank 64 331 us (209 for the bytes), whose groups of ranks read x three times and whose
+// weights come from the L2 for every item.  Large products in fp32 reach a ninth of the rate (0.154 PFLOP/s): 2 084 rows of rank 64, 1000 to 1024 channels, 22 us
+// (5.1 for the bytes), one work-group on a compute unit, on 140 to 150 of them, with loads, 3.3 us of products, sums, loads and 3.4 us of products one behind the other.
 #pragma once
 
 #include <type_traits>
