@@ -99,21 +99,26 @@ __device__ __forceinline__ unsigned reached_by(const unsigned (&v)[N], int k) {
   return found;
 }
 
-// Ranks the keys of a list in LDS by counting: `put(rank, key)` for the n_top largest, and for key 0 where there are fewer.
+// Ranks the keys of a list in LDS by counting, four lanes a key: `put(rank, key)` for the n_top largest, and for key 0 where there are fewer.
 template <int THREADS, typename Put>
 __device__ __forceinline__ void rank_keys(const u64* list, int n, int n_top, Put put) {
-  for (int i = threadIdx.x; i < n; i += THREADS) {
+  const int quarter = threadIdx.x & 3;
+  for (int i = threadIdx.x >> 2; i < n; i += THREADS / 4) {
     const u64 key = list[i];
-    int r = 0, j = 0;
-    for (; j + 8 <= n; j += 8) {
+    unsigned r = 0;
+    int j = quarter;
+    for (; j + 28 < n; j += 32) {
       u64 other[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) other[e] = list[j + e];
+      for (int e = 0; e < 8; ++e) other[e] = list[j + 4 * e];
 #pragma unroll
       for (int e = 0; e < 8; ++e) r += other[e] > key;
     }
-    for (; j < n; ++j) r += list[j] > key;
-    if (r < n_top) put(r, key);
+#pragma unroll 1
+    for (; j < n; j += 4) r += list[j] > key;
+    r += moved<0xb1>(r);                                     // of the four lanes
+    r += moved<0x4e>(r);
+    if (quarter == 0 && r < (unsigned)n_top) put((int)r, key);
   }
   for (int r = n + threadIdx.x; r < n_top; r += THREADS) put(r, (u64)0);
 }
