@@ -25,7 +25,9 @@ bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 
 constexpr int64_t MAX_ROWS = (int64_t)1 << 22;       // of odma_add_norm (a launch has fewer than 2^32 threads, 1024 of them a row)
 constexpr int64_t MAX_LISTED = (int64_t)1 << 27;     // rows of lists
 constexpr int64_t MAX_WG = (1 << 24) - 1;            // work-groups of 256 threads of a launch
-constexpr int LIST_WG = 1024;                    // work-groups up to which the making of lists is dealt out
+// Work-groups up to which the making of lists is dealt out, several requests each beyond: 1 024 requests of one row 6.7 us with 1 024 and 8.5 with 256, 2 048
+// 12.7 with 1 024 and 17.4 with as many as requests; one of 8 192 rows 3.2 in eight work-groups and 5.3 in one.
+constexpr int LIST_WG = 1024;
 
 template <typename T, typename R, int W, int P>
 void launch_add_norm(const AddNormArgs& a, hipStream_t s) {
@@ -33,22 +35,22 @@ void launch_add_norm(const AddNormArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((add_norm_kernel<T, R, W, P>), dim3((unsigned)((a.n_rows + rows - 1) / rows)), dim3(W > 4 ? W * 64 : 256), 0, s, a);
 }
 
-// Waves of a row and pieces of a lane: as many waves as a row fills with one piece a lane, four pieces from 16 waves on; in calls of many
-// rows fewer waves with more pieces each, since a wave alone with its row waits for nobody.
+// Waves of a row and pieces of a lane: as many waves as a row fills with one piece a lane, more pieces from 16 waves on.  With many rows on
+// a compute unit some widths take fewer waves with more pieces each, which wait for each other less.  us a call with few and with many waves: 3584
+// channels 16 384 rows 83.3 (eight waves) and 87.5 (two), 65 869 beside an fp32 residual 526 and 515; 8 192 channels 256 rows 4.9 (16) and 5.0 (8), 1 024
+// 13.0 and 11.6, 4 096 51 and 48.6; 520 channels 4 096 fp32 rows 7.6 (two) and 8.1 (one), 32 768 bf16 rows 32.3 and 29.6.  2 048 channels in one wave were
+// slower throughout (4 096 rows 13.1 and 11.6 in four), in two the same as in four.
+constexpr int64_t NORM_MANY_2 = 64, NORM_MANY_8 = 192, NORM_MANY_16 = 4;   // rows a compute unit, by pieces
 template <typename T, typename R>
-void launch_add_norm(const AddNormArgs& a, bool many, hipStream_t s) {
+void launch_add_norm(const AddNormArgs& a, int64_t n_cu, hipStream_t s) {
   const int pieces = (a.width + 511) / 512;                   // of 64 lanes
-  if (many && pieces <= 4) {
-    if (pieces == 1) launch_add_norm<T, R, 1, 1>(a, s);
-    else if (pieces == 2) launch_add_norm<T, R, 1, 2>(a, s);
-    else launch_add_norm<T, R, 1, 4>(a, s);
-  } else if (many && pieces <= 16) {
-    if (pieces <= 8) launch_add_norm<T, R, 2, 4>(a, s);
-    else launch_add_norm<T, R, 4, 4>(a, s);
-  } else if (pieces == 1) launch_add_norm<T, R, 1, 1>(a, s);
+  if (pieces == 1) launch_add_norm<T, R, 1, 1>(a, s);
+  else if (pieces == 2 && a.n_rows >= NORM_MANY_2 * n_cu) launch_add_norm<T, R, 1, 2>(a, s);
   else if (pieces == 2) launch_add_norm<T, R, 2, 1>(a, s);
   else if (pieces <= 4) launch_add_norm<T, R, 4, 1>(a, s);
+  else if (pieces <= 8 && a.n_rows >= NORM_MANY_8 * n_cu) launch_add_norm<T, R, 2, 4>(a, s);
   else if (pieces <= 8) launch_add_norm<T, R, 8, 1>(a, s);
+  else if (pieces <= 16 && a.n_rows >= NORM_MANY_16 * n_cu) launch_add_norm<T, R, 8, 2>(a, s);
   else if (pieces <= 16) launch_add_norm<T, R, 16, 1>(a, s);
   else if (pieces <= 32) launch_add_norm<T, R, 16, 2>(a, s);
   else launch_add_norm<T, R, 16, 4>(a, s);
@@ -215,10 +217,9 @@ int odma_add_norm(odma_pool_t* pool, int64_t n_rows, const odma_add_norm_t* how,
   a.width = how->width;
   a.gate_kind = how->gate_kind;
   hipStream_t s = (hipStream_t)stream;
-  const bool many = n_rows >= 4 * (int64_t)pool->n_cu;
-  if (f32) launch_add_norm<float, float>(a, many, s);
-  else if (how->residual_dtype == ODMA_F32) launch_add_norm<unsigned short, float>(a, many, s);
-  else launch_add_norm<unsigned short, unsigned short>(a, many, s);
+  if (f32) launch_add_norm<float, float>(a, pool->n_cu, s);
+  else if (how->residual_dtype == ODMA_F32) launch_add_norm<unsigned short, float>(a, pool->n_cu, s);
+  else launch_add_norm<unsigned short, unsigned short>(a, pool->n_cu, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(where, e);
   return ODMA_OK;

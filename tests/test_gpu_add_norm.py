@@ -113,6 +113,13 @@ def test_widths(rows, width, typ, res):
 
 
 @pytest.mark.parametrize("typ,res", TYPES)
+@pytest.mark.parametrize("rows,width", [(16400, 520), (49170, 2056), (1030, 4104), (1030, 8192)])
+def test_many_rows(rows, width, typ, res):
+    """Fewer waves to a row, with more pieces each."""
+    Case(typ, res, rows, width, gate="none" if rows > 20000 else "sigmoid", seed=width).run().check()
+
+
+@pytest.mark.parametrize("typ,res", TYPES)
 @pytest.mark.parametrize("rows", [5, 1031])
 @pytest.mark.parametrize("post", [False, True])
 @pytest.mark.parametrize("gate,one", [("none", False), ("value", False), ("value", True), ("sigmoid", False), ("sigmoid", True)])

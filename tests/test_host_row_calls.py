@@ -76,9 +76,10 @@ def test_add_norm(runtime):  # noqa: F811
         norm(p, rs=0, n=1), norm(p, bs=0), norm(p, bs=4096, rs=2048, gate=GATE, gate_stride=0), norm(p, rs=0, out=None)
         norm(p, residual_dtype=B.F32, rs=1028), norm(f, residual_dtype=B.F32, bs=1028, rs=1028), norm(p, block=None, out=None)
         norm(make_pool(kv_dtype=B.FP8), slot=SLOT), norm(p, x=Q)
-        # few rows: a wave for every 512 channels, rows of up to four waves side by side; many: waves with rows of their own
+        # a wave for every 512 channels, rows of up to four waves side by side; with many rows fewer waves at some widths
         for n, width, wg in ((1, 512, 1), (5, 512, 2), (5, 1024, 3), (5, 2048, 5), (5, 4096, 5), (5, 32768, 5), (1023, 2048, 1023), (1024, 512, 256),
-                             (1025, 2048, 257), (1025, 3584, 513), (1025, 8192, 1025), (1025, 32768, 1025), (1 << 22, 32768, 1 << 22)):
+                             (16383, 1024, 8192), (16384, 1024, 4096), (1025, 2048, 1025), (49151, 3584, 49151), (49152, 3584, 24576), (1023, 8192, 1023),
+                             (1025, 8192, 1025), (1025, 32768, 1025), (1 << 22, 32768, 1 << 22)):
             one = launched(lambda: norm(p, n=n, width=width, bs=width, rs=width))
             assert len(one) == 1 and "add_norm_kernel" in one[0][0] and one[0][1] == (wg, 1, 1), (n, width, one)
         hip.fake_fail_launch(0)
