@@ -524,7 +524,7 @@ size_t odma_adapt_scratch_bytes(const odma_pool_t* pool, const odma_adapters_t* 
 
 /* The adapters' products beside what the shared projection left: for every row in the lists, with its adapter a and column c of part p,
  *   y[row, c] = base[row, c] + scale[a] * sum_k up[a, c, k] * sum_d down[a, p, k, d] * x[row, d].
- * fp32 throughout (bf16 rows: the inner sums enter the outer ones in two bf16 parts, 16 bits), rounded once.
+ * fp32 throughout, also the inner sums that enter the outer ones; rounded once.
  *   items, row_order   DEVICE, from odma_group_adapters (row_order for n_rows rows; entries outside 0 .. n_rows - 1 and items that name
  *                      no adapter are skipped).  No row may be there twice
  *   x, base, y         DEVICE rows, row i at element i * its stride.  y may be base itself (same stride), else it lies apart from x and base;

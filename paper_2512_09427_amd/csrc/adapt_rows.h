@@ -5,8 +5,9 @@
 // The first of two forms h: ranks are the rows of the matrix product, an item's rows its columns.  The channels are cut between the waves of a
 // work-group, which add up in LDS, and, where a batch has few items, between work-groups, whose parts stay apart in scratch: nothing is
 // added up in an order that changes.  The second stages an item's h in LDS, parts added up and scaled, and takes 64 columns a wave at
-// a time.  In bf16, h enters as two bf16 parts (value and rest: 16 bits), which fill the contraction of 32 that a rank of 16 would
-// half leave empty; from 32 ranks on one operand of up is multiplied by both.
+// a time.  In bf16, h enters as three bf16 parts, which hold all its 24 bits: two of them side by side fill the contraction of 32 that a rank of 16 would
+// half leave empty; from 24 ranks on one operand of up is multiplied by all three.  Two parts (16 bits of h) took 211.0 us and three take 212.3 for 43 340 rows of rank 16,
+// 337 and 344 for rank 64, 123 and 137 for 9 326 rows of rank 128, but where base and products cancel the rest of a sum was that of 16 bits.
 //
 // Both are bound by memory: adapters that occur once are the bytes of a decode step, x, base and y those of a prompt.  3584 channels, 4608 columns, rank 16 in
 // bf16: 43 340 rows of prompts 211 us (65 + 150 traced), 5.3 TB/s; 64 rows of as many adapters 11 us, a chain of loads that depend on one another (items, row
@@ -92,15 +93,19 @@ __device__ __forceinline__ void put(T* p, uint4v v) {
   else *(uint4v*)p = v;
 }
 
-// Ranks of h as the second product takes them: eight in bf16, value and rest (finite numbers stay finite: the value is cut off).
-__device__ __forceinline__ void split_ranks(const float* v, uint4v& hi, uint4v& lo) {
+// Eight ranks of h as the second product takes them in bf16: three numbers of 8 bits each that add up to all 24 of h.  What is left of h is cut
+// off, not rounded: finite numbers stay finite, and what is left is exact.
+__device__ __forceinline__ void split_ranks(const float* v, uint4v (&part)[3]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float v0 = v[2 * e], v1 = v[2 * e + 1];
-    const unsigned h0 = __float_as_uint(v0) & 0xffff0000u, h1 = __float_as_uint(v1) & 0xffff0000u;
-    const float l0 = __builtin_isinf(v0) ? 0.f : v0 - __uint_as_float(h0), l1 = __builtin_isinf(v1) ? 0.f : v1 - __uint_as_float(h1);
-    hi[e] = h0 >> 16 | h1;
-    lo[e] = float_to_bf16_bits(l0) | (unsigned)float_to_bf16_bits(l1) << 16;
+    float v0 = v[2 * e], v1 = v[2 * e + 1];
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      const unsigned h0 = __float_as_uint(v0) & 0xffff0000u, h1 = __float_as_uint(v1) & 0xffff0000u;
+      part[q][e] = h0 >> 16 | h1;
+      v0 = __builtin_isinf(v0) ? 0.f : v0 - __uint_as_float(h0);
+      v1 = __builtin_isinf(v1) ? 0.f : v1 - __uint_as_float(h1);
+    }
   }
 }
 
@@ -224,11 +229,15 @@ __global__ __launch_bounds__(256) void adapt_down_kernel(AdaptArgs a) {
   }
 }
 
-// Operands of h for 16 rows: in bf16 value and rest of 32 ranks each, of up to 16 ranks side by side in one; in fp32 16 ranks each.
+// Operands of h for 16 rows: in bf16 three parts of 32 ranks each, of up to 16 ranks two parts side by side in one; in fp32 16 ranks each.
 template <typename T>
 __host__ __device__ constexpr int up_steps(int rank) {
-  return sizeof(T) == 4 ? (rank + 15) / 16 : rank <= 16 ? 1 : (rank + 31) / 32 * 2;
+  return sizeof(T) == 4 ? (rank + 15) / 16 : rank <= 16 ? 2 : (rank + 31) / 32 * 3;
 }
+// Runs of 16 rows whose h is staged at a time, an operand of one 1 KiB, and the LDS for them.  Weights are read again for the next: 9 326 bf16 rows of rank 128 (12
+// operands) 137 us with four runs, 166 with two; 9 326 fp32 rows of rank 160 (10) 525 and 608.
+__host__ __device__ constexpr int up_staged(int steps) { return steps <= 12 ? 4 : steps <= 16 ? 2 : 1; }
+constexpr size_t up_lds(int steps) { return (size_t)(steps <= 12 ? 4 * steps : 32) * 1024; }
 
 // y of an item: grid items x chunks of columns.  SW: waves that share the rows of 64 columns where an item has so many.  LDS, dynamic: h in
 // operand order, [subtile][step][group][row] pieces of 16 bytes.
@@ -252,14 +261,14 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
   while (part + 1 < a.n_parts && chunk >= a.part_chunk[part + 1]) ++part;
   const int c0 = a.part_start[part] + (chunk - a.part_chunk[part]) * a.chunk_columns;
   const int c1 = min(c0 + a.chunk_columns, a.part_start[part + 1]), cols = a.part_start[a.n_parts];
-  const int steps = up_steps<T>(a.rank), eights = X == 8 ? steps * 2 : (a.rank + 15) / 16 * 2;   // (eights of ranks)
-  const int units = X == 8 && steps > 1 ? steps / 2 : steps; // operands of weights: from 32 ranks of them on one serves value and rest of h
+  const bool narrow = X == 8 && a.rank <= 16;
+  const int steps = up_steps<T>(a.rank), units = narrow ? 1 : X == 8 ? steps / 3 : steps;   // (units: operands of weights; in bf16 one serves all parts of h)
+  const int eights = X == 8 && !narrow ? units * 4 : (a.rank + 15) / 16 * 2;                // of ranks
   const int line = lane / LINE, piece = lane % LINE;
   const float scale = a.scale ? a.scale[adapter] : 1.f;
   const T* up = (const T*)a.up + (int64_t)adapter * cols * a.rank;
   float4v* turn = turned[wave];
-  // h of up to 64 rows is staged at a time, of 32 where ranks are more than 128
-  const int most_rows = steps > 8 ? 32 : 64;
+  const int most_rows = up_staged(steps) * 16;
   for (int j0 = 0; j0 < count; j0 += most_rows) {
     const int rows = min(count - j0, most_rows), subtiles = (rows + 15) / 16;
     // this wave's subtiles and columns
@@ -278,7 +287,7 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
         for (int i = 0; i < LOADS; ++i)
           if (row[v][i] >= 0 && c < c1) in[v][i] = taken<STREAM>((const T*)a.base + row[v][i] * a.base_stride + c);
     };
-    auto piece_of = [&](int unit) { return X == 8 && steps == 1 ? g & 1 : 4 * unit + g; };   // ranks of a lane's operand
+    auto piece_of = [&](int unit) { return narrow ? g & 1 : 4 * unit + g; };   // ranks of a lane's operand
     auto weights = [&](uint4v (&av)[4], int cs, int unit) {    // of 64 columns
       const int p = piece_of(unit);
 #pragma unroll
@@ -319,11 +328,12 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
         for (int e = 0; e < 8; ++e) v[e] *= scale;
       }
       uint4v* to = hs + (j >> 4) * steps * 64 + (j & 15);
-      if constexpr (X == 8) {                                  // value and rest
-        uint4v hi, lo;
-        split_ranks(v, hi, lo);
-        to[p * 16] = hi;
-        to[(eights + p) * 16] = lo;
+      if constexpr (X == 8) {
+        uint4v h[3];
+        split_ranks(v, h);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) to[(q * eights + p) * 16] = h[q];
+        if (narrow) to[(3 * eights + p) * 16] = uint4v{0, 0, 0, 0};
       } else {
         to[2 * p * 16] = __builtin_bit_cast(uint4v, float4v{v[0], v[1], v[2], v[3]});
         to[(2 * p + 1) * 16] = __builtin_bit_cast(uint4v, float4v{v[4], v[5], v[6], v[7]});
@@ -347,9 +357,13 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
           const uint4v* b = hs + ((u0 + v * sw) * steps + unit) * 64 + lane;
 #pragma unroll
           for (int t = 0; t < 4; ++t) acc[v][t] = Op::mma(av[t], b[0], acc[v][t]);
-          if (units < steps)
+          if (X == 8) {
 #pragma unroll
             for (int t = 0; t < 4; ++t) acc[v][t] = Op::mma(av[t], b[units * 64], acc[v][t]);
+            if (!narrow)
+#pragma unroll
+              for (int t = 0; t < 4; ++t) acc[v][t] = Op::mma(av[t], b[2 * units * 64], acc[v][t]);
+          }
         }
       }
       const int now = cs + piece * X;
@@ -397,10 +411,11 @@ __global__ __launch_bounds__(512, PT == 1 ? 4 : 2) void adapt_few_kernel(AdaptAr
   using Op = AdaptOp<T>;
   constexpr int X = Op::X, CHUNK = 8 * X, WAVES = 8, AHEAD = PT == 4 ? 2 : 3;   // (AHEAD: runs of channels that a wave has under way)
   constexpr int LINE = 64 / X, LOADS = 16 * LINE / 64;
-  constexpr int UNITS = X == 8 && PT > 1 ? PT / 2 : PT;      // operands of up, as in the second of two launches
+  constexpr int UNITS = X == 8 && PT > 1 ? PT / 2 : PT;      // operands of up and of h, as in the second of two launches
+  constexpr int STEPS = X == 4 ? PT : PT == 1 ? 2 : 3 * UNITS;
   constexpr int TWO = PT < 2 ? PT : 2, WAVE = (16 + TWO * 16) * 8;   // of a wave in LDS: 16 rows and 16 or 32 ranks of 128 bytes, in pieces
   __shared__ __attribute__((aligned(16))) uint4v stage[WAVES * WAVE];
-  __shared__ __attribute__((aligned(16))) uint4v hs[PT * 64];
+  __shared__ __attribute__((aligned(16))) uint4v hs[STEPS * 64];
   int run, chunk;
   item_of(a.chunks, run, chunk);
   const int wave = rfl(threadIdx.x >> 6);
@@ -551,11 +566,12 @@ __global__ __launch_bounds__(512, PT == 1 ? 4 : 2) void adapt_few_kernel(AdaptAr
         v[4 + e] = 0.f;
       }
       if constexpr (X == 8) {
-        uint4v hi, lo;
-        split_ranks(v, hi, lo);
+        uint4v h[3];
+        split_ranks(v, h);
         uint2v* to = (uint2v*)hs + ((2 * wave + (g >> 1)) * 16 + m) * 2 + (g & 1);
-        *to = uint2v{hi[0], hi[1]};
-        to[PT * 64] = uint2v{lo[0], lo[1]};
+#pragma unroll
+        for (int q = 0; q < 3; ++q) to[q * PT * 64] = uint2v{h[q][0], h[q][1]};
+        if (PT == 1) to[3 * 64] = uint2v{0, 0};
       } else {
         hs[(4 * wave + g) * 16 + m] = __builtin_bit_cast(uint4v, float4v{v[0], v[1], v[2], v[3]});
       }
@@ -568,7 +584,7 @@ __global__ __launch_bounds__(512, PT == 1 ? 4 : 2) void adapt_few_kernel(AdaptAr
       for (int t = 0; t < 4; ++t) {
         sum[t] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < PT; ++s) sum[t] = Op::mma(uv[s % UNITS][t], hs[s * 64 + lane], sum[t]);
+        for (int s = 0; s < STEPS; ++s) sum[t] = Op::mma(uv[s % UNITS][t], hs[s * 64 + lane], sum[t]);
       }
       uint4v old[LOADS];
 #pragma unroll

@@ -158,7 +158,7 @@ int launch_adapt(const char* where, const AdaptArgs& a, const AdaptShape& shape,
   e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(where, e);
   const dim3 grid((unsigned)(shape.chunks * a.max_items));
-  const size_t lds = (size_t)(a.rank > 128 ? 2 : 4) * up_steps<T>(a.rank) * 64 * 16;
+  const size_t lds = up_lds(up_steps<T>(a.rank));
   if (shape.stream && shape.lines) hipLaunchKernelGGL((adapt_up_kernel<T, 2, true>), grid, dim3(256), lds, s, a);
   else if (shape.chunk_columns > 64) hipLaunchKernelGGL((adapt_up_kernel<T, 2, false>), grid, dim3(256), lds, s, a);
   else hipLaunchKernelGGL((adapt_up_kernel<T, 4, false>), grid, dim3(256), lds, s, a);

@@ -1,0 +1,44 @@
+"""The calls on a batch's rows around the attention at the ends of their ranges."""
+import numpy as np
+import pytest
+import torch
+
+from tests import test_gpu_adapters as adapters
+
+DEV = "cuda"
+pytestmark = pytest.mark.gpu
+TYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
+FEW, MANY = [3, 20, 1, 64, 70], [300, 1, 2900, 33, 129]
+
+
+# ---- adapters
+
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 48, 64, 72, 96, 128, 136, 168, 256])
+@pytest.mark.parametrize("rows", [FEW, MANY])
+def test_inner_sums_keep_all_bits(rows, rank, typ):
+    """Pairs of ranks whose inner sums, whole numbers of 20 bits, differ by a channel of x, one added and one subtracted."""
+    gen = torch.Generator().manual_seed(rank)
+    c = adapters.Case(typ, [2, 0, 3, 2, 1], rows, 4, 64, [48, 144], rank, seed=rank, scale=False)
+    t = TYPE[typ]
+    x = torch.randint(64, 128, c.x.shape, generator=gen).float()
+    down = torch.randint(64, 127, (4, 2, rank, 64), generator=gen).float()
+    down[:, :, 1::2] = down[:, :, ::2]
+    channel = torch.randint(0, 64, (4, 2, rank // 2, 1), generator=gen)
+    down[:, :, 1::2] += torch.zeros(4, 2, rank // 2, 64).scatter_(3, channel, 1.0)
+    up = torch.zeros(4, 192, rank)
+    for _ in range(2):
+        pair = torch.randint(0, rank // 2, (4, 192, 1), generator=gen)
+        sign = torch.randint(0, 2, (4, 192, 1), generator=gen) * 2.0 - 1
+        up.scatter_(2, 2 * pair, sign).scatter_(2, 2 * pair + 1, -sign)
+    c.x.copy_(x.to(t)), c.down.copy_(down.to(t)), c.up.copy_(up.to(t))
+    c.run()
+    torch.cuda.synchronize()
+    y = c.y.cpu()
+    for r, (a, start) in enumerate(zip(c.adapter, np.cumsum(rows) - rows)):
+        mine = slice(int(start), int(start) + rows[r])
+        for p, (lo, hi) in enumerate(((0, 48), (48, 192))):
+            h = x[mine].double() @ down[a, p].double().T
+            assert (h.abs() @ up[a, lo:hi].double().abs().T).max() < 2 ** 22 and h.max() > 2 ** 18    # (sums are exact, also of their quarters)
+            want = c.base[mine, lo:hi].cpu().double() + h @ up[a, lo:hi].double().T
+            assert torch.equal(y[mine, lo:hi], want.to(t)), (r, p, (y[mine, lo:hi].double() - want).abs().max())
