@@ -7,7 +7,7 @@
 // added up in an order that changes.  The second stages an item's h in LDS, parts added up and scaled, and takes 64 columns a wave at
 // a time.  In bf16, h enters as three bf16 parts, which hold all its 24 bits: two of them side by side fill the contraction of 32 that a rank of 16 would
 // half leave empty; from 24 ranks on one operand of up is multiplied by all three.  Two parts (16 bits of h) took 211.0 us and three take 212.3 for 43 340 rows of rank 16,
-// 337 and 344 for rank 64, 123 and 137 for 9 326 rows of rank 128, but where base and products cancel the rest of a sum was that of 16 bits.
+// 337 and 344 for rank 64, 123 and 137 for 8 326 rows of rank 128, but where base and products cancel the rest of a sum was that of 16 bits.
 //
 // Both are bound by memory: adapters that occur once are the bytes of a decode step, x, base and y those of a prompt.  3584 channels, 4608 columns, rank 16 in
 // bf16: 43 340 rows of prompts 211 us (65 + 150 traced), 5.3 TB/s; 64 rows of as many adapters 11 us, a chain of loads that depend on one another (items, row
@@ -93,18 +93,25 @@ __device__ __forceinline__ void put(T* p, uint4v v) {
   else *(uint4v*)p = v;
 }
 
-// Eight ranks of h as the second product takes them in bf16: three numbers of 8 bits each that add up to all 24 of h.  What is left of h is cut
-// off, not rounded: finite numbers stay finite, and what is left is exact.
-__device__ __forceinline__ void split_ranks(const float* v, uint4v (&part)[3]) {
+// Eight ranks of h as the second product takes them in bf16: N numbers of 8 bits each, three or more, that add up to all 24 of h.  What is left of h is
+// cut off, not rounded: finite numbers stay finite, what is left is exact, and all parts have h's sign.  Where nothing is left a part gives half of itself: none of
+// them is 0 then (but of h below 2^-96, whose halves may be none), which beside an infinite weight would make a NaN of an infinity.
+template <int N>
+__device__ __forceinline__ void split_ranks(const float* v, uint4v (&part)[N]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    float v0 = v[2 * e], v1 = v[2 * e + 1];
+    float left[2] = {v[2 * e], v[2 * e + 1]};
 #pragma unroll
-    for (int q = 0; q < 3; ++q) {
-      const unsigned h0 = __float_as_uint(v0) & 0xffff0000u, h1 = __float_as_uint(v1) & 0xffff0000u;
-      part[q][e] = h0 >> 16 | h1;
-      v0 = __builtin_isinf(v0) ? 0.f : v0 - __uint_as_float(h0);
-      v1 = __builtin_isinf(v1) ? 0.f : v1 - __uint_as_float(h1);
+    for (int q = 0; q < N; ++q) {
+      unsigned bits[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float x = left[i], cut = __uint_as_float(__float_as_uint(x) & 0xffff0000u), half = 0.5f * x;
+        const bool halved = q < N - 1 && cut == x && __builtin_fabsf(x) >= 0x1p-96f;
+        bits[i] = __float_as_uint(halved ? half : cut);
+        left[i] = halved ? half : x - cut;
+      }
+      part[q][e] = bits[0] >> 16 | bits[1];
     }
   }
 }
@@ -229,13 +236,13 @@ __global__ __launch_bounds__(256) void adapt_down_kernel(AdaptArgs a) {
   }
 }
 
-// Operands of h for 16 rows: in bf16 three parts of 32 ranks each, of up to 16 ranks two parts side by side in one; in fp32 16 ranks each.
+// Operands of h for 16 rows: in bf16 three parts of 32 ranks each, of up to 16 ranks four parts, two side by side in one; in fp32 16 ranks each.
 template <typename T>
 __host__ __device__ constexpr int up_steps(int rank) {
   return sizeof(T) == 4 ? (rank + 15) / 16 : rank <= 16 ? 2 : (rank + 31) / 32 * 3;
 }
-// Runs of 16 rows whose h is staged at a time, an operand of one 1 KiB, and the LDS for them.  Weights are read again for the next: 9 326 bf16 rows of rank 128 (12
-// operands) 137 us with four runs, 166 with two; 9 326 fp32 rows of rank 160 (10) 525 and 608.
+// Runs of 16 rows whose h is staged at a time, an operand of one 1 KiB, and the LDS for them.  Weights are read again for the next: 8 326 bf16 rows of rank 128 (12
+// operands) 137 us with four runs, 166 with two; 8 326 fp32 rows of rank 160 (10) 525 and 608.
 __host__ __device__ constexpr int up_staged(int steps) { return steps <= 12 ? 4 : steps <= 16 ? 2 : 1; }
 constexpr size_t up_lds(int steps) { return (size_t)(steps <= 12 ? 4 * steps : 32) * 1024; }
 
@@ -329,11 +336,15 @@ __global__ __launch_bounds__(256) void adapt_up_kernel(AdaptArgs a) {
       }
       uint4v* to = hs + (j >> 4) * steps * 64 + (j & 15);
       if constexpr (X == 8) {
-        uint4v h[3];
-        split_ranks(v, h);
+        auto put_parts = [&](auto parts) {
+          constexpr int N = decltype(parts)::value;
+          uint4v h[N];
+          split_ranks<N>(v, h);
 #pragma unroll
-        for (int q = 0; q < 3; ++q) to[(q * eights + p) * 16] = h[q];
-        if (narrow) to[(3 * eights + p) * 16] = uint4v{0, 0, 0, 0};
+          for (int q = 0; q < N; ++q) to[(q * eights + p) * 16] = h[q];
+        };
+        if (narrow) put_parts(std::integral_constant<int, 4>{});
+        else put_parts(std::integral_constant<int, 3>{});
       } else {
         to[2 * p * 16] = __builtin_bit_cast(uint4v, float4v{v[0], v[1], v[2], v[3]});
         to[(2 * p + 1) * 16] = __builtin_bit_cast(uint4v, float4v{v[4], v[5], v[6], v[7]});
@@ -566,12 +577,12 @@ __global__ __launch_bounds__(512, PT == 1 ? 4 : 2) void adapt_few_kernel(AdaptAr
         v[4 + e] = 0.f;
       }
       if constexpr (X == 8) {
-        uint4v h[3];
-        split_ranks(v, h);
+        constexpr int PARTS = PT == 1 ? 4 : 3;
+        uint4v h[PARTS];
+        split_ranks<PARTS>(v, h);
         uint2v* to = (uint2v*)hs + ((2 * wave + (g >> 1)) * 16 + m) * 2 + (g & 1);
 #pragma unroll
-        for (int q = 0; q < 3; ++q) to[q * PT * 64] = uint2v{h[q][0], h[q][1]};
-        if (PT == 1) to[3 * 64] = uint2v{0, 0};
+        for (int q = 0; q < PARTS; ++q) to[q * PT * 64] = uint2v{h[q][0], h[q][1]};
       } else {
         hs[(4 * wave + g) * 16 + m] = __builtin_bit_cast(uint4v, float4v{v[0], v[1], v[2], v[3]});
       }

@@ -1,4 +1,6 @@
 """The calls on a batch's rows around the attention at the ends of their ranges."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -42,3 +44,26 @@ def test_inner_sums_keep_all_bits(rows, rank, typ):
             assert (h.abs() @ up[a, lo:hi].double().abs().T).max() < 2 ** 22 and h.max() > 2 ** 18    # (sums are exact, also of their quarters)
             want = c.base[mine, lo:hi].cpu().double() + h @ up[a, lo:hi].double().T
             assert torch.equal(y[mine, lo:hi], want.to(t)), (r, p, (y[mine, lo:hi].double() - want).abs().max())
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("rank", [8, 16, 24, 64, 72, 136])
+@pytest.mark.parametrize("rows", [FEW, MANY])
+def test_infinite_weights(rows, rank, typ):
+    """An infinite weight of up gives what the formula gives: infinities of the inner sum's sign, NaN behind a sum of 0 and between
+    infinities of both signs."""
+    c = adapters.Case(typ, [2, 0, 3, 2, 1], rows, 4, 64, [48, 144], rank, seed=rank)
+    c.up[0, 5, 3], c.up[2, 100, rank - 1], c.up[2, 100, 0], c.up[3, 7, 2], c.up[1, 150, rank // 2] = math.inf, math.inf, -math.inf, -math.inf, math.inf
+    c.x[4, 9], c.x[30, 8] = math.inf, -math.inf
+    c.run()
+    torch.cuda.synchronize()
+    x, y, up, seen = c.x.cpu().double(), c.y.cpu().float(), c.up.cpu().double(), 0
+    for r, (a, start) in enumerate(zip(c.adapter, np.cumsum(rows) - rows)):
+        mine = slice(int(start), int(start) + rows[r])
+        for p, (lo, hi) in enumerate(((0, 48), (48, 192))):
+            h = (x[mine, None] * c.ref_down[a, p]).sum(-1)                          # (products one by one: 0 x inf is NaN)
+            want = c.base[mine, lo:hi].cpu().double() + float(c.scale[a]) * (h[:, None] * up[a, None, lo:hi]).sum(-1)
+            want, got = want.to(TYPE[typ]).float(), y[mine, lo:hi]
+            seen += int(torch.isinf(want).sum())
+            assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(nan=0.0), want.nan_to_num(nan=0.0))
+    assert seen > 50
