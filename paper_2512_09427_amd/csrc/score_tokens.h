@@ -60,9 +60,10 @@ __device__ __forceinline__ float rounded_product(float x, float y) {
 #pragma clang fp contract(off)
   return x * y;
 }
-// The states of a wave's lanes together, in all of them.  One that is 0 in the sum adds nothing (its t may be beyond all numbers by then).
+// The states of a wave's lanes together, in all of them.  One that is 0 in the sum adds nothing (its t may be beyond all numbers by then), and one of no
+// tokens has no say in the reference, which may be above all tokens that others have.
 __device__ __forceinline__ ScoreState join_lanes(const ScoreState& s, float scale_log2) {
-  const float m = max_over_wave(s.m), d = s.m - m, f = __builtin_amdgcn_exp2f(d * scale_log2);
+  const float m = max_over_wave(s.l == 0.f ? LOWEST_REF : s.m), d = s.m - m, f = __builtin_amdgcn_exp2f(d * scale_log2);
   const bool none = (f == 0.f && s.l == s.l) || s.l == 0.f;
   return ScoreState{m, sum_over_wave(none ? 0.f : s.l * f), sum_over_wave(none ? 0.f : f * (s.t + s.l * d))};
 }

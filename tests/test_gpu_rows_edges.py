@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from tests import test_gpu_adapters as adapters
+from tests import test_gpu_score_tokens as scores
 
 DEV = "cuda"
 pytestmark = pytest.mark.gpu
@@ -67,3 +68,21 @@ def test_infinite_weights(rows, rank, typ):
             seen += int(torch.isinf(want).sum())
             assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(nan=0.0), want.nan_to_num(nan=0.0))
     assert seen > 50
+
+
+# ---- scores
+
+def check_parts_with_nothing_on(rest, typ):
+    vocab = 131072
+    for on in (slice(70000, None), slice(0, 30), slice(40000, 40001)):
+        x = torch.full((2, vocab), -math.inf)
+        x[0, on] = rest
+        x[1, on] = rest * torch.linspace(0.5, 1, len(x[1, on]))
+        scores.Call(x.to(TYPE[typ]).float(), typ, vocab, [on.start, on.start], 9).run().check()
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("rest", [-3.38e38, -5e30, -1e3, 2.0, 1e3])
+def test_parts_with_nothing_on(rest, typ):
+    """Whole parts of a row are switched off; what is on is far below 0, or above it."""
+    check_parts_with_nothing_on(rest, typ)
