@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <string>
 
 #include "odma_internal.h"
@@ -108,6 +109,9 @@ int odma_score_tokens(odma_pool_t* pool, int64_t n_rows, const void* logits, int
   a.part_len = shape.part_len;
   a.scale = scale;
   a.scale_log2 = scale * 1.4426950408889634f;
+  int power;
+  std::frexp(a.scale_log2, &power);
+  a.far = std::ldexp(1.0f, SCORE_FAR_LOG2 - power);
   hipStream_t s = (hipStream_t)stream;
   const dim3 grid((unsigned)(n_rows * shape.parts));
   if (a.logits_f32) launch_score<float>(a, shape.waves, grid, s);

@@ -24,7 +24,7 @@ namespace {
 constexpr int SCORE_PARTS = 64;             // most parts of a row: a lane each in the joining launch
 constexpr int SCORE_KEPT = 128;             // keys that a wave keeps: a list that is cut down, and what 64 lanes may add
 constexpr int SCORE_RANKED = 128;           // keys that are ranked without another bound
-constexpr float SCORE_FAR = 0x1p100f;
+constexpr int SCORE_FAR_LOG2 = 28;          // scaled logits up to 2^28 either way have a rounded reference
 constexpr float SCORE_SLACK = 8.f;
 typedef unsigned long long u64;
 
@@ -40,6 +40,7 @@ struct ScoreArgs {
   int32_t vocab, n_top, parts, part_len;     // elements of a part
   int32_t logits_f32;
   float scale, scale_log2;
+  float far;                                 // a power of two: far * scale_log2 is exact and at most 2^SCORE_FAR_LOG2
 };
 
 // Floats as whole numbers in the same order; 0 and -0 are one.
@@ -186,10 +187,12 @@ __global__ __launch_bounds__(W * 64) void score_kernel(ScoreArgs a) {
   }
   const float given = token >= 0 && token < a.vocab ? score_element(p + token) : __builtin_nanf("");
   // The lane's state, in powers of two and with a rounded reference: l = sum 2^(c x - r), t = sum 2^(c x - r) (c x - r), c x - r in one rounding.
-  // The reference starts at a logit of -SCORE_FAR; rows whose largest logit is not between it and SCORE_FAR are taken again below.
+  // That rounding is half a step of r, and no term is farther from its value than by a power of it: 2^8 as long as r is within 2^28, while from 2^31 on it
+  // would leave fp32.  So the reference starts at a logit of -far, which lower ones (a mask of -1e9) leave as it is, and rows whose largest
+  // logit is not between -far and far are taken again below.
   // It moves when a logit is 2^SCORE_SLACK times likelier: of 64 lanes one finds a new largest logit in nearly every piece.
   const float c = a.scale_log2, slack = SCORE_SLACK / c;
-  float m = -SCORE_FAR, raise = m, r = rounded_product(m, c), l = 0.f, t = 0.f, top = -INFINITY;    // (top: the largest as it is)
+  float m = -a.far, raise = m, r = rounded_product(m, c), l = 0.f, t = 0.f, top = -INFINITY;    // (top: the largest as it is)
   int larger = 0, held = 0, round = 0;
   u64 bound = (u64)ORDERED_OFF << 32 | 0xffffffffu;          // keys above it are kept
   float least = -INFINITY;                                   // what is not above it cannot be among them
@@ -338,7 +341,7 @@ __global__ __launch_bounds__(W * 64) void score_kernel(ScoreArgs a) {
   top = max_over_wave(lane < W ? tops[lane] : -INFINITY);
   larger = (int)sum_over_wave(lane < W ? (unsigned)larger_of[lane] : 0u);
   const int total = (int)sum_over_wave(lane < W ? (unsigned)held_of[lane] : 0u);
-  if (top > SCORE_FAR || (s.l == 0.f && top > -INFINITY)) {  // (the whole work-group) element by element, by differences
+  if (top > a.far || (top <= -a.far && top > -INFINITY)) {   // (the whole work-group) element by element, by differences
     s = ScoreState{LOWEST_REF, 0.f, 0.f};
     for (int i = e0 + threadIdx.x; i < e1; i += N) {
       const float x = score_element(p + i), most = fmaxf(x, s.m);

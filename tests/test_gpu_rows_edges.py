@@ -86,3 +86,42 @@ def check_parts_with_nothing_on(rest, typ):
 def test_parts_with_nothing_on(rest, typ):
     """Whole parts of a row are switched off; what is on is far below 0, or above it."""
     check_parts_with_nothing_on(rest, typ)
+
+
+def logits_with(fill, vocab, typ):
+    """Rows with `fill` in some places, in all, or nearly all."""
+    x = scores.some(8, vocab, typ, seed=vocab)
+    x[0, : vocab // 2] = fill
+    x[1, :] = fill
+    x[1, [0, vocab // 3, vocab - 1]] = torch.tensor([1.0, 2.0, 0.5])
+    x[2] = fill
+    x[3, ::2] = fill
+    x[4, :4096] = fill
+    x[5, vocab // 2] = fill
+    x[6] = fill * (1 + torch.rand(vocab, generator=torch.Generator().manual_seed(1)) / 2)
+    x[7, :] = -math.inf
+    x[7, vocab // 2:] = fill
+    return x.to(TYPE[typ]).float()
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("fill", [-6e4, -1e6, -1e9, -1e10, -1e20, -1e30, -3.38e38, 1e6, 3e7, 1e10, 1e20, 1e29, 1e31, 1e38])
+@pytest.mark.parametrize("vocab", [9, 4099, 40009])             # (the last is cut into parts)
+def test_logits_far_from_0(vocab, fill, typ):
+    for scale in (1.0, 2.0 ** -24, 1e5, 2.0 ** 24):
+        tokens = [0, vocab // 3, vocab - 1, 2, 1, vocab // 2, 3, vocab - 1]
+        scores.Call(logits_with(fill, vocab, typ), typ, vocab, tokens, 5, scale=scale).run().check()
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [300, 700])                    # eight waves of a work-group, and four
+def test_many_rows_far_from_0(rows, typ):
+    vocab = 2501
+    x = torch.cat([logits_with(f, vocab, typ) for f in (-1e4, -1e9, -1e30, 1e10, 1e30)]).repeat(rows // 40 + 1, 1)[:rows]
+    scores.Call(x, typ, vocab, [37 * r % vocab for r in range(rows)], 5).run().check()
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f32"])
+@pytest.mark.parametrize("rest", [-1e30, -1e20, -1e9, 1e9, 1e10])
+def test_parts_with_nothing_on_far_from_0(rest, typ):
+    check_parts_with_nothing_on(rest, typ)
