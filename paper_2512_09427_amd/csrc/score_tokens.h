@@ -392,6 +392,7 @@ __global__ __launch_bounds__(256) void score_join_kernel(ScoreArgs a) {
   __shared__ int listed;
   const int lane = threadIdx.x & 63;
   const int64_t row = blockIdx.x;
+  if (!row_there(a, row)) return;                            // (its logits may not exist)
   // one round of loads: the states, every part's j-th largest, the keys, the given token
   const float4 v = a.part_state[row * a.parts + min(lane, a.parts - 1)];
   const u64* keys = a.part_key + row * a.parts * a.n_top;
@@ -408,13 +409,11 @@ __global__ __launch_bounds__(256) void score_join_kernel(ScoreArgs a) {
     held[i] = at < n ? keys[at] : 0;
   }
   const int token = a.tokens ? a.tokens[row] : ODMA_TOKEN_NONE;
-  const bool there = row_there(a, row);
   float given = 0.f;
   if (token >= 0 && token < a.vocab) {
     const int64_t at = row * a.stride + token;
     given = a.logits_f32 ? score_element((const float*)a.logits + at) : score_element((const unsigned short*)a.logits + at);
   }
-  if (!there) return;
   if (threadIdx.x == 0) listed = 0;
   ScoreState s{LOWEST_REF, 0.f, 0.f};
   int larger = 0;

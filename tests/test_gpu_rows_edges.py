@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2512_09427_amd import binding as B
 from tests import test_gpu_adapters as adapters
 from tests import test_gpu_score_tokens as scores
 
@@ -125,3 +126,15 @@ def test_many_rows_far_from_0(rows, typ):
 @pytest.mark.parametrize("rest", [-1e30, -1e20, -1e9, 1e9, 1e10])
 def test_parts_with_nothing_on_far_from_0(rest, typ):
     check_parts_with_nothing_on(rest, typ)
+
+
+@pytest.mark.parametrize("rows,vocab", [(6, 40009), (600, 3001)])   # cut into parts, whole
+def test_rows_that_are_not_there_have_no_logits(rows, vocab):
+    """The tensor of logits ends with the last row that is there; tokens of the others may be any."""
+    x = scores.some(rows, vocab, "bf16", seed=5)
+    slots = torch.full((rows,), B.SLOT_NONE, dtype=torch.int64, device=DEV)
+    slots[0], slots[2] = 0, 5
+    for top in (0, 6):
+        c = scores.Call(x, "bf16", vocab, [r % vocab for r in range(rows)], top, slots=slots)
+        c.logits = c.logits[:3 * vocab].clone()
+        c.run().check()
