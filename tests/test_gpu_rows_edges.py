@@ -7,6 +7,7 @@ import torch
 
 from paper_2512_09427_amd import binding as B
 from tests import test_gpu_adapters as adapters
+from tests import test_gpu_add_norm as norms
 from tests import test_gpu_score_tokens as scores
 
 DEV = "cuda"
@@ -138,3 +139,18 @@ def test_rows_that_are_not_there_have_no_logits(rows, vocab):
         c = scores.Call(x, "bf16", vocab, [r % vocab for r in range(rows)], top, slots=slots)
         c.logits = c.logits[:3 * vocab].clone()
         c.run().check()
+
+
+# ---- residual rows
+
+@pytest.mark.parametrize("typ,res", norms.TYPES)
+@pytest.mark.parametrize("rows,width", [(5, 512), (5, 1000), (5, 2048), (6, 3584), (3, 8192), (2, 16384), (2, 32768), (16400, 520), (1030, 8192), (49170, 2056)])
+def test_squares_that_add_up_beyond_fp32(rows, width, typ, res):
+    """Rows whose mean square is within fp32's range and whose sum of squares is not, beside others."""
+    def edit(blk, old):
+        blk[::2] *= 2e18
+        old[::2] *= 1e18
+    for post in (False, True):
+        if not post or rows < 20000:
+            norms.Case(typ, res, rows, width, post=post, seed=width, edit=edit).run().check()
+    norms.Case(typ, res, rows, width, block=False, eps=0.0, edit=edit).run().check()
