@@ -22,7 +22,8 @@ int refuse(const char* where, const char* why) {
 
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
-constexpr int64_t MAX_ROWS = (int64_t)1 << 22;       // of odma_add_norm (a launch has fewer than 2^32 threads, 1024 of them a row)
+constexpr int64_t MAX_ROWS = (int64_t)1 << 22;       // of odma_add_norm
+constexpr int64_t MAX_THREADS = ((int64_t)1 << 32) - 1;   // of a launch
 constexpr int64_t MAX_LISTED = (int64_t)1 << 27;     // rows of lists
 constexpr int64_t MAX_WG = (1 << 24) - 1;            // work-groups of 256 threads of a launch
 // Work-groups up to which the making of lists is dealt out, several requests each beyond: 1 024 requests of one row 6.7 us with 1 024 and 8.5 with 256, 2 048
@@ -39,7 +40,8 @@ void launch_add_norm(const AddNormArgs& a, hipStream_t s) {
 // a compute unit some widths take fewer waves with more pieces each, which wait for each other less.  us a call with few and with many waves: 3584
 // channels 16 384 rows 83.3 (eight waves) and 87.5 (two), 65 869 beside an fp32 residual 526 and 515; 8 192 channels 256 rows 4.9 (16) and 5.0 (8), 1 024
 // 13.0 and 11.6, 4 096 51 and 48.6; 520 channels 4 096 fp32 rows 7.6 (two) and 8.1 (one), 32 768 bf16 rows 32.3 and 29.6.  2 048 channels in one wave were
-// slower throughout (4 096 rows 13.1 and 11.6 in four), in two the same as in four.
+// slower throughout (4 096 rows 13.1 and 11.6 in four), in two the same as in four.  MAX_ROWS rows of 16 waves would be one thread more than a launch may have:
+// they take eight waves.
 constexpr int64_t NORM_MANY_2 = 64, NORM_MANY_8 = 192, NORM_MANY_16 = 4;   // rows a compute unit, by pieces
 template <typename T, typename R>
 void launch_add_norm(const AddNormArgs& a, int64_t n_cu, hipStream_t s) {
@@ -52,6 +54,7 @@ void launch_add_norm(const AddNormArgs& a, int64_t n_cu, hipStream_t s) {
   else if (pieces <= 8) launch_add_norm<T, R, 8, 1>(a, s);
   else if (pieces <= 16 && a.n_rows >= NORM_MANY_16 * n_cu) launch_add_norm<T, R, 8, 2>(a, s);
   else if (pieces <= 16) launch_add_norm<T, R, 16, 1>(a, s);
+  else if (a.n_rows * 1024 > MAX_THREADS) launch_add_norm<T, R, 8, 8>(a, s);
   else if (pieces <= 32) launch_add_norm<T, R, 16, 2>(a, s);
   else launch_add_norm<T, R, 16, 4>(a, s);
 }

@@ -154,3 +154,22 @@ def test_squares_that_add_up_beyond_fp32(rows, width, typ, res):
         if not post or rows < 20000:
             norms.Case(typ, res, rows, width, post=post, seed=width, edit=edit).run().check()
     norms.Case(typ, res, rows, width, block=False, eps=0.0, edit=edit).run().check()
+
+
+@pytest.mark.parametrize("width", [8200, 16392])
+def test_as_many_rows_as_a_call_takes(width):
+    """2^22 rows of more channels than eight waves take at a time; most of them are not there."""
+    rows, at = 1 << 22, [0, 1, 77777, (1 << 22) - 1]
+    c = norms.Case("bf16", "bf16", 1, width, gate="sigmoid", one_gate=True, seed=width)
+    slots = torch.full((rows,), B.SLOT_NONE, dtype=torch.int64, device=DEV)
+    slots[at] = 0
+    x = torch.empty(rows, width, dtype=torch.bfloat16, device=DEV)
+    x[:2000], x[-2000:] = -7, -7
+    # one block, gate and residual for all rows; it is not kept
+    c.pool.odma_add_norm(rows, c.how, c.block, 0, c.old, 0, slots, None, x)
+    torch.cuda.synchronize()
+    c.x.copy_(x[:1])
+    c.check(keep=False)
+    assert all(torch.equal(x[r], x[0]) for r in at) and (x[2:2000] == -7).all() and (x[-2000:-1] == -7).all()
+    del x
+    torch.cuda.empty_cache()
