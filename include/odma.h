@@ -497,7 +497,7 @@ int odma_add_norm(odma_pool_t* pool, int64_t n_rows, const odma_add_norm_t* how,
  *   row_start  DEVICE int64[n + 1] or NULL (one row each): request r's rows are row_start[r] .. row_start[r + 1] - 1
  *              (odma_build_tables; it does not decrease)
  *   row_order  DEVICE int32[max_rows]: the rows of requests with an adapter, by adapter, and by request under each; -1 behind them.
- *              Rows past max_rows of them do not exist
+ *              Rows past max_rows of them do not exist, and one whose number is past 2^31 - 1 stands as -1
  *   items      DEVICE int32[max_items][4]: {adapter, first, count, 0}: rows row_order[first] .. row_order[first + count - 1] have that
  *              adapter, 1 <= count <= ODMA_ADAPTER_ITEM_ROWS; or {ODMA_ADAPTER_NONE, 0, 0, 0}: an item that is empty.  Adapters
  *              ascend; the one with d other adapters in front of it begins at item first / ODMA_ADAPTER_ITEM_ROWS + d

@@ -25,7 +25,9 @@ struct ListArgs {
   int32_t per;                       // requests of a work-group
 };
 
-// LDS: the bit map, (n_adapters + 31) / 32 words.
+// LDS: the bit map, (n_adapters + 31) / 32 words.  CAPPED: for batches whose sums could be beyond 32 bits, which stay at max_rows (2^27 at most) once they are
+// there; what is behind it does not exist.  256 requests of one row 3.00 us without and 3.09 with it, 512 prompts 4.13 and 4.31.
+template <bool CAPPED>
 __global__ __launch_bounds__(256) void group_adapters_kernel(ListArgs a) {
   extern __shared__ unsigned present[];
   __shared__ unsigned sums[2][4][6];
@@ -40,6 +42,7 @@ __global__ __launch_bounds__(256) void group_adapters_kernel(ListArgs a) {
     return (unsigned)(rows < 0 ? 0 : rows < a.max_rows ? rows : a.max_rows);
   };
   const unsigned most = (unsigned)a.max_rows;
+  auto plus = [&](unsigned x, unsigned y) { return CAPPED ? min(x + y, most) : x + y; };
   unsigned all = 0, distinct = 0;                            // rows of the batch that have an adapter, and adapters that have rows
   for (int i = 0; i < a.per; ++i) {
     const int r = blockIdx.x * a.per + i;
@@ -53,16 +56,16 @@ __global__ __launch_bounds__(256) void group_adapters_kernel(ListArgs a) {
       const unsigned rows = rows_of(s, ad);
       if (rows == 0) continue;
       if (i == 0) atomicOr(&present[ad >> 5], 1u << (ad & 31));
-      total += rows;
-      if (ad < mine) first += rows;
-      if (ad == mine) same += rows;
-      if (ad < mine || (ad == mine && s < r)) before += rows;
+      total = plus(total, rows);
+      if (ad < mine) first = plus(first, rows);
+      if (ad == mine) same = plus(same, rows);
+      if (ad < mine || (ad == mine && s < r)) before = plus(before, rows);
       if (ad == mine && s < r) earlier = 1;
     }
-    before = sum_over_wave(before);
-    first = sum_over_wave(first);
-    same = sum_over_wave(same);
-    total = sum_over_wave(total);
+    before = over_wave(before, plus);
+    first = over_wave(first, plus);
+    same = over_wave(same, plus);
+    total = over_wave(total, plus);
     earlier = sum_over_wave(earlier);
     unsigned (*part)[6] = sums[i & 1];                       // (two sets: the one of the request before may still be read)
     if (lane == 0) {
@@ -73,12 +76,12 @@ __global__ __launch_bounds__(256) void group_adapters_kernel(ListArgs a) {
       part[wave][4] = earlier;
     }
     __syncthreads();
-    auto of_all = [&](int k) { return part[0][k] + part[1][k] + part[2][k] + part[3][k]; };
+    auto of_all = [&](int k) { return plus(plus(part[0][k], part[1][k]), plus(part[2][k], part[3][k])); };
     before = of_all(0);
     first = of_all(1);
     same = of_all(2);
     all = of_all(3);
-    earlier = of_all(4);
+    earlier = part[0][4] | part[1][4] | part[2][4] | part[3][4];
     // adapters with rows, all of them and those in front of this one: every wave counts for itself
     unsigned d = 0, in_front = 0;
     for (int wd = lane; wd < words; wd += 64) {
@@ -92,11 +95,12 @@ __global__ __launch_bounds__(256) void group_adapters_kernel(ListArgs a) {
     if (rows) {
       const long long from = a.row_start ? a.row_start[r] : r;
       for (unsigned j = blockIdx.y * 256 + tid; j < rows && before + j < most; j += gridDim.y * 256)
-        a.row_order[before + j] = (int32_t)(from + j);
+        a.row_order[before + j] = from + j <= INT32_MAX ? (int32_t)(from + j) : -1;
       if (!earlier && blockIdx.y == 0) {                     // the adapter's items, and the one that may stay empty behind them
-        const unsigned at = first / ITEM_ROWS + in_front, end = (first + same) / ITEM_ROWS + in_front + 1;
+        const unsigned behind = plus(first, same), stop = min(behind, most);
+        const unsigned at = first / ITEM_ROWS + in_front, end = behind / ITEM_ROWS + in_front + 1;
         for (unsigned j = tid; at + j < end && at + j < (unsigned)a.max_items; j += 256) {
-          const unsigned f = first + j * ITEM_ROWS, stop = min(first + same, most);
+          const unsigned f = first + j * ITEM_ROWS;
           a.items[at + j] = f < stop ? make_int4(mine, (int)f, (int)min(stop - f, (unsigned)ITEM_ROWS), 0) : make_int4(ODMA_ADAPTER_NONE, 0, 0, 0);
         }
       }

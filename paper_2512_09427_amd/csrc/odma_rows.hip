@@ -250,7 +250,10 @@ int odma_group_adapters(odma_pool_t* pool, int32_t n, const int32_t* adapter, in
   a.per = std::max(1, (n + LIST_WG - 1) / LIST_WG);
   const int64_t wg = std::max(1, (n + a.per - 1) / a.per), longest = row_start ? max_rows / wg : 1;
   const int64_t split = std::max<int64_t>(1, std::min<int64_t>((longest + 1023) / 1024, LIST_WG / wg));
-  hipLaunchKernelGGL(group_adapters_kernel, dim3((unsigned)wg, (unsigned)split), dim3(256), (size_t)(n_adapters + 31) / 32 * 4, (hipStream_t)stream, a);
+  const dim3 grid((unsigned)wg, (unsigned)split);
+  const size_t lds = (size_t)(n_adapters + 31) / 32 * 4;
+  if (row_start && n * max_rows > UINT32_MAX) hipLaunchKernelGGL((group_adapters_kernel<true>), grid, dim3(256), lds, (hipStream_t)stream, a);
+  else hipLaunchKernelGGL((group_adapters_kernel<false>), grid, dim3(256), lds, (hipStream_t)stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(where, e);
   return ODMA_OK;

@@ -72,6 +72,44 @@ def test_infinite_weights(rows, rank, typ):
     assert seen > 50
 
 
+def lists_of(adapter, start, n_adapters, max_rows, max_items):
+    """The lists, for any number of rows."""
+    order, items = np.full(max_rows, -1), np.tile(np.array([B.ADAPTER_NONE, 0, 0, 0]), (max_items, 1))
+    at, seen = 0, 0
+    for a in range(n_adapters):
+        first, some = at, False
+        for r in np.flatnonzero(adapter == a):
+            some = some or start[r + 1] > start[r]
+            row = np.arange(start[r], start[r] + min(start[r + 1] - start[r], max_rows - at))
+            order[at:at + len(row)] = np.where(row < 2 ** 31, row, -1)
+            at += len(row)
+        for f in range(first, at, 64):
+            items[first // 64 + seen + (f - first) // 64] = a, f, min(64, at - f), 0
+        seen += some
+    return order, items
+
+
+ROWS = [[1 << 27] * 70, [100, 1 << 40, 3, 0, 5] * 9, [300] + [0] * 9 + [(1 << 31) - 301, 7, 1 << 32, 9, (1 << 27) - 1], [1 << 22] * 1500, [5, 1 << 27, 1 << 27] * 60]
+
+
+@pytest.mark.parametrize("rows,max_rows", [(r, m) for r in ROWS for m in (1, 63, 1000, 70001)] + [(ROWS[0], 1 << 26), (ROWS[3], 4000001), (ROWS[4], 30000000)])
+def test_lists_of_more_rows_than_32_bits_count(rows, max_rows):
+    """Also with lists so long that sums of what fits into them are beyond 32 bits."""
+    n = len(rows)
+    start = np.concatenate([[0], np.cumsum(np.array(rows, np.int64))])
+    p, rng = adapters.pool(), np.random.default_rng(n)
+    for adapter in (np.arange(n) // 33, (np.arange(n) < 34).astype(np.int64), rng.integers(-1, 5, n))[:3 if max_rows < 1 << 17 else 2]:
+        n_adapters = int(adapter.max()) + 1
+        max_items = max_rows // 64 + min(n, n_adapters) + 2
+        order = torch.full((max_rows + 8,), 77, dtype=torch.int32, device=DEV)
+        items = torch.full((max_items + 2, 4), 77, dtype=torch.int32, device=DEV)
+        ad, rs = torch.tensor(adapter, dtype=torch.int32, device=DEV), torch.tensor(start, device=DEV)
+        p.odma_group_adapters(n, ad, n_adapters, rs, max_rows, order, max_items, items)
+        want = [torch.from_numpy(w).to(DEV) for w in lists_of(adapter, start, n_adapters, max_rows, max_items)]
+        assert torch.equal(order[:max_rows].long(), want[0]) and torch.equal(items[:max_items].long(), want[1])
+        assert (order[max_rows:] == 77).all() and (items[max_items:] == 77).all()
+
+
 # ---- scores
 
 def check_parts_with_nothing_on(rest, typ):

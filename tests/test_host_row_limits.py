@@ -22,3 +22,14 @@ def test_add_norm_launches_fewer_threads_than_a_launch_may_have(runtime):  # noq
                     assert grid[0] * max(256, 64 * waves) < 1 << 32, (n, width, name, grid)
                     assert waves * pieces * 512 >= width and grid[0] * (4 // waves if waves < 4 else 1) >= n
     """))
+
+
+def test_group_adapters_of_batches_beyond_32_bits(runtime):  # noqa: F811
+    """Lists whose sums may be beyond 32 bits are made by a kernel of their own."""
+    run(runtime, textwrap.dedent(CALLS) + textwrap.dedent("""
+        p = make_pool(max_requests=3000)
+        for n, max_rows, start, capped in ((2, 1 << 27, OFFS, False), (31, 1 << 27, OFFS, False), (32, 1 << 27, OFFS, True), (32, (1 << 27) - 1, OFFS, False),
+                                           (3000, 1431655, OFFS, False), (3000, 1431656, OFFS, True), (3000, 1 << 27, None, False)):
+            (name, grid, lds), = launched(lambda: group(p, n=n, max_rows=max_rows, start=start, max_items=(max_rows >> 6) + 4))
+            assert "group_adapters_kernel" in name and ("Lb1E" in name) == capped, (n, max_rows, name)
+    """))
