@@ -514,7 +514,7 @@ typedef struct odma_adapters {
   const int32_t* ranks;      /* DEVICE [n_adapters] or NULL (rank): of every adapter, taken as 0 to rank and as the next multiple of 8; what
                                 lies behind it in down and up is ignored */
   int32_t n_adapters, rank;  /* rank: a multiple of 8 up to ODMA_MAX_RANK */
-  int32_t width;             /* channels of a row of x: a multiple of 8 */
+  int32_t width;             /* channels of a row of x: a multiple of 8 up to ODMA_MAX_WIDTH */
   int32_t n_parts;           /* 1..ODMA_MAX_PARTS */
   int32_t part_start[ODMA_MAX_PARTS + 1];   /* columns of part p: part_start[p] .. part_start[p + 1] - 1; from 0 on, multiples of 16 */
 } odma_adapters_t;
@@ -530,7 +530,9 @@ size_t odma_adapt_scratch_bytes(const odma_pool_t* pool, const odma_adapters_t* 
  *   x, base, y         DEVICE rows, row i at element i * its stride.  y may be base itself (same stride), else it lies apart from x and base;
  *                      rows of y that are in no item stay as they were.  Pointers and strides are multiples of 16 bytes
  *   scratch            DEVICE, odma_adapt_scratch_bytes() bytes or more, 256-byte aligned, any contents; calls that may overlap need
- *                      scratch of their own.  Uses no workspace of the pool */
+ *                      scratch of their own.  Uses no workspace of the pool
+ * n_rows <= 2^27.  max_items, as the next multiple of 32, times the parts' columns in pieces of 512 (a part's last one may be shorter) and times n_parts x rank
+ * in pieces of 64 must both be below 2^24. */
 int odma_adapt_rows(odma_pool_t* pool, int64_t n_rows, const odma_adapters_t* adapters, int32_t max_items, const int32_t* items,
                     const int32_t* row_order, const void* x, int64_t x_stride, const void* base, int64_t base_stride, void* y,
                     int64_t y_stride, void* scratch, size_t scratch_bytes, void* stream);

@@ -33,3 +33,18 @@ def test_group_adapters_of_batches_beyond_32_bits(runtime):  # noqa: F811
             (name, grid, lds), = launched(lambda: group(p, n=n, max_rows=max_rows, start=start, max_items=(max_rows >> 6) + 4))
             assert "group_adapters_kernel" in name and ("Lb1E" in name) == capped, (n, max_rows, name)
     """))
+
+
+def test_adapt_rows_takes_what_the_header_says(runtime):  # noqa: F811
+    run(runtime, textwrap.dedent(CALLS) + textwrap.dedent("""
+        p = make_pool()
+        for cols, rank in (((64, 32), 16), ((4096, 512, 520 - 8), 16), ((16,), 256), ((1040, 16, 16, 16), 256)):
+            pieces = max(sum(-(-c // 512) for c in cols), -(-len(cols) * rank // 64))
+            most = ((1 << 24) - 1) // pieces // 32 * 32
+            ad = make(part_cols=cols, rank=rank)
+            wide = dict(n=1 << 27, ad=ad, bs=sum(cols), ys=sum(cols))
+            assert len(launched(lambda: adapt(p, max_items=most, **wide))) == 2 and p.odma_adapt_scratch_bytes(ad, most)
+            assert refused(adapt, p, max_items=most + 1, **wide), (cols, rank)
+        adapt(p, ad=make(width=32768), xs=32768)
+        assert refused(adapt, p, ad=make(width=32776), xs=32776) and refused(adapt, p, n=(1 << 27) + 1)
+    """))
