@@ -95,6 +95,7 @@ __global__ __launch_bounds__(W > 4 ? W * 64 : 256) void add_norm_kernel(AddNormA
       for (int i = 0; i < W; ++i) s += part[turn][mine][i];
       if (s == INFINITY) {
         small = 0.f;
+#pragma unroll 1
         for (int i = 0; i < W; ++i) small += part[turn][mine][i] == INFINITY ? again[turn][mine][i] : part[turn][mine][i] * TINY * TINY;
       }
     }
