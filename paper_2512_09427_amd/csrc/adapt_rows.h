@@ -94,8 +94,8 @@ __device__ __forceinline__ void put(T* p, uint4v v) {
 }
 
 // Eight ranks of h as the second product takes them in bf16: N numbers of 8 bits each, three or more, that add up to all 24 of h.  What is left of h is
-// cut off, not rounded: finite numbers stay finite, what is left is exact, and all parts have h's sign.  Where nothing is left a part gives half of itself: none of
-// them is 0 then (but of h below 2^-96, whose halves may be none), which beside an infinite weight would make a NaN of an infinity.
+// cut off, not rounded: finite numbers stay finite, what is left is exact, and all parts have h's sign.  Where nothing is left a part gives half of itself, so that
+// none is 0 but of h of 0 (and of some below 2^-130), which beside an infinite weight would make a NaN of an infinity.
 template <int N>
 __device__ __forceinline__ void split_ranks(const float* v, uint4v (&part)[N]) {
 #pragma unroll
@@ -107,7 +107,7 @@ __device__ __forceinline__ void split_ranks(const float* v, uint4v (&part)[N]) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const float x = left[i], cut = __uint_as_float(__float_as_uint(x) & 0xffff0000u), half = 0.5f * x;
-        const bool halved = q < N - 1 && cut == x && __builtin_fabsf(x) >= 0x1p-96f;
+        const bool halved = q < N - 1 && cut == x;
         bits[i] = __float_as_uint(halved ? half : cut);
         left[i] = halved ? half : x - cut;
       }
