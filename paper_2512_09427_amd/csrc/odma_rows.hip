@@ -86,13 +86,16 @@ constexpr int ADAPT_UP_WG = 1024;
 // Runs of 16 rows of the items, as many as there can be if the lists are of these rows, in eights
 inline int64_t few_runs(int64_t n_rows, int64_t items) { return (n_rows / 16 + std::min(items, n_rows) + 7) / 8 * 8; }
 
+// Bytes of an element of the batch's rows: those of fp8 pools are bf16.
+inline int row_bytes_of(const odma_pool_t* pool) { return pool->elem_bytes == 4 ? 4 : 2; }
+
 // What the adapters' launches look like, or why they are refused.  n_rows < 0: for the scratch of any number of rows.
 struct AdaptShape {
   int flat, tiles, groups, splits, split_channels, chunk_columns, chunks;
   bool few, stream, lines;
   size_t scratch;
 };
-const char* adapt_shape(const odma_adapters_t* ad, int elem_bytes, int64_t n_rows, int64_t max_items, AdaptShape* shape) {
+const char* adapt_shape(const odma_adapters_t* ad, int row_bytes, int64_t n_rows, int64_t max_items, AdaptShape* shape) {
   if (!ad || !ad->down || !ad->up) return "adapters without weights";
   if (ad->n_adapters < 1 || ad->n_adapters > ODMA_MAX_ADAPTERS) return "1 to ODMA_MAX_ADAPTERS adapters";
   if (ad->rank < 8 || ad->rank > ODMA_MAX_RANK || ad->rank % 8) return "the rank must be a multiple of 8 up to ODMA_MAX_RANK";
@@ -124,11 +127,11 @@ const char* adapt_shape(const odma_adapters_t* ad, int elem_bytes, int64_t n_row
   const int few_wg = ad->rank <= 16 ? ADAPT_FEW_WG : ad->n_parts > 1 ? ADAPT_FEW_WG_PARTS : ADAPT_FEW_WG_WIDE;
   int few_columns = 512;
   while (few_columns < 4096 && runs * chunks_of(few_columns) > few_wg) few_columns *= 2;
-  const int64_t work = (int64_t)(ad->rank + 15) / 16 * 16 * ad->width * (elem_bytes == 4 ? 8 : 2);
-  const int64_t bound = std::min<int64_t>(ADAPT_FEW_WORK + ADAPT_FEW_ROW * n_rows, elem_bytes == 4 ? ADAPT_FEW_MOST_F32 : ADAPT_FEW_MOST);
+  const int64_t work = (int64_t)(ad->rank + 15) / 16 * 16 * ad->width * (row_bytes == 4 ? 8 : 2);
+  const int64_t bound = std::min<int64_t>(ADAPT_FEW_WORK + ADAPT_FEW_ROW * n_rows, row_bytes == 4 ? ADAPT_FEW_MOST_F32 : ADAPT_FEW_MOST);
   shape->few = ad->rank <= 64 && n_rows >= 0 && n_rows <= ADAPT_FEW && items <= 1024 && cols <= 1 << 17 &&
                work * std::max<int64_t>(runs * chunks_of(few_columns), ADAPT_FEW_CU) <= bound * ADAPT_FEW_CU;
-  shape->stream = n_rows * cols * elem_bytes > (int64_t)4 << 20 && items * cols / 512 >= ADAPT_UP_WG;
+  shape->stream = n_rows * cols * row_bytes > (int64_t)4 << 20 && items * cols / 512 >= ADAPT_UP_WG;
   shape->chunk_columns = shape->few ? few_columns : 64;
   while (!shape->few && shape->chunk_columns < 512 && items * cols / shape->chunk_columns > ADAPT_UP_WG) shape->chunk_columns *= 2;
   if ((items + 31) / 32 * 32 * std::max<int64_t>(chunks_of(shape->chunk_columns), shape->splits * shape->groups) > MAX_WG) return "too many items";
@@ -262,7 +265,7 @@ int odma_group_adapters(odma_pool_t* pool, int32_t n, const int32_t* adapter, in
 size_t odma_adapt_scratch_bytes(const odma_pool_t* pool, const odma_adapters_t* adapters, int32_t max_items) {
   const char* where = "odma_adapt_scratch_bytes";
   AdaptShape shape;
-  const char* why = pool ? adapt_shape(adapters, (int)pool->elem_bytes, -1, max_items, &shape) : "null pool";
+  const char* why = pool ? adapt_shape(adapters, row_bytes_of(pool), -1, max_items, &shape) : "null pool";
   if (why) {
     refuse(where, why);
     return 0;
@@ -280,9 +283,10 @@ int odma_adapt_rows(odma_pool_t* pool, int64_t n_rows, const odma_adapters_t* ad
   if (n_rows < 0 || !items || !row_order || !x || !base || !y || !scratch) return refuse(where, "invalid argument");
   if (n_rows > MAX_LISTED) return refuse(where, "too many rows");
   AdaptShape shape;
-  const char* why = adapt_shape(adapters, (int)pool->elem_bytes, n_rows, max_items, &shape);
+  const int row_bytes = row_bytes_of(pool);
+  const char* why = adapt_shape(adapters, row_bytes, n_rows, max_items, &shape);
   if (why) return refuse(where, why);
-  const int unit = pool->elem_bytes == 4 ? 4 : 8;              // elements of 16 bytes
+  const int unit = 16 / row_bytes;                            // elements of 16 bytes
   if (!aligned(x, 16) || !aligned(base, 16) || !aligned(y, 16) || x_stride < 0 || x_stride % unit || base_stride < 0 || base_stride % unit ||
       y_stride < 0 || y_stride % unit)
     return refuse(where, "rows must start on 16-byte boundaries");
@@ -292,8 +296,8 @@ int odma_adapt_rows(odma_pool_t* pool, int64_t n_rows, const odma_adapters_t* ad
   if (!aligned(items, 16) || !aligned(scratch, 256)) return refuse(where, "items must be 16-byte aligned, scratch 256-byte aligned");
   if (scratch_bytes < shape.scratch) return refuse(where, "scratch smaller than odma_adapt_scratch_bytes()");
   // whole lines of base and y in every work-group's columns
-  shape.lines = aligned(base, 128) && aligned(y, 128) && base_stride * pool->elem_bytes % 128 == 0 && y_stride * pool->elem_bytes % 128 == 0;
-  for (int p = 1; p < adapters->n_parts; ++p) shape.lines = shape.lines && adapters->part_start[p] * pool->elem_bytes % 128 == 0;
+  shape.lines = aligned(base, 128) && aligned(y, 128) && base_stride * row_bytes % 128 == 0 && y_stride * row_bytes % 128 == 0;
+  for (int p = 1; p < adapters->n_parts; ++p) shape.lines = shape.lines && adapters->part_start[p] * row_bytes % 128 == 0;
   AdaptArgs a;
   a.down = adapters->down;
   a.up = adapters->up;
@@ -326,7 +330,7 @@ int odma_adapt_rows(odma_pool_t* pool, int64_t n_rows, const odma_adapters_t* ad
   for (int p = 0; p < ODMA_MAX_PARTS; ++p)
     a.part_chunk[p + 1] = a.part_chunk[p] + (a.part_start[p + 1] - a.part_start[p] + a.chunk_columns - 1) / a.chunk_columns;
   hipStream_t s = (hipStream_t)stream;
-  return pool->elem_bytes == 4 ? launch_adapt<float>(where, a, shape, s) : launch_adapt<unsigned short>(where, a, shape, s);
+  return row_bytes == 4 ? launch_adapt<float>(where, a, shape, s) : launch_adapt<unsigned short>(where, a, shape, s);
 }
 
 }  // extern "C"

@@ -49,6 +49,17 @@ def test_inner_sums_keep_all_bits(rows, rank, typ):
             assert torch.equal(y[mine, lo:hi], want.to(t)), (r, p, (y[mine, lo:hi].double() - want).abs().max())
 
 
+@pytest.mark.parametrize("total,cols", [([3, 20, 1, 64], [64, 48]), ([150] * 300, [1024, 576])])
+def test_rows_of_fp8_pools(total, cols):
+    """They are bf16: few of them, and more than the caches keep, in lines that are whole."""
+    c = adapters.Case("bf16", np.arange(len(total)) % 4, total, 4, 264, cols, 16)
+    kv = torch.zeros(80 * 128, dtype=torch.uint8, device=DEV)
+    c.pool = B.Pool(*B.make_config(n_layers=1, n_q_heads=1, n_kv_heads=1, head_dim=128, kv_dtype=B.FP8, out_dtype=B.BF16, main_tokens=64, safety_tokens=16,
+                                   large_cap=16, boundaries=(16,), quantiles=((1, 2),), max_requests=8, k_pool=kv, v_pool=kv.clone()))
+    assert c.pool.odma_adapt_scratch_bytes(c.ad, len(c.items)) == c.scratch.numel()
+    c.run().check()
+
+
 @pytest.mark.parametrize("typ", ["bf16", "f32"])
 @pytest.mark.parametrize("rank", [8, 16, 24, 64, 72, 136])
 @pytest.mark.parametrize("rows", [FEW, MANY])

@@ -48,3 +48,14 @@ def test_adapt_rows_takes_what_the_header_says(runtime):  # noqa: F811
         adapt(p, ad=make(width=32768), xs=32768)
         assert refused(adapt, p, ad=make(width=32776), xs=32776) and refused(adapt, p, n=(1 << 27) + 1)
     """))
+
+
+def test_adapt_rows_of_fp8_pools_launch_as_those_of_bf16_pools(runtime):  # noqa: F811
+    """Their rows are bf16 too: the same bytes to a line and past the caches."""
+    run(runtime, textwrap.dedent(CALLS) + textwrap.dedent("""
+        p, q = make_pool(), make_pool(kv_dtype=B.FP8)
+        for n, items, cols, rank in ((100, 6, (64, 32), 16), (100000, 1590, (3584, 512, 512), 16), (100000, 1590, (64, 4544), 16), (100000, 1590, (4672,), 64),
+                                     (20000, 4000, (192,), 16), (9000, 8000, (320,), 8)):
+            one, two = (launched(lambda: adapt(pool, n=n, max_items=items, bs=sum(cols), ys=sum(cols), ad=make(part_cols=cols, rank=rank))) for pool in (p, q))
+            assert one == two, (one, two)
+    """))
