@@ -6,12 +6,12 @@
 // work-group, which add up in LDS, and, where a batch has few items, between work-groups, whose parts stay apart in scratch: nothing is
 // added up in an order that changes.  The second stages an item's h in LDS, parts added up and scaled, and takes 64 columns a wave at
 // a time.  In bf16, h enters as three bf16 parts, which hold all its 24 bits: two of them side by side fill the contraction of 32 that a rank of 16 would
-// half leave empty; from 24 ranks on one operand of up is multiplied by all three.  Two parts (16 bits of h) took 211.0 us and three take 212.3 for 43 340 rows of rank 16,
-// 337 and 344 for rank 64, 123 and 137 for 8 326 rows of rank 128, but where base and products cancel the rest of a sum was that of 16 bits.
+// half leave empty; from 24 ranks on one operand of up is multiplied by all three.  Two parts (16 bits of h) took 211 us and three take 213 for 43 340 rows of rank 16,
+// 338 and 349 for rank 64, 123 and 137 for 8 326 rows of rank 128, but where base and products cancel the rest of a sum was that of 16 bits.
 //
 // Both are bound by memory: adapters that occur once are the bytes of a decode step, x, base and y those of a prompt.  3584 channels, 4608 columns, rank 16 in
-// bf16: 43 340 rows of prompts 211 us (65 + 150 traced), 5.3 TB/s; 64 rows of as many adapters 11 us, a chain of loads that depend on one another (items, row
-// numbers, x, columns) around 33 MB.  Larger ranks are not: 41 423 rows of rank 64 331 us (209 for the bytes), whose groups of ranks read x three times and whose
+// bf16: 43 340 rows of prompts 213 us (66 + 156 traced), 5.2 TB/s; 64 rows of as many adapters 11.4 us, a chain of loads that depend on one another (items, row
+// numbers, x, columns) around 33 MB.  Larger ranks are not: 41 423 rows of rank 64 340 us (209 for the bytes), whose groups of ranks read x three times and whose
 // weights come from the L2 for every item.  Large products in fp32 reach a ninth of the rate (0.154 PFLOP/s): 2 084 rows of rank 64, 1000 to 1024 channels, 22 us
 // (5.1 for the bytes), one work-group on a compute unit, on 140 to 150 of them, with loads, 3.3 us of products, sums, loads and 3.4 us of products one behind the other.
 #pragma once

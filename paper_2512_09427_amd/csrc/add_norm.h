@@ -6,7 +6,7 @@
 //
 // Bound by memory: block, residual and gate are read once, the new residual and x written once; a row stays in registers from its
 // loads to its stores.  A row's channels are dealt out to the lanes of W waves in pieces of eight.  65 869 rows of 3584 channels in bf16 beside
-// a residual in fp32, both norms: 515 us, 5.5 TB/s (a copy of 1 GiB: 5.2); 256 rows 3.6 us, one row 2.2, which is a launch.
+// a residual in fp32, both norms: 515 us, 5.5 TB/s (a copy of 1 GiB: 5.2); 256 rows 3.7 us, one row 2.2, which is a launch.
 #pragma once
 
 #include "kernels_common.h"

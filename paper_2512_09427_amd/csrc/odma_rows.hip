@@ -62,11 +62,12 @@ void launch_add_norm(const AddNormArgs& a, int64_t n_cu, hipStream_t s) {
 // Both products in one launch (adapt_few_kernel) or in two.  Every work-group of the one forms h for itself: its matrix instructions (counted as bytes of
 // the ranks in bf16, in whole tiles of 16, four times as many for fp32) times the rounds of work-groups that the chip goes through must stay within what two launches
 // cost more, which grows with the rows, and within a most.  One and two, us a call, 3584 channels, 4608 columns in three parts (1024 in one), requests of one row / adapters:
-//   bf16, rank 16: 1 / 4 6.6 and 8.9, 64 / 64 11.0 and 15.8, 1 024 / 32 16.5 and 19.4, 4 096 / 32 42.3 and 43.4, 8 192 / 32 71 and 58
-//   bf16, rank 32: 1 / 4 7.7 and 9.4, 256 / 32 16.9 and 17.3, 2 048 / 32 29.4 and 30.3, 4 096 / 32 55.5 and 51.4
-//   bf16, rank 64: 1 / 4 12.1 and 10.0, 256 / 32 24.1 and 22.3 (13.4 and 16.2), 1 024 / 32 32.6 and 32.8 (14.4 and 18.9), 4 096 / 32 85 and 74 (32 and 31)
-//   fp32, rank 64: 1 / 4 28 and 14, 256 / 32 58 and 46 (30 and 26), 1 024 / 32 77 and 90 (30.7 and 31.3), 4 096 / 32 180 and 191, 8 192 / 32 322 and 266
-// other channels: bf16 208 / 3 of rank 64, 8 160 to 816 23.0 and 17.1; 15 / 15, 992 to 320 6.1 and 9.3; 4 132 rows of rank 16, 128 to 1072 8.0 and 13.4.
+//   bf16, rank 16: 1 / 4 7.0 and 9.9, 64 / 64 11.7 and 16.8, 1 024 / 32 17.2 and 20.6, 4 096 / 32 43.2 and 44.9, 8 192 / 32 73 and 59.5
+//   bf16, rank 32: 1 / 4 8.0 and 10.0, 256 / 32 17.6 and 18.1, 2 048 / 32 30.1 and 31.1, 4 096 / 32 56 and 52.7
+//   bf16, rank 64: 1 / 4 12.6 and 10.5, 256 / 32 25.1 and 23.2 (13.8 and 17.2), 1 024 / 32 33.2 and 34.5 (14.9 and 19.9), 4 096 / 32 87 and 75 (32.9 and 32.3)
+//   fp32, rank 64: 1 / 4 28.8 and 14.3, 256 / 32 59 and 46.5 (30 and 26.4), 1 024 / 32 78.5 and 90.5 (31.4 and 31.8), 4 096 / 32 180 and 192, 8 192 / 32 323 and 266
+// other channels: bf16 208 / 3 of rank 64, 8 160 to 816 23.2 and 17.6; 15 / 15 of rank 64, 992 to 320 7.1 and 9.9; 4 132 / 32 of rank 16, 128 to 1072 10.0 and 16.8.
+// (Figures below were taken when h had two parts in bf16; with three they are 1 to 4 % more on both sides.)
 constexpr int64_t ADAPT_FEW = 8192, ADAPT_FEW_WORK = 320 << 10, ADAPT_FEW_ROW = 3 << 10, ADAPT_FEW_MOST = 560 << 10, ADAPT_FEW_MOST_F32 = 6 << 20, ADAPT_FEW_CU = 256;
 // Work-groups that it is cut into, as far as the adapters that a batch may have let it be known.  Two share a compute unit with ranks up to 16: 64 / 64 as above
 // 11.0 us with 260 and 12.3 with 390, 256 / 32 9.1 with 360 and 11.4 with 160.  With more it is one; parts narrower than the others' runs of columns
@@ -81,6 +82,7 @@ constexpr int ADAPT_UP_WG = 1024;
 // beside 1024 columns 132 us with two and 153 with four.  Rows past the caches (shape.stream) where lines are whole, since two halves of a line that are
 // stored one by one cross the memory twice: 93 308 rows of 80 + 2 000 columns, rank 64, 434 us past them and 324 through them, of 64 + 2 048 columns
 // 263 and 277; 41 423 rows of 4 608 columns, rank 16, 219 and 245.
+// ADAPT_UP_WG stands for long calls there too: work-groups of 512 columns.
 // Of the first, groups of ranks of four neighbouring items on one XCD: 41 423 rows, three parts of rank 64, 332 us and 360 without.
 
 // Runs of 16 rows of the items, as many as there can be if the lists are of these rows, in eights

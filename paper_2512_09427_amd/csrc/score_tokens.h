@@ -12,7 +12,7 @@
 // in LDS, the bound is renewed as a row's read part doubles, and in the end those that are left are ranked by counting.  A list
 // that fills up all the same (ascending rows, equal ones) is cut down to its n_top largest, whose last is a bound too.
 //
-// Bound by memory for many rows (4 096 rows of 50 001 in fp32 5.9 TB/s, in bf16, where a byte brings twice the work, 4.9).  Few long rows are
+// Bound by memory for many rows (4 096 rows of 50 001 in fp32 5.9 TB/s, in bf16, where a byte brings twice the work, 5.1 to 5.3).  Few long rows are
 // cut into parts, a work-group each, whose states and largest a second launch joins.
 #pragma once
 
